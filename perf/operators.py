@@ -1,0 +1,367 @@
+"""The operators on logits and on packed weights, in plain form and through the binding's entry points.
+
+``listed()`` names eleven uses, ``draw(rng)`` gives more of the same ranges; ``prepare(case, seed)`` makes what a program
+holds before the call, ``run(state)`` is one pass, ``exact(case, seed)`` the same outputs in 64 bits from the definitions,
+``work(case)`` the bytes and operations that a pass cannot do without.
+
+Uses (``kind``):
+  score     log probabilities of given tokens, entropy and top alternatives, from a row of logits per token; with
+            ``grad`` also the gradient of the logits for given gradients of log probability and entropy
+  distill   loss against a teacher's top logits and a label, and the gradient of the student's logits
+  linear    tokens, rounded to 8 bits with a scale each, times weights held as the codec's packed 8-bit codes
+
+Definitions, per row of logits z with temperature T, m = max z, t = (z - m) / T, S = sum exp t:
+  log probability of i: t_i - log S;  entropy: log S - (sum t exp t) / S;  stats: {m, log S}
+  top alternatives: by z downwards, equal ones by index upwards
+  d z_j = (g ([j = i] - p_j) - h p_j (log p_j + entropy)) / T
+  a token below 0 is none: log probability 0, no gradient. A row of nothing but -inf: log probability -inf, entropy 0,
+  gradient 0.
+Distillation, teacher's list (index, logit) with absent slots -1: p = softmax(logit / T) over the list, q = softmax(z / T),
+  loss = a T^2 sum p (log p - log q_index) + (1 - a) (-log softmax(z)_label)
+  d z_j = scale (a T (q_j - sum p_k [index_k = j]) + (1 - a) (softmax(z)_j - [j = label])); a label below 0 is none
+Product: s = max |x| / 127 in 32 bits, x' = rint(x / s), weight = base + scale * code per bucket of a channel,
+  y = s * sum x' weight + bias
+"""
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+VOCAB = 50257  # the framework's GPT shapes
+CELLS = 8192 * VOCAB  # logits of the largest case
+
+
+def listed():
+    return [
+        # one decoded token of one user: float logits, the alternatives a client asks for
+        dict(name="score-one-token", kind="score", rows=1, vocab=VOCAB, pad=0, dtype="f32", top=20, temperature=0.8,
+             masked=0.0, grad=False),
+        # a serving batch whose grammar masks half of the vocabulary, one row masked whole
+        dict(name="score-batch", kind="score", rows=48, vocab=VOCAB, pad=47, dtype="bf16", top=8, temperature=1.0,
+             masked=0.5, grad=False),
+        # a teacher labels a long batch: its top 64 of every position
+        dict(name="score-teacher", kind="score", rows=4096, vocab=VOCAB, pad=0, dtype="f32", top=64, temperature=1.0,
+             masked=0.0, grad=False),
+        # a policy-gradient step: log probabilities and entropy, then their gradient
+        dict(name="score-train", kind="score", rows=4096, vocab=VOCAB, pad=0, dtype="bf16", top=0, temperature=1.0,
+             masked=0.0, grad=True),
+        # a small vocabulary and a short batch, all in 32 bits
+        dict(name="distill-small", kind="distill", rows=77, vocab=8191, pad=0, dtype="f32", top=20, temperature=1.0,
+             alpha=1.0),
+        # a training step's micro-batch at context 2048, softened targets and labels
+        dict(name="distill-step", kind="distill", rows=2048, vocab=VOCAB, pad=0, dtype="bf16", top=64, temperature=2.0,
+             alpha=0.5),
+        # four of them at once, rows padded to a multiple of 64
+        dict(name="distill-long", kind="distill", rows=8192, vocab=VOCAB, pad=47, dtype="bf16", top=32, temperature=2.0,
+             alpha=0.9),
+        # one token through the up-projection of the 1.3B model, a bucket per channel
+        dict(name="linear-one-token", kind="linear", m=1, n=8192, k=2048, bucket=2048, dtype="bf16", out="bf16", bias=True),
+        # sixteen users' tokens onto the vocabulary (tied embedding), two buckets per channel as the codec's default leaves it
+        dict(name="linear-head", kind="linear", m=16, n=VOCAB, k=2048, bucket=1024, dtype="bf16", out="f32", bias=False),
+        # odd sizes everywhere: channels of 1000 in padded buckets
+        dict(name="linear-odd", kind="linear", m=333, n=4093, k=1000, bucket=1024, dtype="f16", out="f16", bias=True),
+        # the down-projection of the 1.3B model over a long batch
+        dict(name="linear-long", kind="linear", m=8192, n=2048, k=8192, bucket=8192, dtype="bf16", out="bf16", bias=False),
+    ]
+
+
+def draw(rng):
+    def size(lo, hi):  # any integer, spread over its logarithm
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    kind = rng.choice(["score", "score", "distill", "distill", "linear", "linear"])
+    dtype = rng.choice(["f32", "bf16", "bf16", "f16"])
+    if kind != "linear":
+        vocab = rng.choice([VOCAB, size(1000, 131072)])
+        most = CELLS // vocab // (2 if dtype == "f32" else 1)
+        case = dict(kind=kind, vocab=vocab, pad=rng.choice([0, 0, -vocab % 64, rng.randrange(1, 200)]), dtype=dtype,
+                    temperature=rng.choice([1.0, 1.0, 0.7, 2.0]))
+        if kind == "score":
+            grad = rng.random() < 0.4
+            case.update(rows=size(1, max(1, most // 2)), top=rng.choice([0, 1, 8, 20, 64, 128]), grad=grad,
+                        masked=rng.choice([0.0, 0.0, 0.3, 0.95]))
+        else:
+            case.update(rows=size(1, most), top=rng.choice([1, 8, 20, 64, 128]), alpha=rng.choice([1.0, 0.9, 0.5]))
+        return case
+    buckets, bucket = rng.choice([(1, 0), (1, 0), (2, 1024), (4, 512), (3, 256), (8, 1024)])
+    k = bucket * buckets if bucket else rng.choice([768, 1024, 2048, 4096, 8192, size(64, 8192)])
+    while True:
+        m, n = size(1, 16384), rng.choice([768, 1024, 2048, 4096, 8192, VOCAB, size(64, 16384)])
+        if m * n * k <= 8192 * 2048 * 8192:
+            break
+    return dict(kind="linear", m=m, n=n, k=k, bucket=bucket or -(-k // 32) * 32, dtype=dtype,
+                out=rng.choice([dtype, dtype, "f32"]), bias=rng.random() < 0.5)
+
+
+def work(case):
+    if case["kind"] == "linear":
+        m, n, k = case["m"], case["n"], case["k"]
+        buckets = -(-k // case["bucket"])
+        return {"bytes": m * k * SIZE[case["dtype"]] + n * k + 8 * n * buckets + (4 * n if case["bias"] else 0)
+                + m * n * SIZE[case["out"]], "flops": 2.0 * m * n * k}
+    rows, cells = case["rows"], case["rows"] * case["vocab"] * SIZE[case["dtype"]]
+    both = case["kind"] == "distill" or case["grad"]
+    lists = rows * case["top"] * 8
+    return {"bytes": cells * (2 if both else 1) + lists + 24 * rows, "flops": (12.0 if both else 6.0) * rows * case["vocab"]}
+
+
+def _generator(seed):
+    return torch.Generator(device="cuda").manual_seed(int(seed))
+
+
+def _logits(case, gen):
+    """Logits of a trained model's spread, in rows that may be padded."""
+    rows, vocab, pitch = case["rows"], case["vocab"], case["vocab"] + case["pad"]
+    z = torch.empty((rows, pitch), dtype=DTYPES[case["dtype"]], device="cuda")
+    z.normal_(0.0, 3.0, generator=gen)
+    return z[:, :vocab]
+
+
+def prepare(case, seed):
+    gen = _generator(seed)
+    dev, f32 = "cuda", torch.float32
+    s = {"case": dict(case)}
+    if case["kind"] == "linear":
+        m, n, k, bucket = case["m"], case["n"], case["k"], case["bucket"]
+        buckets = -(-k // bucket)
+        x = torch.empty((m, k), dtype=f32, device=dev).normal_(0.0, 1.0, generator=gen)
+        x *= torch.empty((m, 1), dtype=f32, device=dev).uniform_(0.1, 4.0, generator=gen)
+        s["x"] = x.to(DTYPES[case["dtype"]])
+        # min-max codes of normal weights, every bucket of a channel on its own, slots past k zero
+        w = torch.empty((n, buckets * bucket), dtype=f32, device=dev).normal_(0.0, 0.02, generator=gen)
+        low = w.view(n, buckets, bucket).amin(2)
+        scale = (w.view(n, buckets, bucket).amax(2) - low) / 255.0
+        codes = ((w.view(n, buckets, bucket) - low[..., None]) / scale[..., None]).round_().clamp_(0, 255)
+        codes = codes.view(n, -1).to(torch.uint8)
+        codes[:, k:] = 0
+        s["codes"] = codes.view(torch.int32)
+        s["meta"] = torch.stack([low, scale], 2).contiguous()
+        s["bias"] = torch.empty(n, dtype=f32, device=dev).normal_(0.0, 0.1, generator=gen) if case["bias"] else None
+        s["y"] = torch.empty((m, n), dtype=DTYPES[case["out"]], device=dev)
+        wide = -(-k // 128) * 128
+        s["workspace"] = torch.empty(m * (wide + 4 + 4 * buckets) + 4096, dtype=torch.uint8, device=dev)
+        return s
+    rows, vocab, top = case["rows"], case["vocab"], case["top"]
+    s["logits"] = z = _logits(case, gen)
+    tokens = torch.randint(0, vocab, (rows,), device=dev, generator=gen)
+    tokens[torch.rand(rows, device=dev, generator=gen) < 0.05] = -100  # positions without a token
+    s["tokens"] = tokens
+    s["workspace"] = torch.empty(1 << 20, dtype=torch.uint8, device=dev)
+    if case["kind"] == "score":
+        if case["masked"]:
+            for r in range(0, rows, 1024):  # piece by piece, as the draws take 4 bytes each
+                part = z[r:r + 1024]
+                part.masked_fill_(torch.rand(part.shape, device=dev, generator=gen) < case["masked"], -math.inf)
+            if rows > 8:
+                z[rows // 2] = -math.inf
+        s["logprob"], s["entropy"] = (torch.empty(rows, dtype=f32, device=dev) for _ in range(2))
+        s["stats"] = torch.empty((rows, 2), dtype=f32, device=dev)
+        if top:
+            s["top_logprob"] = torch.empty((rows, top), dtype=f32, device=dev)
+            s["top_index"] = torch.empty((rows, top), dtype=torch.int32, device=dev)
+        if case["grad"]:
+            s["d_logprob"] = torch.empty(rows, dtype=f32, device=dev).normal_(0.0, 1.0, generator=gen)
+            s["d_entropy"] = torch.empty(rows, dtype=f32, device=dev).normal_(0.0, 0.1, generator=gen)
+            s["d_logits"] = torch.empty((rows, vocab), dtype=z.dtype, device=dev)
+        return s
+    # a list of distinct indices per row, its logits downwards, some rows' lists shorter
+    start = torch.randint(0, vocab, (rows, 1), device=dev, generator=gen)
+    index = (start + torch.arange(top, device=dev) * (vocab // top)) % vocab
+    length = torch.randint(max(1, top // 2), top + 1, (rows, 1), device=dev, generator=gen)
+    s["index"] = torch.where(torch.arange(top, device=dev) < length, index, -1).to(torch.int32)
+    logit = torch.empty((rows, top), dtype=f32, device=dev).normal_(6.0, 2.0, generator=gen)
+    s["logit"] = logit.sort(dim=1, descending=True).values
+    # the mean over the batch; in half precision with the loss scaled, as such training does
+    s["scale"] = torch.full((rows,), (1024.0 if case["dtype"] == "f16" else 1.0) / rows, dtype=f32, device=dev)
+    s["loss"] = torch.empty(rows, dtype=f32, device=dev)
+    s["d_logits"] = torch.empty((rows, vocab), dtype=z.dtype, device=dev)
+    return s
+
+
+def run(s):
+    kind = s["case"]["kind"]
+    if own:
+        return {"score": _own_score, "distill": _own_distill, "linear": _own_linear}[kind](s)
+    return {"score": _plain_score, "distill": _plain_distill, "linear": _plain_linear}[kind](s)
+
+
+# ---- through the framework ------------------------------------------------------------------------------------------
+def _own_score(s):
+    from paper_2302_02390_amd import binding as qb
+    case = s["case"]
+    out = {n: s[n] for n in ("logprob", "entropy", "stats", "top_logprob", "top_index") if n in s}
+    qb.qsdp_token_logprobs(s["logits"], s["tokens"], case["temperature"], s["logprob"], s["entropy"], s["stats"],
+                           s.get("top_logprob"), s.get("top_index"), s["workspace"])
+    if case["grad"]:
+        qb.qsdp_token_logprobs_backward(s["logits"], s["tokens"], case["temperature"], s["stats"], s["entropy"],
+                                        s["d_logprob"], s["d_entropy"], s["d_logits"])
+        out["d_logits"] = s["d_logits"]
+    return out
+
+
+def _own_distill(s):
+    from paper_2302_02390_amd import binding as qb
+    case = s["case"]
+    qb.qsdp_distill_loss(s["logits"], s["index"], s["logit"], s["tokens"], case["temperature"], case["alpha"], s["scale"],
+                         s["loss"], None, s["d_logits"], s["workspace"])
+    return {"loss": s["loss"], "d_logits": s["d_logits"]}
+
+
+def _own_linear(s):
+    from paper_2302_02390_amd import binding as qb
+    qb.qsdp_linear_codes(s["x"], s["codes"], s["meta"], s["case"]["n"], s["case"]["bucket"], s["bias"], s["y"],
+                         s["workspace"])
+    return {"y": s["y"]}
+
+
+# ---- plain forms ------------------------------------------------------------------------------------------------------
+def _shifted(z, temperature):
+    """m, t = (z - m) / T and log of the sum of exp t, per row; a row of nothing but -inf gets t = -inf."""
+    m = z.amax(1, keepdim=True)
+    t = (z - m.clamp(min=torch.finfo(z.dtype).min)) / temperature
+    e = t.exp()
+    return m, t, e, e.sum(1, keepdim=True)
+
+
+def _plain_score(s):
+    case = s["case"]
+    z = s["logits"].float()
+    tokens, temperature = s["tokens"], case["temperature"]
+    m, t, e, total = _shifted(z, temperature)
+    log_total = total.log()
+    empty = total == 0
+    given = tokens >= 0
+    at = tokens.clamp(min=0)[:, None]
+    logprob = torch.where(empty, -math.inf, t.gather(1, at) - log_total)[:, 0]
+    mean = (e * t.clamp(min=-200.0)).sum(1, keepdim=True) / total
+    entropy = torch.where(empty, 0.0, log_total - mean)
+    out = {"logprob": torch.where(given, logprob, 0.0), "entropy": entropy[:, 0], "stats": torch.cat([m, log_total], 1)}
+    if case["top"]:
+        bits = (z + 0.0).view(torch.int32)
+        key = torch.where(bits < 0, bits ^ 0x7FFFFFFF, bits).to(torch.int64) << 32
+        key += torch.arange(0xFFFFFFFF, 0xFFFFFFFF - z.shape[1], -1, device=z.device)
+        index = 0xFFFFFFFF - (key.topk(case["top"], 1).values & 0xFFFFFFFF)
+        out["top_logprob"] = torch.where(empty, -math.inf, t.gather(1, index) - log_total)
+        out["top_index"] = index.to(torch.int32)
+    if case["grad"]:
+        p = torch.where(empty, 0.0, e / total)
+        h = s["d_entropy"][:, None]
+        d = -p * (s["d_logprob"] * given)[:, None] - h * p * ((t - log_total).clamp(min=-200.0) + entropy)
+        d.scatter_add_(1, at, torch.where(empty[:, 0] | ~given, 0.0, s["d_logprob"])[:, None])
+        out["d_logits"] = torch.where(empty, 0.0, d / temperature).to(s["logits"].dtype)
+    return out
+
+
+def _plain_distill(s):
+    case = s["case"]
+    z = s["logits"].float()
+    alpha, temperature, vocab = case["alpha"], case["temperature"], case["vocab"]
+    present = (s["index"] >= 0) & (s["index"] < vocab)
+    index = torch.where(present, s["index"], 0).long()
+    _, u, f, mass = _shifted(torch.where(present, s["logit"], -math.inf), temperature)
+    log_p = u - mass.log()
+    p = f / mass
+    m, t, e, total = _shifted(z, temperature)
+    log_q = t.gather(1, index) - total.log()
+    kl = torch.where(p > 0, p * (log_p - log_q), 0.0).sum(1)
+    d = alpha * temperature * e / total
+    d.scatter_add_(1, index, -alpha * temperature * p)
+    loss = alpha * temperature * temperature * kl
+    if alpha < 1.0:
+        given = s["tokens"] >= 0
+        at = s["tokens"].clamp(min=0)[:, None]
+        _, t, e, total = _shifted(z, 1.0)
+        loss = loss - (1 - alpha) * torch.where(given, (t.gather(1, at) - total.log())[:, 0], 0.0)
+        d += ((1 - alpha) * given)[:, None] * e / total
+        d.scatter_add_(1, at, -((1 - alpha) * given)[:, None])
+    return {"loss": loss, "d_logits": (d * s["scale"][:, None]).to(s["logits"].dtype)}
+
+
+def _plain_linear(s):
+    case = s["case"]
+    n, k, bucket = case["n"], case["k"], case["bucket"]
+    x = s["x"].float()
+    scale = x.abs().amax(1, keepdim=True) / 127.0
+    q = torch.where(scale > 0, (x / scale).round(), 0.0).clamp(-127, 127)
+    codes = s["codes"].view(torch.uint8).view(n, -1, bucket).float()
+    w = (codes * s["meta"][..., 1:] + s["meta"][..., :1]).view(n, -1)[:, :k]
+    y = (q @ w.t()) * scale
+    if s["bias"] is not None:
+        y = y + s["bias"]
+    return {"y": y.to(s["y"].dtype)}
+
+
+# ---- in 64 bits -------------------------------------------------------------------------------------------------------
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["kind"] == "linear":
+        x32 = s["x"].to(torch.float32)
+        scale = (x32.double().abs().amax(1) / 127.0).float()  # held in 32 bits by definition, and so is the quotient
+        q = torch.nan_to_num(torch.round(x32 / scale[:, None])).double()
+        n, k, bucket = case["n"], case["k"], case["bucket"]
+        y = torch.zeros((case["m"], n), dtype=torch.float64, device=q.device)
+        for b, lo in enumerate(range(0, k, bucket)):
+            hi = min(lo + bucket, k)
+            c = s["codes"].view(torch.uint8)[:, lo:hi].double()
+            meta = s["meta"][:, b].double()
+            y += q[:, lo:hi].contiguous() @ (meta[:, :1] + meta[:, 1:] * c).t().contiguous()
+        y *= scale.double()[:, None]
+        return {"y": y + s["bias"].double() if s["bias"] is not None else y}
+    parts = [(_exact_score if case["kind"] == "score" else _exact_distill)(s, r, min(r + 512, case["rows"]))
+             for r in range(0, case["rows"], 512)]
+    return {name: None if parts[0][name] is None else torch.cat([p[name] for p in parts]) for name in parts[0]}
+
+
+def _exact_score(s, lo, hi):
+    case = s["case"]
+    z = s["logits"][lo:hi].double()
+    tau, token = case["temperature"], s["tokens"][lo:hi]
+    lse = torch.logsumexp(z / tau, 1)
+    none = torch.isinf(lse)
+    log_p = torch.where(none[:, None], -math.inf, z / tau - torch.where(none, 0.0, lse)[:, None])
+    p = log_p.exp()
+    info = torch.where(p > 0, p * log_p, 0.0)
+    entropy = -info.sum(1)
+    rows = torch.arange(hi - lo, device=z.device)
+    at = torch.clamp(token, min=0)
+    out = {"logprob": torch.where(token >= 0, log_p[rows, at], 0.0), "entropy": entropy,
+           "stats": torch.stack([z.max(1).values, torch.where(none, -math.inf, lse - z.max(1).values / tau)], 1)}
+    if case["top"]:
+        # equal logits have equal log probabilities, so the order among them does not show here
+        out["top_logprob"] = log_p.topk(case["top"], 1).values
+        out["top_index"] = None
+    if case["grad"]:
+        g, h = s["d_logprob"][lo:hi].double() * (token >= 0) * ~none, s["d_entropy"][lo:hi].double()
+        d = -g[:, None] * p - h[:, None] * (info + p * entropy[:, None])
+        d[rows, at] += g
+        out["d_logits"] = d / tau
+    return out
+
+
+def _exact_distill(s, lo, hi):
+    case = s["case"]
+    z = s["logits"][lo:hi].double()
+    tau, alpha, vocab = case["temperature"], case["alpha"], case["vocab"]
+    index, token = s["index"][lo:hi].long(), s["tokens"][lo:hi]
+    rows = torch.arange(hi - lo, device=z.device)
+    target = torch.zeros((hi - lo, vocab + 1), dtype=torch.float64, device=z.device)
+    teacher = s["logit"][lo:hi].double() / tau
+    absent = (index < 0) | (index >= vocab)
+    p = torch.softmax(teacher.masked_fill(absent, -math.inf), 1)
+    target.scatter_add_(1, torch.where(absent, vocab, index), p)
+    target = target[:, :vocab]
+    log_q = z / tau - torch.logsumexp(z / tau, 1, keepdim=True)
+    loss = alpha * tau ** 2 * (torch.special.xlogy(target, target) - target * log_q).sum(1)
+    d = alpha * tau * (log_q.exp() - target)
+    if alpha < 1.0:
+        log_1 = z - torch.logsumexp(z, 1, keepdim=True)
+        given = (token >= 0).double()
+        at = torch.clamp(token, min=0)
+        loss -= (1 - alpha) * given * log_1[rows, at]
+        hard = log_1.exp()
+        hard[rows, at] -= 1.0
+        d += (1 - alpha) * given[:, None] * hard
+    return {"loss": loss, "d_logits": d * s["scale"][lo:hi].double()[:, None]}
