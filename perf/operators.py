@@ -149,8 +149,8 @@ def prepare(case, seed):
     tokens = torch.randint(0, vocab, (rows,), device=dev, generator=gen)
     tokens[torch.rand(rows, device=dev, generator=gen) < 0.05] = -100  # positions without a token
     s["tokens"] = tokens
-    s["workspace"] = torch.empty(1 << 20, dtype=torch.uint8, device=dev)
     if case["kind"] == "score":
+        s["workspace"] = torch.empty(1 << 20, dtype=torch.uint8, device=dev)
         if case["masked"]:
             for r in range(0, rows, 1024):  # piece by piece, as the draws take 4 bytes each
                 part = z[r:r + 1024]
@@ -206,7 +206,7 @@ def _own_distill(s):
     from paper_2302_02390_amd import binding as qb
     case = s["case"]
     qb.qsdp_distill_loss(s["logits"], s["index"], s["logit"], s["tokens"], case["temperature"], case["alpha"], s["scale"],
-                         s["loss"], None, s["d_logits"], s["workspace"])
+                         s["loss"], None, s["d_logits"])
     return {"loss": s["loss"], "d_logits": s["d_logits"]}
 
 
