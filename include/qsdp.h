@@ -595,6 +595,114 @@ int qsdp_recv_adamw_step_segmented(float* x, float* m, float* v, const qsdp_segm
                                    float delta, uint64_t seed, uint32_t flags, uint32_t* wcodes,
                                    float* wmeta, uint64_t* n_saturated, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators on logits and on packed weights: what a run that trains or serves quantized weights
+ * does next to the codec. Conventions as above but for alignment: matrices of logits, tokens and
+ * outputs need the alignment of their elements only, 16 bytes are needed where said. A matrix is
+ * rows of consecutive elements, `row_stride` elements apart (at least the row's length; not looked
+ * at for a single row). Formats QSDP_F32, QSDP_BF16, QSDP_F16 in and out, binary32 (or exact whole
+ * numbers) inside, one rounding at the end. No rows (rows or m = 0): QSDP_OK, nothing is done.
+ * Rows and lengths are below 2^31; infinities and NaN are allowed here, with the results stated.
+ * ---------------------------------------------------------------------------------------------
+ *
+ * Log probabilities of given tokens, entropy and top alternatives of every row z of logits. With
+ * m = max z, t = (z - m) / temperature, S = sum exp(t):
+ *   logprob[r]   t[tokens[r]] - log S; 0 where tokens[r] < 0 (no token), NaN where it is >= vocab
+ *   entropy[r]   log S - (sum t exp(t)) / S
+ *   stats[2r..]  {m, log S}, what the gradient needs; m / temperature + log S is the row's
+ *                log-sum-exp
+ *   top_logprob, top_index  [rows, top]: the `top` largest logits downwards, equal ones (0 and -0
+ *                among them) by index upwards, a NaN above all; t[i] - log S and i. top <= 128, <= vocab
+ * logprob, entropy and stats are each left out where NULL; tokens may be NULL where logprob is.
+ * A masked entry is -inf (or the format's lowest value) and has probability 0. A row of nothing
+ * but -inf: logprob -inf, entropy 0, stats {-inf, -inf}, gradient 0. A row with a NaN or +inf:
+ * NaN in every result but the order of its alternatives.
+ *   workspace    16-byte aligned; of qsdp_token_logprobs_bytes bytes it lets a call of few rows
+ *                share each row among workgroups. Less or none is allowed and slower. Its contents
+ *                need no preparation and are not kept.
+ */
+size_t qsdp_token_logprobs_bytes(uint64_t rows, uint64_t vocab, int top);
+int qsdp_token_logprobs(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab,
+                        uint64_t row_stride, const int64_t* tokens, float temperature, int top,
+                        float* logprob, float* entropy, float* stats, float* top_logprob,
+                        int32_t* top_index, void* workspace, uint64_t workspace_bytes,
+                        void* stream);
+
+/*
+ * The gradient of the logits for given gradients g of logprob and h of entropy (either may be
+ * NULL; stats, and with h the entropy, as qsdp_token_logprobs gave them):
+ *   d_logits[r, j] = (g ([j = tokens[r]] - p_j) - h p_j (log p_j + entropy)) / temperature
+ * in the format of the logits, which d_logits may overwrite (same pointer and stride). A row
+ * without a token has no part from g.
+ */
+int qsdp_token_logprobs_backward(const void* logits, qsdp_dtype dtype, uint64_t rows,
+                                 uint64_t vocab, uint64_t row_stride, const int64_t* tokens,
+                                 float temperature, const float* stats, const float* entropy,
+                                 const float* d_logprob, const float* d_entropy, void* d_logits,
+                                 uint64_t d_row_stride, void* stream);
+
+/*
+ * Distillation from a teacher's top logits. Row r's list: teacher_index and teacher_logit
+ * [rows, top] (log probabilities serve as logits); slots whose index is outside [0, vocab) are
+ * absent, an index given twice counts twice. p = softmax of the list at the temperature, q =
+ * softmax(z / temperature) over the whole vocabulary:
+ *   loss[r] = alpha temperature^2 sum_k p_k (log p_k - log q_{i_k})
+ *             + (1 - alpha) (-log softmax(z)[labels[r]])
+ *   d_logits[r, j] = row_scale[r] (alpha temperature (q_j - sum_{k: i_k = j} p_k)
+ *             + (1 - alpha) (softmax(z)_j - [j = labels[r]]))
+ * A list without present slots (or all at -inf) drops the first term, a label below 0 the second;
+ * a label >= vocab gives a NaN loss. With d_logits the gradient comes out of the same pass over
+ * the logits (row_scale: the gradient of the total by loss[r], 1 where NULL); without it, or where
+ * that gradient is not known yet, `stats` ([rows, 3], nullable: maximum, logs of the sums at the
+ * temperature and at 1) goes to qsdp_distill_loss_backward with it as d_loss. d_logits may
+ * overwrite the logits. labels may be NULL for alpha = 1, the list for alpha = 0 (top = 0).
+ * A row of nothing but -inf: loss +inf if anything is asked of it, gradient 0. top <= 128.
+ */
+int qsdp_distill_loss(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab,
+                      uint64_t row_stride, const int32_t* teacher_index,
+                      const float* teacher_logit, int top, const int64_t* labels,
+                      float temperature, float alpha, const float* row_scale, float* loss,
+                      float* stats, void* d_logits, uint64_t d_row_stride, void* stream);
+int qsdp_distill_loss_backward(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab,
+                               uint64_t row_stride, const int32_t* teacher_index,
+                               const float* teacher_logit, int top, const int64_t* labels,
+                               float temperature, float alpha, const float* stats,
+                               const float* d_loss, void* d_logits, uint64_t d_row_stride,
+                               void* stream);
+
+/*
+ * Products with weights held as packed 8-bit codes (qsdp_quantize_weight and the steps, bits = 8):
+ * y[m, n] = x W^T + bias, W [n, k] with w = base + scale * code by bucket. A channel (row of W)
+ * is whole buckets: k a multiple of `bucket` (the flat matrix as one vector), or every channel
+ * encoded as a tensor of its own (segmented calls; k <= bucket: one bucket, the rest of its slots
+ * unused). So wcodes holds ceil(k / bucket) * bucket bytes per channel, wmeta ceil(k / bucket)
+ * pairs. bucket is a multiple of 128 where a channel has more than one; k <= 2^20.
+ *
+ * qsdp_quantize_tokens rounds each row of x to 8 bits: s = max |x| * (1/127), q = x / s to the
+ * nearest whole number (binary32: product with the rounded 1/127, IEEE division; all zero for a
+ * row of zeros).
+ *   codes  out  int8[m, ceil(k / 128) * 128], 16-byte aligned: q, zeros past k
+ *   scale  out  float[m]: s; NaN for a row with a NaN or an infinity
+ *   sums   out  float[m, ceil(k / bucket)]: sum of q over each bucket (exact)
+ * qsdp_matmul_codes multiplies them: with D = sum q (code - 128) per bucket, exact in 32 bits,
+ *   y = s * sum_buckets (scale D + (base + 128 scale) sums) + bias
+ *   wcodes 16-byte, wmeta 8-byte aligned; bias nullable float[n]
+ * qsdp_linear_codes does both; workspace: qsdp_tokens_bytes(m, k, bucket) bytes, 16-byte aligned.
+ */
+size_t qsdp_tokens_bytes(uint64_t m, uint64_t k, int bucket);
+int qsdp_quantize_tokens(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k,
+                         uint64_t row_stride, int bucket, int8_t* codes, float* scale,
+                         float* sums, void* stream);
+int qsdp_matmul_codes(const int8_t* codes, const float* scale, const float* sums, uint64_t m,
+                      const uint32_t* wcodes, const float* wmeta, uint64_t n, uint64_t k,
+                      int bucket, const float* bias, qsdp_dtype out_dtype, void* y,
+                      uint64_t y_row_stride, void* stream);
+int qsdp_linear_codes(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k,
+                      uint64_t row_stride, const uint32_t* wcodes, const float* wmeta, uint64_t n,
+                      int bucket, const float* bias, qsdp_dtype out_dtype, void* y,
+                      uint64_t y_row_stride, void* workspace, uint64_t workspace_bytes,
+                      void* stream);
+
 #ifdef __cplusplus
 }
 #endif

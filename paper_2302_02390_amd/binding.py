@@ -93,6 +93,20 @@ _SIGNATURES = {
     "qsdp_quantize_levels_segmented": (_i32,
         [_vp, _vp, _u32, _u64, _i32, _i32, _vp, _i32, _u64, _u64, _vp, _vp, _vp]),
     "qsdp_dequantize_levels_segmented": (_i32, [_vp, _vp, _vp, _u32, _u64, _i32, _i32, _vp, _i32, _vp, _vp]),
+    "qsdp_token_logprobs_bytes": (C.c_size_t, [_u64, _u64, _i32]),
+    "qsdp_token_logprobs": (_i32,
+        [_vp, _i32, _u64, _u64, _u64, _vp, _f32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _u64, _vp]),
+    "qsdp_token_logprobs_backward": (_i32,
+        [_vp, _i32, _u64, _u64, _u64, _vp, _f32, _vp, _vp, _vp, _vp, _vp, _u64, _vp]),
+    "qsdp_distill_loss": (_i32,
+        [_vp, _i32, _u64, _u64, _u64, _vp, _vp, _i32, _vp, _f32, _f32, _vp, _vp, _vp, _vp, _u64, _vp]),
+    "qsdp_distill_loss_backward": (_i32,
+        [_vp, _i32, _u64, _u64, _u64, _vp, _vp, _i32, _vp, _f32, _f32, _vp, _vp, _vp, _u64, _vp]),
+    "qsdp_tokens_bytes": (C.c_size_t, [_u64, _u64, _i32]),
+    "qsdp_quantize_tokens": (_i32, [_vp, _i32, _u64, _u64, _u64, _i32, _vp, _vp, _vp, _vp]),
+    "qsdp_matmul_codes": (_i32, [_vp, _vp, _vp, _u64, _vp, _vp, _u64, _u64, _i32, _vp, _i32, _vp, _u64, _vp]),
+    "qsdp_linear_codes": (_i32,
+        [_vp, _i32, _u64, _u64, _u64, _vp, _vp, _u64, _i32, _vp, _i32, _vp, _u64, _vp, _u64, _vp]),
 }
 EXPORTS = tuple(_SIGNATURES)
 # Where the entry points take pointers, the stream left out.
@@ -835,6 +849,170 @@ def qsdp_fused_adamw_step_opts(x, g, m, v, lr, beta1, beta2, eps, weight_decay, 
     """The same with AdamW (moments m, v in float32, updated in place) between the two quantizers."""
     _step_opts("qsdp_fused_adamw_step_opts", x, g, lr, wbits, gbits, bucket, delta, seed, index_offset, flags, segs,
                x16, seed_increment, wcodes, wmeta, n_saturated, (m, v, beta1, beta2, eps, weight_decay, bias1, bias2))
+
+
+# ---- operators on logits and on packed weights ------------------------------------------------------------------
+def _matrix(t):
+    """The format and the distance of the rows of a 2-D GPU tensor with contiguous rows in one of the three formats."""
+    dt = _DTYPES.get(t.dtype)
+    if dt is None:
+        raise TypeError("expected float32, bfloat16 or float16")
+    _is_rows(t, t.dtype)
+    return dt, t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _per_row(rows, dtype, *tensors):
+    for t in tensors:
+        if t is not None:
+            _is(t, dtype)
+            if t.numel() != rows:
+                raise ValueError(f"{t.numel()} values for {rows} rows")
+
+
+def _like_logits(logits, d_logits):
+    if d_logits.dtype != logits.dtype or d_logits.shape != logits.shape:
+        raise ValueError("the gradient has the logits' format and shape")
+    return _matrix(d_logits)[1]
+
+
+def _bytes_of(workspace):
+    if workspace is None:
+        return 0
+    _is(workspace, torch.uint8)
+    return workspace.numel()
+
+
+def token_logprobs_bytes(rows, vocab, top):
+    """Bytes of workspace with which qsdp_token_logprobs shares each of few rows among workgroups."""
+    return int(lib().qsdp_token_logprobs_bytes(int(rows), int(vocab), int(top)))
+
+
+def qsdp_token_logprobs(logits, tokens, temperature, logprob, entropy=None, stats=None, top_logprob=None, top_index=None,
+                        workspace=None):
+    """logits [rows, vocab] in float32, bfloat16 or float16; tokens int64[rows]; logprob, entropy float32[rows]; stats
+    float32[rows, 2]; top_logprob float32 and top_index int32 [rows, top]; workspace uint8 or None."""
+    dt, stride = _matrix(logits)
+    rows, vocab = logits.shape
+    _per_row(rows, torch.int64, tokens)
+    _per_row(rows, torch.float32, logprob, entropy)
+    _per_row(2 * rows, torch.float32, stats)
+    top = 0
+    if (top_logprob is None) != (top_index is None):
+        raise ValueError("top_logprob and top_index come together")
+    if top_index is not None:
+        _is(top_logprob, torch.float32); _is(top_index, torch.int32)
+        if top_index.dim() != 2 or top_index.shape[0] != rows or top_logprob.shape != top_index.shape:
+            raise ValueError("top_logprob and top_index must be [rows, top]")
+        top = top_index.shape[1]
+    _launch(logits, "qsdp_token_logprobs", logits, dt, rows, vocab, stride, tokens, temperature, top, logprob, entropy,
+            stats, top_logprob, top_index, workspace, _bytes_of(workspace))
+
+
+def qsdp_token_logprobs_backward(logits, tokens, temperature, stats, entropy, d_logprob, d_entropy, d_logits):
+    """d_logits: as logits, which it may be; d_logprob or d_entropy may be None."""
+    dt, stride = _matrix(logits)
+    rows, vocab = logits.shape
+    _per_row(rows, torch.int64, tokens)
+    _per_row(rows, torch.float32, entropy, d_logprob, d_entropy)
+    _per_row(2 * rows, torch.float32, stats)
+    _launch(logits, "qsdp_token_logprobs_backward", logits, dt, rows, vocab, stride, tokens, temperature, stats, entropy,
+            d_logprob, d_entropy, d_logits, _like_logits(logits, d_logits))
+
+
+def _teacher_list(rows, index, logit):
+    if index is None and logit is None:
+        return 0
+    _is(index, torch.int32); _is(logit, torch.float32)
+    if index.dim() != 2 or index.shape[0] != rows or index.shape != logit.shape:
+        raise ValueError("teacher_index and teacher_logit must be [rows, top]")
+    return index.shape[1]
+
+
+def qsdp_distill_loss(logits, teacher_index, teacher_logit, labels, temperature, alpha, row_scale, loss, stats=None,
+                      d_logits=None):
+    """logits [rows, vocab]; teacher_index int32, teacher_logit float32 [rows, top] (None with alpha 0); labels int64[rows]
+    (None with alpha 1); row_scale (or None), loss float32[rows]; stats float32[rows, 3]; d_logits: as logits, which it may
+    be."""
+    dt, stride = _matrix(logits)
+    rows, vocab = logits.shape
+    top = _teacher_list(rows, teacher_index, teacher_logit)
+    _per_row(rows, torch.int64, labels)
+    _per_row(rows, torch.float32, row_scale, loss)
+    _per_row(3 * rows, torch.float32, stats)
+    _launch(logits, "qsdp_distill_loss", logits, dt, rows, vocab, stride, teacher_index, teacher_logit, top, labels,
+            temperature, alpha, row_scale, loss, stats, d_logits, 0 if d_logits is None else _like_logits(logits, d_logits))
+
+
+def qsdp_distill_loss_backward(logits, teacher_index, teacher_logit, labels, temperature, alpha, stats, d_loss, d_logits):
+    """The gradient alone, for d_loss float32[rows]; stats as qsdp_distill_loss gave them."""
+    dt, stride = _matrix(logits)
+    rows, vocab = logits.shape
+    top = _teacher_list(rows, teacher_index, teacher_logit)
+    _per_row(rows, torch.int64, labels)
+    _per_row(rows, torch.float32, d_loss)
+    _per_row(3 * rows, torch.float32, stats)
+    _launch(logits, "qsdp_distill_loss_backward", logits, dt, rows, vocab, stride, teacher_index, teacher_logit, top, labels,
+            temperature, alpha, stats, d_loss, d_logits, _like_logits(logits, d_logits))
+
+
+def tokens_bytes(m, k, bucket):
+    """Bytes of workspace that qsdp_linear_codes needs."""
+    return int(lib().qsdp_tokens_bytes(int(m), int(k), int(bucket)))
+
+
+def _channels_ok(wcodes, wmeta, n, k, bucket, bias):
+    """The packed weights hold n channels of whole buckets. An invalid bucket is left to the library to report."""
+    _is(wcodes, torch.int32); _is(wmeta, torch.float32)
+    if bucket > 0:
+        buckets = -(-k // bucket)
+        _need(wcodes, -(-n * buckets * bucket // 4), "codes")
+        _need(wmeta, 2 * n * buckets, "meta")
+    if bias is not None:
+        _is(bias, torch.float32)
+        if bias.numel() != n:
+            raise ValueError(f"{bias.numel()} bias values for {n} channels")
+
+
+def qsdp_quantize_tokens(x, bucket, codes, scale, sums):
+    """x [m, k]; codes int8[m, k rounded up to 128], scale float32[m], sums float32[m, buckets of a channel]."""
+    dt, stride = _matrix(x)
+    m, k = x.shape
+    _is(codes, torch.int8); _is(sums, torch.float32)
+    _per_row(m, torch.float32, scale)
+    if bucket > 0:
+        _need(codes, m * (-(-k // 128) * 128), "codes")
+        _need(sums, m * -(-k // bucket), "sums")
+    _launch(x, "qsdp_quantize_tokens", x, dt, m, k, stride, bucket, codes, scale, sums)
+
+
+def qsdp_matmul_codes(codes, scale, sums, wcodes, wmeta, n, k, bucket, bias, y):
+    """y [m, n] in any of the three formats, from qsdp_quantize_tokens' outputs and packed 8-bit weights [n, k]."""
+    dt, stride = _matrix(y)
+    m = y.shape[0]
+    _is(codes, torch.int8); _is(sums, torch.float32)
+    _per_row(m, torch.float32, scale)
+    _channels_ok(wcodes, wmeta, n, k, bucket, bias)
+    if bucket > 0:
+        _need(codes, m * (-(-k // 128) * 128), "codes")
+        _need(sums, m * -(-k // bucket), "sums")
+    if y.shape[1] != n:
+        raise ValueError(f"y has {y.shape[1]} columns for {n} channels")
+    _launch(y, "qsdp_matmul_codes", codes, scale, sums, m, wcodes, wmeta, n, k, bucket, bias, dt, y, stride)
+
+
+def qsdp_linear_codes(x, wcodes, wmeta, n, bucket, bias, y, workspace=None):
+    """y [m, n] = x [m, k] W^T + bias with packed 8-bit weights W [n, k]. Without a workspace (uint8, tokens_bytes) one is
+    taken from torch's allocator for the call."""
+    dt, stride = _matrix(x)
+    out, y_stride = _matrix(y)
+    m, k = x.shape
+    if y.shape[0] != m or y.shape[1] != n:
+        raise ValueError(f"y is {tuple(y.shape)}, not {(m, n)}")
+    _channels_ok(wcodes, wmeta, n, k, bucket, bias)
+    if workspace is None:
+        workspace = torch.empty(tokens_bytes(m, k, bucket), dtype=torch.uint8, device=x.device)
+    _launch(x, "qsdp_linear_codes", x, dt, m, k, stride, wcodes, wmeta, n, bucket, bias, out, y, y_stride, workspace,
+            _bytes_of(workspace))
 
 
 def _devices_ok(name, args, kwargs):

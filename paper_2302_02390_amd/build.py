@@ -38,6 +38,10 @@ TILE_SHAPES = [(1, 2), (4, 2), (1, 4), (1, 6), (1, 8), (4, 4), (4, 6), (4, 8)]
 # shapes of the level fit: (values per lane, waves per batch), for buckets of up to 64 * values * waves
 FIT_SHAPES = [(2, 1), (4, 1), (8, 1), (16, 1), (32, 1), (16, 4), (16, 8)]
 
+# the operators on logits and on packed weights (csrc/lm): masks are infinities there, and a NaN has to come through
+LM_SOURCES = ["lm_api", "lm_rows", "lm_linear"]
+LM_FLAGS = ["-fhonor-nans"]
+
 
 def _units():
     units = [("qsdp_api.o", "qsdp_api.hip", [])]
@@ -51,6 +55,8 @@ def _units():
         units.append((f"qsdp_tile_{w}_{r}.o", "qsdp_tile_inst.hip", [f"-DQSDP_TILE_W={w}", f"-DQSDP_TILE_R={r}"]))
     for v, w in FIT_SHAPES:
         units.append((f"qsdp_fit_{v}_{w}.o", "qsdp_fit_inst.hip", [f"-DQSDP_FIT_V={v}", f"-DQSDP_FIT_W={w}"]))
+    for name in LM_SOURCES:
+        units.append((f"{name}.o", os.path.join("lm", f"{name}.hip"), LM_FLAGS))
     return units
 
 

@@ -123,7 +123,8 @@ const Entry entries[] = {
     E(qsdp_fused_step_segmented), E(qsdp_fused_step_segmented_mp), E(qsdp_dequantize_segmented),
     E(qsdp_fused_adamw_step_segmented), E(qsdp_fused_step_codes_segmented), E(qsdp_recv_step_segmented),
     E(qsdp_recv_adamw_step_segmented), E(qsdp_fit_levels_segmented), E(qsdp_quantize_levels_segmented),
-    E(qsdp_dequantize_levels_segmented)};
+    E(qsdp_dequantize_levels_segmented), E(qsdp_token_logprobs), E(qsdp_token_logprobs_backward), E(qsdp_distill_loss),
+    E(qsdp_distill_loss_backward), E(qsdp_quantize_tokens), E(qsdp_matmul_codes), E(qsdp_linear_codes)};
 #undef E
 
 // Call sites name their entry points by literals, which Python interns, so the object itself is compared.
