@@ -64,7 +64,7 @@ int qsdp_token_logprobs(const void* logits, qsdp_dtype dtype, uint64_t rows, uin
     if (!aligned(logits, width(dtype)) || !aligned(tokens, 8) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
         !aligned(stats, 4) || !aligned(top_logprob, 4) || !aligned(top_index, 4) || !aligned(workspace, 16))
         return QSDP_EALIGN;
-    const ScoreParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature}, tokens, top, logprob, entropy, stats,
+    const ScoreParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, tokens, top, logprob, entropy, stats,
                            top_logprob, top_index};
     return status_of(launch_score(dtype, p, static_cast<hipStream_t>(stream)));
 }
@@ -80,7 +80,7 @@ int qsdp_token_logprobs_backward(const void* logits, qsdp_dtype dtype, uint64_t 
     if (!aligned(logits, width(dtype)) || !aligned(tokens, 8) || !aligned(stats, 4) || !aligned(entropy, 4) ||
         !aligned(d_logprob, 4) || !aligned(d_entropy, 4) || !aligned(d_logits, width(dtype)))
         return QSDP_EALIGN;
-    const ScoreBackwardParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature}, tokens, stats, entropy,
+    const ScoreBackwardParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, tokens, stats, entropy,
                                    d_logprob, d_entropy, d_logits, d_row_stride};
     return status_of(launch_score_backward(dtype, p, static_cast<hipStream_t>(stream)));
 }
@@ -96,7 +96,7 @@ int qsdp_distill_loss(const void* logits, qsdp_dtype dtype, uint64_t rows, uint6
     if (!aligned(logits, width(dtype)) || !aligned(teacher_index, 4) || !aligned(teacher_logit, 4) || !aligned(labels, 8) ||
         !aligned(row_scale, 4) || !aligned(loss, 4) || !aligned(stats, 4) || !aligned(d_logits, width(dtype)))
         return QSDP_EALIGN;
-    const DistillParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature}, teacher_index, teacher_logit, top,
+    const DistillParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, teacher_index, teacher_logit, top,
                              labels, temperature, alpha, row_scale, nullptr, loss, stats, d_logits, d_row_stride};
     return status_of(launch_distill(dtype, p, static_cast<hipStream_t>(stream)));
 }
@@ -112,7 +112,7 @@ int qsdp_distill_loss_backward(const void* logits, qsdp_dtype dtype, uint64_t ro
     if (!aligned(logits, width(dtype)) || !aligned(teacher_index, 4) || !aligned(teacher_logit, 4) || !aligned(labels, 8) ||
         !aligned(stats, 4) || !aligned(d_loss, 4) || !aligned(d_logits, width(dtype)))
         return QSDP_EALIGN;
-    const DistillParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature}, teacher_index, teacher_logit, top,
+    const DistillParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, teacher_index, teacher_logit, top,
                              labels, temperature, alpha, nullptr, d_loss, nullptr, const_cast<float*>(stats), d_logits,
                              d_row_stride};
     return status_of(launch_distill(dtype, p, static_cast<hipStream_t>(stream)));

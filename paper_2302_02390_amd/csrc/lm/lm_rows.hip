@@ -1,251 +1,711 @@
 // Kernels on rows of logits: log probabilities with entropy and top alternatives, their gradient, and distillation from a
-// teacher's top logits. One workgroup per row.
+// teacher's top logits. A workgroup per row; its threads hold the row in registers in the logits' format, 16 bytes to a
+// piece, so that the logits are read once whatever follows: maximum, sums of exponentials, alternatives, gradient. Rows that
+// do not fit are read once per use, chunk by chunk.
+#include <type_traits>
+
 #include "lm_common.hpp"
 #include "lm_rows.hpp"
+
+// A lambda is part of the function that calls it: what it refers to has to stay in registers.
+#define QSDP_INLINE __attribute__((always_inline))
 
 namespace qsdp_lm {
 namespace {
 
-constexpr int kThreads = 256;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kLn2 = 0.69314718055994531f;
 // Where exp2 has long been 0: keeps 0 * (-inf) out of the sums.
 constexpr float kLeast = -400.0f;
 
-// A row's maximum m (0 where nothing is finite, so that differences stay -inf), and its sums of 2^a and a 2^a,
-// a = (z - m) log2(e) / temperature.
-struct RowSums {
-    float m, total, mean;
-    bool empty;
+// The same number, unknown to the compiler: what follows from it is computed where it is used, and not once ahead of all
+// passes over a row, which would take more registers than the row.
+__device__ __forceinline__ uint32_t fresh(uint32_t scalar) {
+    asm volatile("" : "+s"(scalar));
+    return scalar;
+}
+__device__ __forceinline__ uint32_t fresh_thread() {
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    return thread;
+}
+
+// f(0) ... f(N - 1), each number a constant: registers cannot be indexed.
+template <int N, class F>
+__device__ __forceinline__ void times(F f) {
+    if constexpr (N > 0) {
+        times<N - 1>(f);
+        f(std::integral_constant<int, N - 1>());
+    }
+}
+
+// Nothing is moved past every fourth element: side by side, a piece's elements take more registers than the row leaves.
+__device__ __forceinline__ void keep_order(int e) {
+    if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ float exp2_fast(float a) { return __builtin_amdgcn_exp2f(a); }  // 1 ulp, 0 below 2^-126
+
+// ---- a row in pieces -----------------------------------------------------------------------------------------------
+// Piece i of a thread holds elements (first + i * THREADS + thread) * PER ... of the row; what is past the row is -inf.
+// STREAM: the row has more pieces than the workgroup holds and passes through chunk by chunk.
+template <class T, int THREADS, int NV, bool STREAM>
+struct Row {
+    static constexpr uint32_t CHUNK = THREADS * NV;  // pieces
+    const typename T::raw* z;
+    uint32_t n, pieces, first;
+    u32x4 v[NV];
+
+    __device__ __forceinline__ Row(const typename T::raw* z_, uint64_t n_) : z(z_), n((uint32_t)n_) {
+        pieces = (n + T::PER - 1) / T::PER;
+        load(0);
+    }
+    __device__ __forceinline__ uint32_t chunks() const { return STREAM ? (pieces + CHUNK - 1) / CHUNK : 1u; }
+    __device__ __forceinline__ void load(uint32_t chunk) {
+        first = STREAM ? chunk * CHUNK : 0u;
+        const uint32_t whole = fresh(n) / T::PER, thread = fresh_thread();
+        times<NV>([&](auto i) QSDP_INLINE {
+            const uint32_t at = first + i * THREADS;  // a scalar: the thread's part of the address is the same for all i
+            v[i] = u32x4{T::NONE, T::NONE, T::NONE, T::NONE};
+            if (at + thread < whole) v[i] = load16<T>(z + (uint64_t)at * T::PER + thread * T::PER);
+        });
+        const uint32_t rest = n % T::PER, slot = whole - first;  // of the piece that the row ends in
+        if (rest != 0 && slot < CHUNK && slot % THREADS == thread) {
+            const u32x4 last = load_part<T>(z + (uint64_t)whole * T::PER, (int)rest);
+            times<NV>([&](auto i) QSDP_INLINE {
+                if (slot / THREADS == (uint32_t)i) v[i] = last;
+            });
+        }
+    }
+    // f(i, index of the piece's first element) for the pieces that the thread's wave has any of. The pieces are made opaque:
+    // otherwise the compiler keeps their elements unpacked from one pass to the next, in twice the registers and more.
+    template <class F>
+    __device__ __forceinline__ void pieces_of_wave(F f) {
+        times<NV>([&](auto i) QSDP_INLINE { asm volatile("" : "+v"(v[i])); });
+        const uint32_t end = fresh(pieces), wave = (uint32_t)wave_index() * 64, lane = threadIdx.x % 64;
+        times<NV>([&](auto i) QSDP_INLINE {
+            const uint32_t at = first + i * THREADS + wave;
+            if (at < end) f(i, (at + lane) * T::PER);
+        });
+    }
+    // all chunks in turn; a row of one chunk stays where it is
+    template <class F>
+    __device__ __forceinline__ void each_chunk(F f) {
+        if constexpr (STREAM) {
+            for (uint32_t c = 0;;) {
+                f();
+                if (++c >= chunks()) break;
+                load(c);
+            }
+        } else {
+            f();
+        }
+    }
+    __device__ __forceinline__ void again() {
+        if (STREAM) load(0);
+    }
+    // to[..] = f(element) for all of them; the piece that the row ends in goes by itself, once for all i
+    template <class F>
+    __device__ __forceinline__ void write(typename T::raw* to, F f) {
+        const uint32_t whole = fresh(n) / T::PER, thread = fresh_thread();
+        pieces_of_wave([&](auto i, uint32_t) QSDP_INLINE {
+            float d[T::PER];
+            times<T::PER>([&](auto e) QSDP_INLINE {
+                d[e] = f(T::at(v[i], e));
+                keep_order(e);
+            });
+            const uint32_t at = first + i * THREADS;
+            if (at + thread < whole) store16<T>(to + (uint64_t)at * T::PER + thread * T::PER, T::pack(d));
+        });
+        const uint32_t rest = n % T::PER, slot = whole - first;
+        if (rest != 0 && slot < CHUNK && slot % THREADS == thread) {
+            u32x4 last = v[0];
+            times<NV>([&](auto i) QSDP_INLINE {
+                if (slot / THREADS == (uint32_t)i) last = v[i];
+            });
+            float d[T::PER];
+            times<T::PER>([&](auto e) QSDP_INLINE { d[e] = f(T::at(last, e)); });
+            store_part<T>(to + (uint64_t)whole * T::PER, T::pack(d), (int)rest);
+        }
+    }
+    // A bit for every element of the thread for which hit(value) holds: bit i * PER + e. -inf past the row counts like any.
+    template <class H>
+    __device__ __forceinline__ uint64_t mask(H hit) {
+        static_assert(NV * T::PER <= 64, "a bit for every element");
+        uint32_t low = 0, high = 0;
+        pieces_of_wave([&](auto i, uint32_t) QSDP_INLINE {
+            times<T::PER>([&](auto e) QSDP_INLINE {
+                const int bit = i * T::PER + e;
+                if (bit < 32) low |= hit(T::at(v[i], e)) ? 1u << bit : 0u;
+                else high |= hit(T::at(v[i], e)) ? 1u << (bit - 32) : 0u;
+            });
+        });
+        return (uint64_t)high << 32 | low;
+    }
+    __device__ __forceinline__ uint32_t index_of(int bit) const {
+        return (first + (uint32_t)bit / T::PER * THREADS + threadIdx.x) * T::PER + (uint32_t)bit % T::PER;
+    }
 };
 
-template <class T, bool MEAN>
-__device__ RowSums row_sums(const typename T::raw* z, uint64_t n, float scale2, float* scratch) {
-    RowSums r;
-    float m = kNegInf;
-    for (uint64_t j = threadIdx.x; j < n; j += kThreads) m = fmaxf(m, T::get(z[j]));
-    m = reduce_block<kThreads>(m, Max(), scratch);
+// ---- sums of exponentials --------------------------------------------------------------------------------------------
+// The maximum m and, with a = (z - m) * scale2, the sums s of 2^a and u of 2^a a, over part of a row. Where nothing is
+// above -inf all three stay at their start; a NaN or +inf makes the sums NaN.
+struct Sums {
+    float m, s, u;
+};
+__device__ __forceinline__ float shift_of(float m, float top, float scale2) { return fmaxf((m - top) * scale2, kLeast); }
+__device__ __forceinline__ void rescale(Sums& a, float top, float scale2) {
+    if (a.m == top) return;
+    const float d = shift_of(a.m, top, scale2), f = exp2_fast(d);
+    a.u = f * fmaf(d, a.s, a.u);
+    a.s = f * a.s;
+    a.m = top;
+}
+
+// A wave's sums over its pieces of every chunk, the maximum its own: no workgroup has to meet for it.
+template <bool MEAN, class R, class T>
+__device__ __forceinline__ void add_chunk(R& row, float scale2, Sums& a, T) {
+    float m = a.m;
+    row.pieces_of_wave([&](auto i, uint32_t) QSDP_INLINE {
+        times<T::PER>([&](auto e) QSDP_INLINE { m = fmaxf(m, T::at(row.v[i], e)); });
+    });
+    m = reduce64(m, Max());
+    rescale(a, m, scale2);
     const float at = m == kNegInf ? 0.0f : m;
-    float total = 0.0f, mean = 0.0f;
-    for (uint64_t j = threadIdx.x; j < n; j += kThreads) {
-        const float a = (T::get(z[j]) - at) * scale2;
-        const float e = exp2f(a);
-        total += e;
-        if (MEAN) mean += e * fmaxf(a, kLeast);
+    float s = 0.0f, u = 0.0f;
+    row.pieces_of_wave([&](auto i, uint32_t) QSDP_INLINE {
+        times<T::PER>([&](auto e) QSDP_INLINE {
+            const float d = (T::at(row.v[i], e) - at) * scale2;
+            const float p = exp2_fast(d);
+            s += p;
+            if (MEAN) u = fmaf(p, fmaxf(d, kLeast), u);
+            keep_order(e);
+        });
+    });
+    a.s += s;  // lane by lane; the wave's lanes are added up by join
+    if (MEAN) a.u += u;
+}
+
+// The workgroup's sums from its waves'; every thread gets them. room: 3 floats for each wave.
+template <int THREADS, bool MEAN>
+__device__ __forceinline__ Sums join(Sums a, float scale2, float (*room)[3]) {
+    constexpr int WAVES = THREADS / 64;
+    a.s = reduce64(a.s, Add());
+    if (MEAN) a.u = reduce64(a.u, Add());
+    if (threadIdx.x % 64 == 0) {
+        float* w = room[threadIdx.x / 64];
+        w[0] = a.m, w[1] = a.s, w[2] = a.u;
     }
-    r.total = reduce_block<kThreads>(total, Add(), scratch);
-    r.mean = MEAN ? reduce_block<kThreads>(mean, Add(), scratch) : 0.0f;
-    r.m = m;
-    r.empty = r.total == 0.0f;
-    return r;
+    __syncthreads();
+    const int w = threadIdx.x % 16;
+    Sums b = {kNegInf, 0.0f, 0.0f};
+    if (w < WAVES) b = {room[w][0], room[w][1], room[w][2]};
+    const float m = reduce16(b.m, Max());
+    rescale(b, m, scale2);
+    return {m, reduce16(b.s, Add()), MEAN ? reduce16(b.u, Add()) : 0.0f};
 }
 
-// Order of the alternatives: value downwards (a NaN above all), then index upwards; larger keys first.
-__device__ __forceinline__ uint64_t order_key(float z, uint32_t index) {
+// ---- top alternatives ------------------------------------------------------------------------------------------------
+// Order: value downwards (a NaN above all, the two zeros equal), then index upwards; larger keys first.
+__device__ __forceinline__ uint32_t value_key(float z) {
     const uint32_t u = __float_as_uint(z + 0.0f);
-    const uint32_t key = z != z ? 0xFFFFFFFFu : (u >> 31) ? ~u : u | 0x80000000u;
-    return (uint64_t)key << 32 | (0xFFFFFFFFu - index);
+    return z != z ? 0xffffffffu : (int32_t)u < 0 ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ uint32_t key_index(uint64_t key) { return 0xFFFFFFFFu - (uint32_t)key; }
-
+__device__ __forceinline__ float key_value(uint32_t key) {
+    return __uint_as_float(key == 0xffffffffu ? 0x7fc00000u : (int32_t)key < 0 ? key ^ 0x80000000u : ~key);
+}
+// Low bits of a value's key that its format leaves all zero or all one.
 template <class T>
-__device__ void score_row(const ScoreParams& p, uint64_t row) {
-    __shared__ float scratch[kThreads / 64];
-    __shared__ uint64_t keys[128];
-    __shared__ int counts[kThreads / 64];
-    __shared__ int found;
-    const uint64_t n = p.in.vocab;
-    const auto* z = static_cast<const typename T::raw*>(p.in.logits) + row * p.in.stride;
+constexpr int key_low_bits() { return sizeof(typename T::raw) == 4 ? 0 : T::NONE == BF16::NONE ? 16 : 13; }
+
+constexpr uint32_t kKeyNan = 0xffffffffu, kKeyNegInf = 0x007fffffu;
+constexpr int kMostTop = 128;
+constexpr uint32_t kRoom = 512;  // candidates that are ranked
+
+template <int THREADS>
+struct TopRoom {
+    static constexpr int GROUPS = THREADS < 256 ? THREADS : 256;
+    uint32_t group[GROUPS];
+    uint64_t list[kRoom];
+    uint32_t words[THREADS / 64];
+    uint32_t count, least;
+};
+
+// Appends the row's elements for which hit(value) holds to the list, as far as it has room, and counts all of them. They are
+// few and read from memory once more: which of its registers a thread needs is not known when the code is compiled.
+template <class T, int THREADS, class R, class H>
+__device__ __forceinline__ void collect(R& row, TopRoom<THREADS>& room, H hit) {
+    row.again();
+    row.each_chunk([&]() QSDP_INLINE {
+        uint64_t mine = row.mask(hit);
+        if (mine == 0) return;
+        uint32_t to = atomicAdd(&room.count, (uint32_t)__popcll(mine));
+        for (; mine != 0 && to < kRoom; mine &= mine - 1, ++to) {
+            const uint32_t index = row.index_of(__ffsll((unsigned long long)mine) - 1);
+            room.list[to] = (uint64_t)value_key(T::get(row.z[index])) << 32 | ~index;
+        }
+    });
+}
+
+// The `top` first elements, as keys in room.list[0 .. return value), in no order and with some more. Threshold: the top-th
+// largest of up to 256 groups' maxima, which at least `top` elements reach and on ordinary data not many more (about
+// -g log(1 - top / g) of g groups: 74 for 64). Where too many reach it (ties, masks, large values in few groups) or a NaN takes
+// part, the top-th value itself is found bit by bit, and of its equals the first by index are taken.
+template <class T, int THREADS, class R>
+__device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, TopRoom<THREADS>& room) {
+    constexpr int GROUPS = TopRoom<THREADS>::GROUPS, SHARE = THREADS / GROUPS, LOW = key_low_bits<T>();
+    const int lane = threadIdx.x % 64, wave = wave_index();
+    if (threadIdx.x == 0) room.count = 0;
+    float m = kNegInf;
+    row.again();
+    row.each_chunk([&]() QSDP_INLINE {
+        row.pieces_of_wave([&](auto i, uint32_t) QSDP_INLINE {
+            times<T::PER>([&](auto e) QSDP_INLINE { m = fmaxf(m, T::at(row.v[i], e)); });
+        });
+    });
+    if (SHARE >= 2) m = fmaxf(m, dpp<0xB1>(m));
+    if (SHARE >= 4) m = fmaxf(m, dpp<0x4E>(m));
+    if (threadIdx.x % SHARE == 0) room.group[threadIdx.x / SHARE] = value_key(m);
+    __syncthreads();
+    if (wave == 0) {
+        uint32_t key[GROUPS / 64];
+#pragma unroll
+        for (int g = 0; g < GROUPS / 64; ++g) key[g] = room.group[g * 64 + lane] >> LOW;
+        uint32_t high = 0;
+        for (int bit = 31 - LOW; bit >= 0; --bit) {
+            const uint32_t trial = high | 1u << bit;
+            uint32_t reach = 0;
+#pragma unroll
+            for (int g = 0; g < GROUPS / 64; ++g) reach += __popcll(__ballot(key[g] >= trial));
+            if (reach >= top) high = trial;
+        }
+        high <<= LOW;
+        if ((int32_t)high >= 0) high |= (1u << LOW) - 1;  // a negative value's low bits
+        if (lane == 0) room.least = high;
+    }
+    __syncthreads();
+    uint32_t least = room.least;
+    float bound = key_value(least);
+    if (plain && bound != kNegInf) {
+        collect<T>(row, room, [&](float z) QSDP_INLINE { return z >= bound; });
+        __syncthreads();
+        if (room.count <= kRoom) return room.count;
+    }
+    // the value bit by bit, unless the threshold is it already: fewer than `top` are above it
+    bool known = plain;
+    uint32_t above;
+    for (;;) {
+        if (!known) {
+            uint32_t nans = 0;
+            row.again();
+            row.each_chunk([&]() QSDP_INLINE { nans += __popcll(row.mask([](float z) QSDP_INLINE { return z != z; })); });
+            nans = reduce_block<THREADS>(nans, Add(), room.words);
+            least = 0;
+            for (int bit = 31; bit >= 0; --bit) {
+                const float trial = key_value(least | 1u << bit);  // nothing reaches a NaN but NaNs
+                uint32_t reach = 0;
+                row.again();
+                row.each_chunk([&]() QSDP_INLINE { reach += __popcll(row.mask([&](float z) QSDP_INLINE { return z >= trial; })); });
+                if (reduce_block<THREADS>(reach, Add(), room.words) + nans >= top) least |= 1u << bit;
+            }
+            least = least < kKeyNegInf ? kKeyNegInf : least;
+        }
+        bound = key_value(least);
+        __syncthreads();
+        if (threadIdx.x == 0) room.count = 0;
+        __syncthreads();
+        if (least != kKeyNan) collect<T>(row, room, [&](float z) QSDP_INLINE { return !(z <= bound); });
+        __syncthreads();
+        above = room.count;
+        if (above < top) break;
+        known = false;
+    }
+    // of the equal ones the first by index: a piece of every thread at a time, which is the order of the row
+    uint32_t found = above;
+    const uint64_t below = (1ull << lane) - 1;
+    row.again();
+    for (uint32_t c = 0; c < row.chunks() && found < top; ++c) {
+        if (c > 0) row.load(c);
+        uint64_t mine = row.mask([&](float z) QSDP_INLINE { return z == bound || (z != z && bound != bound); });
+        for (uint32_t i = 0; i < R::CHUNK / THREADS && found < top; ++i, mine >>= T::PER) {
+            const uint32_t index = row.index_of(i * T::PER);
+            uint32_t bits = (uint32_t)mine & ((1u << T::PER) - 1);
+            if (index + T::PER > row.n) bits &= index < row.n ? (1u << (row.n - index)) - 1 : 0u;
+            const uint32_t many = __popc(bits);
+            uint32_t before = 0, total = 0;  // the lanes' counts, bit by bit
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const uint64_t lanes = __ballot(many >> b & 1);
+                before += __popcll(lanes & below) << b;
+                total += __popcll(lanes) << b;
+            }
+            __syncthreads();
+            if (lane == 0) room.words[wave] = total;
+            __syncthreads();
+            uint32_t to = found + before;
+            for (int w = 0; w < THREADS / 64; ++w) {
+                to += w < wave ? room.words[w] : 0u;
+                found += room.words[w];
+            }
+            for (; bits != 0 && to < top; bits &= bits - 1, ++to)
+                room.list[to] = (uint64_t)least << 32 | ~(index + (uint32_t)(__ffs((int)bits) - 1));
+        }
+    }
+    __syncthreads();
+    return top;
+}
+
+template <class T, int THREADS, int NV, bool STREAM, bool TOP>
+__device__ __forceinline__ void score_row(const ScoreParams& p, uint64_t r) {
+    __shared__ float waves[THREADS / 64][3];
+    const auto* z = static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride;
     const float scale2 = p.in.inv_temperature * kLog2e;
-    const RowSums r = row_sums<T, true>(z, n, scale2, scratch);
-    const float log2_total = log2f(r.total);
+    Row<T, THREADS, NV, STREAM> row(z, p.in.vocab);
+    Sums a = {kNegInf, 0.0f, 0.0f};
+    row.each_chunk([&]() QSDP_INLINE { add_chunk<true>(row, scale2, a, T()); });
+    a = join<THREADS, true>(a, scale2, waves);
+    const bool empty = a.s == 0.0f;
+    const float log_total = logf(a.s);
     if (threadIdx.x == 0) {
         if (p.logprob) {
-            const int64_t t = p.tokens[row];
+            const int64_t t = p.tokens[r];
             float v = 0.0f;
-            if (t >= 0) v = r.empty ? kNegInf : __builtin_nanf("");
-            if (t >= 0 && (uint64_t)t < n && !r.empty) v = (T::get(z[t]) - r.m) * p.in.inv_temperature - log2_total * kLn2;
-            p.logprob[row] = v;
+            if (t >= 0) v = empty ? kNegInf : __builtin_nanf("");
+            if (t >= 0 && (uint64_t)t < p.in.vocab && !empty) v = (T::get(z[t]) - a.m) * p.in.inv_temperature - log_total;
+            p.logprob[r] = v;
         }
-        if (p.entropy) p.entropy[row] = r.empty ? 0.0f : (log2_total - r.mean / r.total) * kLn2;
+        if (p.entropy) p.entropy[r] = empty ? 0.0f : log_total - a.u / a.s * kLn2;
         if (p.stats) {
-            p.stats[2 * row] = r.m;
-            p.stats[2 * row + 1] = log2_total * kLn2;
+            p.stats[2 * r] = a.m;
+            p.stats[2 * r + 1] = log_total;
         }
     }
-    if (p.top == 0) return;
-    // the key of the last alternative, bit by bit: the largest that at least `top` keys reach
-    uint64_t least = 0;
-    for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t trial = least | 1ull << bit;
-        int count = 0;
-        for (uint64_t j = threadIdx.x; j < n; j += kThreads) count += order_key(T::get(z[j]), (uint32_t)j) >= trial;
-        if (reduce_block<kThreads>(count, Add(), counts) >= p.top) least = trial;
-    }
-    if (threadIdx.x == 0) found = 0;
-    __syncthreads();
-    for (uint64_t j = threadIdx.x; j < n; j += kThreads) {
-        const uint64_t key = order_key(T::get(z[j]), (uint32_t)j);
-        if (key >= least) keys[atomicAdd(&found, 1)] = key;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < p.top; i += kThreads) {
-        int rank = 0;
-        for (int o = 0; o < p.top; ++o) rank += keys[o] > keys[i];
-        const uint32_t j = key_index(keys[i]);
-        p.top_index[row * p.top + rank] = (int32_t)j;
-        p.top_logprob[row * p.top + rank] = 
-            r.empty ? kNegInf : (T::get(z[j]) - r.m) * p.in.inv_temperature - log2_total * kLn2;
+    if constexpr (TOP) {
+        __shared__ TopRoom<THREADS> room;
+        const uint32_t top = (uint32_t)p.top;
+        const uint32_t count = top_list<T>(row, top, a.s == a.s, room);
+        for (uint32_t i = threadIdx.x; i < count; i += THREADS) {
+            const uint64_t key = room.list[i];
+            uint32_t rank = 0;
+            for (uint32_t o = 0; o < count; ++o) rank += room.list[o] > key;
+            if (rank < top) {
+                p.top_index[r * top + rank] = (int32_t)~(uint32_t)key;
+                p.top_logprob[r * top + rank] =
+                    empty ? kNegInf : (key_value((uint32_t)(key >> 32)) - a.m) * p.in.inv_temperature - log_total;
+            }
+        }
     }
 }
 
-// d z_j = (g ([j = i] - p_j) - h p_j (log p_j + entropy)) / temperature
+template <class T, int THREADS, int NV, bool STREAM, bool TOP>
+__global__ __launch_bounds__(THREADS, STREAM ? 4 : 8) void score_kernel(ScoreParams p) {
+    score_row<T, THREADS, NV, STREAM, TOP>(p, p.in.first + blockIdx.x);
+}
+
+// ---- gradient of log probability and entropy --------------------------------------------------------------------------
+// Element by element once a row's sums are known: rows are cut into segments of 256 threads x 4 x 16 bytes.
+constexpr int kSegment = 4;
+
 template <class T>
-__device__ void score_backward_row(const ScoreBackwardParams& p, uint64_t row) {
-    const uint64_t n = p.in.vocab;
-    const auto* z = static_cast<const typename T::raw*>(p.in.logits) + row * p.in.stride;
-    auto* dz = static_cast<typename T::raw*>(p.d_logits) + row * p.d_stride;
-    const float m = p.stats[2 * row], log_total = p.stats[2 * row + 1];
-    const bool empty = log_total == kNegInf;
-    const float scale2 = p.in.inv_temperature * kLog2e, log2_total = log_total * kLog2e;
-    int64_t token = p.tokens ? p.tokens[row] : -1;
-    if ((uint64_t)token >= n) token = -1;
-    const float g = p.d_logprob && token >= 0 ? p.d_logprob[row] * p.in.inv_temperature : 0.0f;
-    const float h = p.d_entropy ? p.d_entropy[row] * p.in.inv_temperature : 0.0f;
-    const float entropy = p.d_entropy ? p.entropy[row] : 0.0f;
-    for (uint64_t j = threadIdx.x; j < n; j += kThreads) {
-        const float a = (T::get(z[j]) - m) * scale2 - log2_total;
-        const float prob = exp2f(a);
-        const float d = -prob * (g + h * (fmaxf(a, kLeast) * kLn2 + entropy)) + ((int64_t)j == token ? g : 0.0f);
-        dz[j] = T::put(empty ? 0.0f : d);
+struct Segment {
+    static constexpr uint32_t PIECES = 256 * kSegment;
+    uint64_t row;
+    uint32_t n, first;
+    static uint64_t of(uint64_t n) { return ((n + T::PER - 1) / T::PER + PIECES - 1) / PIECES; }
+    __device__ __forceinline__ Segment(uint64_t item, uint32_t n_) : n(n_) {
+        const uint32_t each = ((n + T::PER - 1) / T::PER + PIECES - 1) / PIECES;
+        row = item / each;
+        first = (uint32_t)(item % each) * PIECES;
     }
-}
-
-// The teacher's list of a row: its softmax, the places that count, and the student's logits there.
-struct List {
-    float p[128], z[128];
-    int32_t index[128];
+    __device__ __forceinline__ uint32_t lo() const { return first * T::PER; }
+    __device__ __forceinline__ uint32_t hi() const { return n - lo() < PIECES * T::PER ? n : lo() + PIECES * T::PER; }
+    __device__ __forceinline__ void load(const typename T::raw* z, u32x4* v) const {
+        times<kSegment>([&](auto i) QSDP_INLINE {
+            const uint32_t at = first + i * 256 + threadIdx.x;
+            v[i] = u32x4{0, 0, 0, 0};
+            if (at < n / T::PER) v[i] = load16<T>(z + (uint64_t)at * T::PER);
+            else if (at == n / T::PER) v[i] = load_part<T>(z + (uint64_t)at * T::PER, (int)(n % T::PER));
+        });
+    }
+    // dz[j] = f(z[j], j)
+    template <class F>
+    __device__ __forceinline__ void write(const u32x4* v, typename T::raw* dz, F f) const {
+        times<kSegment>([&](auto i) QSDP_INLINE {
+            const uint32_t at = first + i * 256 + threadIdx.x;
+            float d[T::PER];
+            times<T::PER>([&](auto e) QSDP_INLINE { d[e] = f(T::at(v[i], e), at * T::PER + e); });
+            if (at < n / T::PER) store16<T>(dz + (uint64_t)at * T::PER, T::pack(d));
+            else if (at == n / T::PER) store_part<T>(dz + (uint64_t)at * T::PER, T::pack(d), (int)(n % T::PER));
+        });
+    }
 };
 
-template <class T>
-__device__ void distill_row(const DistillParams& p, uint64_t row) {
-    __shared__ float scratch[kThreads / 64];
-    __shared__ List list;
-    const uint64_t n = p.in.vocab;
-    const auto* z = static_cast<const typename T::raw*>(p.in.logits) + row * p.in.stride;
+// d z_j = (g ([j = i] - p_j) - h p_j (log p_j + entropy)) / temperature
+template <class T, bool ENTROPY>
+__global__ __launch_bounds__(256) void score_backward_kernel(ScoreBackwardParams p) {
+    const uint32_t n = (uint32_t)p.in.vocab;
     const float scale2 = p.in.inv_temperature * kLog2e;
-    // teacher: softmax over the slots that are there
+    const Segment<T> part(p.in.first + blockIdx.x, n);
+    const uint64_t r = part.row;
+    u32x4 v[kSegment];
+    part.load(static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride, v);
+    const float m = p.stats[2 * r], log_total = p.stats[2 * r + 1], log2_total = log_total * kLog2e;
+    const bool empty = log_total == kNegInf;
+    const int64_t asked = p.d_logprob && p.tokens ? p.tokens[r] : -1;
+    const uint32_t token = (uint64_t)asked < (uint64_t)n && !empty ? (uint32_t)asked : ~0u;  // ~0: none
+    const float g = token != ~0u ? p.d_logprob[r] * p.in.inv_temperature : 0.0f;
+    const float h = ENTROPY ? p.d_entropy[r] * p.in.inv_temperature * kLn2 : 0.0f;  // entropies in bits below
+    const float entropy = ENTROPY ? p.entropy[r] * kLog2e : 0.0f;
+    part.write(v, static_cast<typename T::raw*>(p.d_logits) + r * p.d_stride, [&](float z, uint32_t j) QSDP_INLINE {
+        const float a = fmaf(z - m, scale2, -log2_total);
+        const float prob = exp2_fast(a);
+        const float d = -prob * (ENTROPY ? fmaf(h, fmaxf(a, kLeast) + entropy, g) : g);
+        return empty ? 0.0f : j == token ? d + g : d;
+    });
+}
+
+// ---- distillation ------------------------------------------------------------------------------------------------------
+// The teacher's list of a row: probabilities, their logs to base 2, places, and the student's logits there.
+struct List {
+    float p[kMostTop], log2_p[kMostTop], z[kMostTop];
+    int32_t index[kMostTop];
+};
+
+// A value that is the same for all threads, in a scalar register.
+__device__ __forceinline__ float same(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+}
+
+__device__ __forceinline__ uint32_t label_of(int64_t asked, uint32_t n) {  // ~0: none
+    return __builtin_amdgcn_readfirstlane((uint64_t)asked < (uint64_t)n ? (uint32_t)asked : ~0u);
+}
+
+// One exponential: at 1 where the list has no part, else at the temperature.
+template <bool BOTH>
+__device__ __forceinline__ float one_scale2(const DistillParams& p) {
+    return !BOTH && p.alpha == 0.0f ? kLog2e : p.in.inv_temperature * kLog2e;
+}
+
+template <class T, int THREADS>
+__device__ __forceinline__ bool fill_list(const DistillParams& p, const typename T::raw* z, uint64_t r, List& list,
+                                          float* scratch) {
+    const float teacher2 = p.in.inv_temperature * kLog2e;
     const int k = (int)threadIdx.x;
     int32_t index = -1;
     float u = kNegInf;
     if (k < p.top) {
-        index = p.teacher_index[row * p.top + k];
-        if (index < 0 || (uint64_t)index >= n) index = -1;
-        if (index >= 0) u = p.teacher_logit[row * p.top + k];
-    }
-    const float um = reduce_block<kThreads>(u, Max(), scratch);
-    const float ua = (u - (um == kNegInf ? 0.0f : um)) * scale2;
-    const float e = index >= 0 ? exp2f(ua) : 0.0f;
-    const float mass = reduce_block<kThreads>(e, Add(), scratch);
-    const bool taught = mass != 0.0f;  // a NaN counts as taught
-    const float prob = taught ? e / mass : 0.0f;
-    const float log2_p = ua - log2f(mass);
-    if (k < p.top) {
-        list.p[k] = prob;
+        index = p.teacher_index[r * p.top + k];
+        if (index < 0 || (uint64_t)index >= p.in.vocab) index = -1;
         list.index[k] = index;
-        list.z[k] = index >= 0 ? T::get(z[index]) : 0.0f;
+        list.z[k] = 0.0f;
+        if (index >= 0) {
+            u = p.teacher_logit[r * p.top + k];
+            list.z[k] = T::get(z[index]);
+        }
     }
-    int64_t label = p.labels && p.alpha < 1.0f ? p.labels[row] : -1;
-    const bool bad_label = label >= 0 && (uint64_t)label >= n;
-    if (bad_label) label = -1;
-    // student
-    float m, soft2, hard2;  // maximum, log2 of the sums at the temperature and at 1
-    if (p.loss) {
-        const RowSums s = row_sums<T, false>(z, n, scale2, scratch);
-        const RowSums o = row_sums<T, false>(z, n, kLog2e, scratch);
-        m = s.m, soft2 = log2f(s.total), hard2 = log2f(o.total);
-        if (p.stats && k == 0) {
-            p.stats[3 * row] = m;
-            p.stats[3 * row + 1] = soft2 * kLn2;
-            p.stats[3 * row + 2] = hard2 * kLn2;
+    const float um = reduce_block<THREADS>(u, Max(), scratch);
+    const float ua = (u - (um == kNegInf ? 0.0f : um)) * teacher2;
+    const float e = index >= 0 ? exp2f(ua) : 0.0f;
+    const float mass = reduce_block<THREADS>(e, Add(), scratch);
+    if (k < p.top) {
+        list.p[k] = mass != 0.0f ? e / mass : 0.0f;
+        list.log2_p[k] = ua - log2f(mass);
+    }
+    return mass != 0.0f;  // a NaN counts as taught
+}
+
+// What the gradient of a row's loss is made of: d z_v = soft 2^(...) + hard 2^(...), less the targets at the list's places and
+// at the label. BOTH: the temperature's exponentials and those at 1 are two; otherwise one serves (scale2).
+template <bool BOTH>
+struct Slope {
+    float m, scale2, soft_log, hard_log, soft, hard, one;
+    uint32_t label;  // ~0: none
+    __device__ __forceinline__ Slope(const DistillParams& p, float scale2_, float m_, float soft_log_, float hard_log_, bool taught,
+                                     uint32_t label_, float g)
+        : m(m_), scale2(scale2_), soft_log(soft_log_), hard_log(hard_log_), label(label_) {
+        soft = same(taught ? g * p.alpha * p.temperature : 0.0f);
+        hard = same(label != ~0u ? g * (1.0f - p.alpha) : 0.0f);
+        one = same(soft + hard);
+    }
+    __device__ __forceinline__ bool nothing() const { return soft_log == kNegInf || (soft == 0.0f && hard == 0.0f); }
+    __device__ __forceinline__ float operator()(float v) const {
+        const float d = v - m;
+        if (!BOTH) return one * exp2_fast(fmaf(d, scale2, -soft_log));
+        return fmaf(hard, exp2_fast(fmaf(d, kLog2e, -hard_log)), soft * exp2_fast(fmaf(d, scale2, -soft_log)));
+    }
+    __device__ __forceinline__ float target(const List& list, int top, uint32_t j) const {
+        float sum = 0.0f;
+#pragma unroll 1
+        for (int o = 0; o < top; ++o) sum += (uint32_t)list.index[o] == j ? list.p[o] : 0.0f;
+        return soft * sum + (j == label ? hard : 0.0f);
+    }
+    // The places of the list and the label, among elements [lo, hi), once more with their targets; slots of the same index
+    // write the same value. After a barrier behind the writes of all elements.
+    template <class T>
+    __device__ __forceinline__ void aim(const List& list, int top, float z_label, typename T::raw* dz, uint32_t lo,
+                                        uint32_t hi) const {
+        const int k = (int)threadIdx.x;
+        if (k < top) {
+            const uint32_t j = (uint32_t)list.index[k];
+            if (j >= lo && j < hi) dz[j] = T::put((*this)(list.z[k]) - target(list, top, j));
         }
-        const bool empty = soft2 == kNegInf;
-        float kl = 0.0f;
+        if (k == 0 && label >= lo && label < hi) dz[label] = T::put((*this)(z_label) - target(list, top, label));
+    }
+};
+
+// Loss, and in the same pass the gradient if it is asked for.
+template <class T, int THREADS, int NV, bool STREAM, bool BOTH>
+__global__ __launch_bounds__(THREADS, STREAM ? 4 : 8) void distill_kernel(DistillParams p) {
+    __shared__ float waves[THREADS / 64][3], waves1[THREADS / 64][3], scratch[THREADS / 64];
+    __shared__ List list;
+    const uint64_t r = p.in.first + blockIdx.x;
+    const uint32_t n = (uint32_t)p.in.vocab;
+    const auto* z = static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride;
+    const float scale2 = one_scale2<BOTH>(p);
+    Row<T, THREADS, NV, STREAM> row(z, n);
+    const bool taught = fill_list<T, THREADS>(p, z, r, list, scratch);
+    const int64_t asked = p.labels && p.alpha < 1.0f ? p.labels[r] : -1;
+    const uint32_t label = label_of(asked, n);
+    const float z_label = same(label != ~0u ? T::get(z[label]) : 0.0f);
+    Sums a = {kNegInf, 0.0f, 0.0f}, b = a;
+    row.each_chunk([&]() QSDP_INLINE {
+        add_chunk<false>(row, scale2, a, T());
+        if (BOTH) add_chunk<false>(row, kLog2e, b, T());
+    });
+    a = join<THREADS, false>(a, scale2, waves);
+    // maximum, log2 of the sums at the temperature and at 1
+    const float m = same(a.m), soft_log = same(log2f(a.s));
+    const float hard_log = BOTH ? same(log2f(join<THREADS, false>(b, kLog2e, waves1).s)) : soft_log;
+    const bool empty = soft_log == kNegInf;
+    const int k = (int)threadIdx.x;
+    float kl = 0.0f;
+    if (k < p.top) {
+        const float prob = list.p[k];
         if (prob > 0.0f || prob != prob) {
-            const float log2_q = empty ? kNegInf : (list.z[k] - m) * scale2 - soft2;
-            kl = prob * (log2_p - log2_q);
+            const float log2_q = empty ? kNegInf : (list.z[k] - m) * (p.in.inv_temperature * kLog2e) - soft_log;
+            kl = prob * (list.log2_p[k] - log2_q);
         }
-        kl = reduce_block<kThreads>(kl, Add(), scratch) * kLn2;
-        if (k == 0) {
-            float loss = p.alpha > 0.0f ? p.alpha * p.temperature * p.temperature * kl : 0.0f;
-            if (label >= 0)
-                loss -= (1.0f - p.alpha) * (empty ? kNegInf : ((T::get(z[label]) - m) * kLog2e - hard2) * kLn2);
-            p.loss[row] = bad_label ? __builtin_nanf("") : loss;
+    }
+    kl = reduce_block<THREADS>(kl, Add(), scratch) * kLn2;
+    if (k == 0) {
+        float loss = p.alpha > 0.0f ? p.alpha * p.temperature * p.temperature * kl : 0.0f;
+        if (label != ~0u) loss -= (1.0f - p.alpha) * (empty ? kNegInf : (z_label - m) - hard_log * kLn2);
+        p.loss[r] = asked >= (int64_t)n ? __builtin_nanf("") : loss;
+        if (p.stats) {
+            p.stats[3 * r] = m;
+            p.stats[3 * r + 1] = soft_log * kLn2;
+            p.stats[3 * r + 2] = hard_log * kLn2;
         }
-    } else {
-        m = p.stats[3 * row], soft2 = p.stats[3 * row + 1] * kLog2e, hard2 = p.stats[3 * row + 2] * kLog2e;
     }
     if (!p.d_logits) return;
-    const float* scales = p.loss ? p.row_scale : p.d_loss;
-    const float g = scales ? scales[row] : 1.0f;
-    const float soft = taught ? g * p.alpha * p.temperature : 0.0f, hard = label >= 0 ? g * (1.0f - p.alpha) : 0.0f;
-    const bool empty = soft2 == kNegInf;
-    auto* dz = static_cast<typename T::raw*>(p.d_logits) + row * p.d_stride;
-    const float z_label = label >= 0 ? T::get(z[label]) : 0.0f;
-    __syncthreads();  // everything outside the own elements has been read: the gradient may overwrite the logits
-    auto grad = [&](float v) {
-        float d = 0.0f;
-        if (soft != 0.0f) d += soft * exp2f((v - m) * scale2 - soft2);
-        if (hard != 0.0f) d += hard * exp2f((v - m) * kLog2e - hard2);
-        return d;
-    };
-    for (uint64_t j = threadIdx.x; j < n; j += kThreads) dz[j] = T::put(empty ? 0.0f : grad(T::get(z[j])));
-    if (empty) return;
-    __syncthreads();
-    // the places of the list, once more with their targets; slots of the same index write the same value
-    auto target = [&](int32_t j) {
-        float sum = 0.0f;
-        for (int o = 0; o < p.top; ++o) sum += list.index[o] == j ? list.p[o] : 0.0f;
-        return soft * sum + ((int64_t)j == label ? hard : 0.0f);
-    };
-    if (k < p.top && index >= 0) dz[index] = T::put(grad(list.z[k]) - target(index));
-    if (k == 0 && label >= 0) dz[label] = T::put(grad(z_label) - target((int32_t)label));
-}
-
-// A workgroup takes every gridDim-th row.
-template <class P, void (*ROW)(const P&, uint64_t)>
-__global__ __launch_bounds__(kThreads) void rows_kernel(P p) {
-    for (uint64_t row = blockIdx.x; row < p.in.rows; row += gridDim.x) {
-        ROW(p, row);
-        __syncthreads();  // the next row uses the same shared memory
+    auto* dz = static_cast<typename T::raw*>(p.d_logits) + r * p.d_stride;
+    const Slope<BOTH> slope(p, scale2, m, soft_log, hard_log, taught, label, same(p.row_scale ? p.row_scale[r] : 1.0f));
+    row.again();
+    __syncthreads();  // the list is there, and what is read outside the own pieces has been read
+    if (slope.nothing()) {
+        for (uint32_t j = threadIdx.x; j < n; j += THREADS) dz[j] = T::put(0.0f);
+        return;
     }
+    row.each_chunk([&]() QSDP_INLINE { row.write(dz, slope); });
+    __syncthreads();
+    slope.template aim<T>(list, p.top, z_label, dz, 0, n);
 }
 
-template <class P>
-using Kernel = void (*)(P);
+// The gradient alone, from the row's statistics: rows are cut into pieces as for the gradient of log probabilities.
+template <class T, bool BOTH>
+__global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p) {
+    __shared__ float scratch[4];
+    __shared__ List list;
+    const uint32_t n = (uint32_t)p.in.vocab;
+    const Segment<T> part(p.in.first + blockIdx.x, n);
+    const uint64_t r = part.row;
+    const auto* z = static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride;
+    auto* dz = static_cast<typename T::raw*>(p.d_logits) + r * p.d_stride;
+    u32x4 v[kSegment];
+    part.load(z, v);
+    const bool taught = fill_list<T, 256>(p, z, r, list, scratch);
+    const uint32_t label = label_of(p.labels && p.alpha < 1.0f ? p.labels[r] : -1, n);
+    const float z_label = same(label != ~0u ? T::get(z[label]) : 0.0f);
+    const Slope<BOTH> slope(p, one_scale2<BOTH>(p), same(p.stats[3 * r]), same(p.stats[3 * r + 1] * kLog2e),
+                            same(p.stats[3 * r + 2] * kLog2e), taught, label, same(p.d_loss[r]));
+    const bool nothing = slope.nothing();
+    __syncthreads();  // the list is there
+    part.write(v, dz, [&](float v, uint32_t) QSDP_INLINE { return nothing ? 0.0f : slope(v); });
+    if (nothing) return;
+    __syncthreads();
+    slope.template aim<T>(list, p.top, z_label, dz, part.lo(), part.hi());
+}
 
+// ---- which kernel ------------------------------------------------------------------------------------------------------
+// A workgroup for each of `work` items (rows or parts of them), in several launches where they are more than a grid holds:
+// a loop over rows inside a kernel costs it 20 registers.
 constexpr uint64_t kMaxGrid = 1u << 20;
 
 template <class P>
-hipError_t go(Kernel<P> f32, Kernel<P> bf16, Kernel<P> f16, qsdp_dtype dtype, const P& p, hipStream_t s) {
-    const Kernel<P> kernel = dtype == QSDP_F32 ? f32 : dtype == QSDP_BF16 ? bf16 : f16;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.in.rows < kMaxGrid ? p.in.rows : kMaxGrid)), dim3(kThreads), 0, s, p);
-    return hipGetLastError();
+hipError_t go(void (*kernel)(P), int threads, uint64_t work, P p, hipStream_t s) {
+    for (p.in.first = 0; p.in.first < work; p.in.first += kMaxGrid) {
+        const uint64_t left = work - p.in.first;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)(left < kMaxGrid ? left : kMaxGrid)), dim3(threads), 0, s, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// Threads and pieces per thread by the row's length: the smallest team that holds it, as 64 registers to a lane keep a
+// compute unit's 2048 threads; longer rows take fewer, larger threads, and the longest pass chunk by chunk.
+template <class T, class F>
+hipError_t by_length(uint64_t n, F f) {
+    const uint64_t pieces = (n + T::PER - 1) / T::PER;
+    std::integral_constant<int, 2> two;
+    std::integral_constant<int, 8> eight;
+    if (pieces <= 128 * 2) return f(std::integral_constant<int, 128>(), two, std::false_type());
+    if (pieces <= 256 * 8) return f(std::integral_constant<int, 256>(), eight, std::false_type());
+    if (pieces <= 512 * 8) return f(std::integral_constant<int, 512>(), eight, std::false_type());
+    if (pieces <= 1024 * 8) return f(std::integral_constant<int, 1024>(), eight, std::false_type());
+    return f(std::integral_constant<int, 1024>(), eight, std::true_type());
+}
+
+template <class F>
+hipError_t by_format(qsdp_dtype dtype, F f) {
+    return dtype == QSDP_F32 ? f(F32()) : dtype == QSDP_BF16 ? f(BF16()) : f(F16());
 }
 
 }  // namespace
 
-#define QSDP_LM_ROWS(P, ROW, dtype, p, s) \
-    go<P>(rows_kernel<P, ROW<F32>>, rows_kernel<P, ROW<BF16>>, rows_kernel<P, ROW<F16>>, dtype, p, s)
 hipError_t launch_score(qsdp_dtype dtype, const ScoreParams& p, hipStream_t s) {
-    return QSDP_LM_ROWS(ScoreParams, score_row, dtype, p, s);
+    return by_format(dtype, [&](auto t) {
+        using T = decltype(t);
+        return by_length<T>(p.in.vocab, [&](auto threads, auto nv, auto stream) {
+            if (p.top) return go(score_kernel<T, threads, nv, stream, true>, threads, p.in.rows, p, s);
+            return go(score_kernel<T, threads, nv, stream, false>, threads, p.in.rows, p, s);
+        });
+    });
 }
+
 hipError_t launch_score_backward(qsdp_dtype dtype, const ScoreBackwardParams& p, hipStream_t s) {
-    return QSDP_LM_ROWS(ScoreBackwardParams, score_backward_row, dtype, p, s);
+    return by_format(dtype, [&](auto t) {
+        using T = decltype(t);
+        const uint64_t work = p.in.rows * Segment<T>::of(p.in.vocab);
+        return p.d_entropy ? go(score_backward_kernel<T, true>, 256, work, p, s)
+                           : go(score_backward_kernel<T, false>, 256, work, p, s);
+    });
 }
+
 hipError_t launch_distill(qsdp_dtype dtype, const DistillParams& p, hipStream_t s) {
-    return QSDP_LM_ROWS(DistillParams, distill_row, dtype, p, s);
+    const bool both = p.alpha > 0.0f && p.alpha < 1.0f && p.temperature != 1.0f;
+    return by_format(dtype, [&](auto t) {
+        using T = decltype(t);
+        if (!p.loss) {
+            const uint64_t work = p.in.rows * Segment<T>::of(p.in.vocab);
+            return both ? go(distill_backward_kernel<T, true>, 256, work, p, s)
+                        : go(distill_backward_kernel<T, false>, 256, work, p, s);
+        }
+        return by_length<T>(p.in.vocab, [&](auto threads, auto nv, auto stream) {
+            if (both) return go(distill_kernel<T, threads, nv, stream, true>, threads, p.in.rows, p, s);
+            return go(distill_kernel<T, threads, nv, stream, false>, threads, p.in.rows, p, s);
+        });
+    });
 }
-#undef QSDP_LM_ROWS
 
 }  // namespace qsdp_lm

@@ -12,6 +12,7 @@ struct Rows {
     const void* logits;
     uint64_t rows, vocab, stride;  // elements
     float inv_temperature;
+    uint64_t first;  // item of a launch's first workgroup
 };
 
 struct ScoreParams {
