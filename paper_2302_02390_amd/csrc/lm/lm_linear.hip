@@ -90,6 +90,131 @@ __global__ __launch_bounds__(64) void matmul_kernel(MatmulParams p) {
     }
 }
 
+// ---- tiles ----------------------------------------------------------------------------------------------------------------
+// A workgroup computes TN channels x TM tokens in steps of 128 codes. Both operands' codes go straight from memory into LDS,
+// two steps deep: while one is multiplied the next is on its way, and one barrier a step separates them. LDS holds rows of
+// 128 bytes whose eight pieces of 16 are permuted by the row (piece c of row r in place c ^ (r % 8)), so that sixteen rows
+// read the same piece from all banks; the permutation is in the addresses that the lanes read from memory. A wave multiplies
+// WN channels (first operand, so that four consecutive channels of a token end up in a lane) by WM tokens.
+constexpr int kStep = 128;
+
+typedef __attribute__((address_space(1))) const void* global_ptr;
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+template <int TN, int TM, int WN, int WM>
+struct Tile {
+    static constexpr int WAVES = TN / WN * (TM / WM), THREADS = WAVES * 64;
+    static constexpr int ROWS = TN + TM, BYTES = ROWS * kStep;      // of a step in LDS
+    static constexpr int W_LOADS = TN / 8 / WAVES, X_LOADS = TM / 8 / WAVES;  // of 8 rows, for each wave
+    static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0, "whole loads");
+};
+
+// Which tile: workgroups go to the eight dies in turn, so each die takes a contiguous run of the tiles, which walk through
+// `kBand` token tiles for every channel tile and share their operands in the die's L2.
+constexpr uint32_t kDies = 8, kBand = 4;
+
+__device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_tiles, uint32_t& n, uint32_t& m) {
+    const uint32_t all = n_tiles * m_tiles, each = all / kDies, more = all % kDies, die = id % kDies;
+    const uint32_t at = die * each + (die < more ? die : more) + id / kDies;
+    const uint32_t band = at / (kBand * n_tiles), left = m_tiles - band * kBand, high = left < kBand ? left : kBand;
+    const uint32_t in = at - band * kBand * n_tiles;
+    n = in / high;
+    m = band * kBand + in % high;
+}
+
+template <int TN, int TM, int WN, int WM, bool BUCKETS, class O>
+__global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(MatmulParams p, uint32_t n_tiles,
+                                                                                 uint32_t m_tiles) {
+    typedef Tile<TN, TM, WN, WM> S;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][S::BYTES];
+    constexpr int A = WN / 16, B = WM / 16;
+    uint32_t n_tile, m_tile;
+    place(blockIdx.x, n_tiles, m_tiles, n_tile, m_tile);
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const uint64_t n0 = (uint64_t)n_tile * TN, m0 = (uint64_t)m_tile * TM;
+    // what the lane loads: a piece of 16 bytes of a row of eight; rows past the matrix are its last one
+    const uint32_t piece = (uint32_t)((lane % 8) ^ (lane / 8)) * 16;
+    uint32_t w_at[S::W_LOADS], x_at[S::X_LOADS];
+#pragma unroll
+    for (int i = 0; i < S::W_LOADS; ++i) {
+        uint64_t row = (uint64_t)(wave * S::W_LOADS + i) * 8 + lane / 8;
+        if (n0 + row >= p.n) row = p.n - 1 - n0;
+        w_at[i] = (uint32_t)(row * p.w_pitch) + piece;
+    }
+#pragma unroll
+    for (int i = 0; i < S::X_LOADS; ++i) {
+        uint64_t row = (uint64_t)(wave * S::X_LOADS + i) * 8 + lane / 8;
+        if (m0 + row >= p.m) row = p.m - 1 - m0;
+        x_at[i] = (uint32_t)(row * p.x_pitch) + piece;
+    }
+    const uint8_t* w = p.w + n0 * p.w_pitch;
+    const int8_t* x = p.x + m0 * p.x_pitch;
+    auto fetch = [&](uint8_t* to, uint32_t k0) __attribute__((always_inline)) {
+        const uint8_t* wk = w + k0;
+        const int8_t* xk = x + k0;
+        // a channel's codes end at a multiple of 32: pieces past that are read from its start, the tokens' codes there are zero
+        const bool past = k0 + piece >= p.w_pitch;
+#pragma unroll
+        for (int i = 0; i < S::W_LOADS; ++i)
+            __builtin_amdgcn_global_load_lds((global_ptr)(wk + (past ? w_at[i] - piece : w_at[i])),
+                                             (lds_ptr)(to + (wave * S::W_LOADS + i) * 1024), 16, 0, 0);
+#pragma unroll
+        for (int i = 0; i < S::X_LOADS; ++i)
+            __builtin_amdgcn_global_load_lds((global_ptr)(xk + x_at[i]),
+                                             (lds_ptr)(to + TN * kStep + (wave * S::X_LOADS + i) * 1024), 16, 0, 0);
+    };
+    const int wn = wave % (TN / WN) * WN, wm = wave / (TN / WN) * WM;
+    const int r = lane % 16, part = lane / 16;
+    v4i d[A][B];
+#pragma unroll
+    for (int a = 0; a < A; ++a)
+#pragma unroll
+        for (int b = 0; b < B; ++b) d[a][b] = v4i{0, 0, 0, 0};
+    auto multiply = [&](const uint8_t* from) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int at = r * kStep + ((k * 4 + part) ^ (r % 8)) * 16;
+            v4i wv[A], xv[B];
+#pragma unroll
+            for (int a = 0; a < A; ++a)
+                wv[a] = *reinterpret_cast<const v4i*>(from + (wn + a * 16) * kStep + at) ^ (int)0x80808080;
+#pragma unroll
+            for (int b = 0; b < B; ++b) xv[b] = *reinterpret_cast<const v4i*>(from + (TN + wm + b * 16) * kStep + at);
+#pragma unroll
+            for (int a = 0; a < A; ++a)
+#pragma unroll
+                for (int b = 0; b < B; ++b) d[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[a], xv[b], d[a][b], 0, 0, 0);
+        }
+    };
+    const uint32_t steps = (uint32_t)((p.k + kStep - 1) / kStep);
+    fetch(lds[0], 0);
+    for (uint32_t s = 0; s < steps; ++s) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();  // this step's codes are there, and the step before has been multiplied
+        if (s + 1 < steps) fetch(lds[(s + 1) & 1], (s + 1) * kStep);
+        multiply(lds[s & 1]);
+    }
+    // d[a][b][c]: channel wn + a * 16 + part * 4 + c of token wm + b * 16 + r
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        const uint64_t m = m0 + wm + b * 16 + r;
+        if (m >= p.m) continue;
+        const float scale = p.x_scale[m], sum = p.x_sums[m];
+        auto* y = static_cast<typename O::raw*>(p.y) + m * p.y_stride;
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint64_t n = n0 + wn + a * 16 + part * 4 + c;
+                if (n >= p.n) continue;
+                const float base = p.meta[2 * n], step = p.meta[2 * n + 1];
+                const float v = fmaf(step, (float)d[a][b][c], fmaf(128.0f, step, base) * sum);
+                y[n] = O::put(p.bias ? fmaf(scale, v, p.bias[n]) : scale * v);
+            }
+        }
+    }
+}
+
 }  // namespace
 
 hipError_t launch_tokens(qsdp_dtype dtype, const TokenParams& p, hipStream_t s) {
@@ -99,7 +224,19 @@ hipError_t launch_tokens(qsdp_dtype dtype, const TokenParams& p, hipStream_t s) 
     return hipGetLastError();
 }
 
+template <int TN, int TM, int WN, int WM, class O>
+static hipError_t launch_tiles(const MatmulParams& p, hipStream_t s) {
+    const uint32_t n_tiles = (uint32_t)((p.n + TN - 1) / TN), m_tiles = (uint32_t)((p.m + TM - 1) / TM);
+    hipLaunchKernelGGL((tiles_kernel<TN, TM, WN, WM, false, O>), dim3(n_tiles * m_tiles), dim3(Tile<TN, TM, WN, WM>::THREADS), 0,
+                       s, p, n_tiles, m_tiles);
+    return hipGetLastError();
+}
+
 hipError_t launch_matmul(qsdp_dtype out, const MatmulParams& p, hipStream_t s) {
+    if (p.m > 64 && p.buckets == 1)
+        return out == QSDP_F32    ? launch_tiles<256, 256, 64, 128, F32>(p, s)
+               : out == QSDP_BF16 ? launch_tiles<256, 256, 64, 128, BF16>(p, s)
+                                  : launch_tiles<256, 256, 64, 128, F16>(p, s);
     const dim3 grid((unsigned)((p.n + 15) / 16 * ((p.m + 15) / 16)));
     auto kernel = out == QSDP_F32 ? matmul_kernel<F32> : out == QSDP_BF16 ? matmul_kernel<BF16> : matmul_kernel<F16>;
     hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, p);
