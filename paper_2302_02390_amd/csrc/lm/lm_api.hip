@@ -125,7 +125,7 @@ int qsdp_quantize_tokens(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k
     if (!x || !codes || !scale || !sums) return QSDP_EINVAL;
     if (!aligned(x, width(dtype)) || !aligned(codes, 16) || !aligned(scale, 4) || !aligned(sums, 4)) return QSDP_EALIGN;
     const TokenParams p = {x, m, k, row_stride, (uint32_t)bucket, (uint32_t)buckets_of(k, bucket), codes, token_pitch(k),
-                           scale, sums};
+                           scale, sums, 0};
     return status_of(launch_tokens(dtype, p, static_cast<hipStream_t>(stream)));
 }
 

@@ -11,41 +11,92 @@
 namespace qsdp_lm {
 namespace {
 
+constexpr uint64_t kMaxGrid = 1u << 20;
+
 typedef int v4i __attribute__((ext_vector_type(4)));
 
-constexpr int kTokenThreads = 256;
-
-// s = max |x| times the rounded 1/127, q = rint(x / s) with an IEEE division in binary32; slots past k are zero.
+// ---- tokens --------------------------------------------------------------------------------------------------------------
+// s = max |x| times the rounded 1/127, q = rint(x / s) with an IEEE division in binary32; slots past k are zero. A workgroup
+// per token, which keeps the token in registers between its maximum and its codes: eight elements to a thread at a time, of
+// which the NV-th part is the last that is held; a longer token is read twice.
 template <class T>
-__global__ __launch_bounds__(kTokenThreads) void tokens_kernel(TokenParams p) {
-    __shared__ float scratch[kTokenThreads / 64];
-    __shared__ int counts[kTokenThreads / 64];
-    for (uint64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
-        const auto* x = static_cast<const typename T::raw*>(p.x) + row * p.stride;
-        int8_t* codes = p.codes + row * p.pitch;
-        float most = 0.0f;
-        int odd = 0;  // a NaN or an infinity
-        for (uint64_t k = threadIdx.x; k < p.k; k += kTokenThreads) {
-            const float a = fabsf(T::get(x[k]));
-            odd |= !(a < __builtin_inff());
-            most = fmaxf(most, a);
-        }
-        most = reduce_block<kTokenThreads>(most, Max(), scratch);
-        odd = reduce_block<kTokenThreads>(odd, Max(), counts);
-        const float scale = odd ? __builtin_nanf("") : most * (1.0f / 127.0f);
-        for (uint32_t b = 0; b < p.buckets; ++b) {
-            const uint64_t lo = (uint64_t)b * p.bucket, hi = b + 1 == p.buckets ? p.pitch : lo + p.bucket;
-            int sum = 0;
-            for (uint64_t k = lo + threadIdx.x; k < hi; k += kTokenThreads) {
-                int q = 0;
-                if (k < p.k && scale > 0.0f) q = (int)fminf(fmaxf(rintf(T::get(x[k]) / scale), -127.0f), 127.0f);
-                codes[k] = (int8_t)q;
-                sum += q;
+struct Eight {
+    float v[8];
+    // elements k ... k + 7 of n, zeros past the end
+    __device__ __forceinline__ void load(const typename T::raw* x, uint64_t k, uint64_t n) {
+        if (k + 8 <= n) {
+            if constexpr (T::PER == 8) {
+                const u32x4 p = load16<T>(x + k);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = T::at(p, e);
+            } else {
+                const u32x4 p = load16<T>(x + k), q = load16<T>(x + k + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = T::at(p, e), v[4 + e] = T::at(q, e);
             }
-            sum = reduce_block<kTokenThreads>(sum, Add(), counts);
-            if (threadIdx.x == 0) p.sums[row * p.buckets + b] = (float)sum;  // below 2^24: exact
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = k + e < n ? T::get(x[k + e]) : 0.0f;
         }
-        if (threadIdx.x == 0) p.scale[row] = scale;
+    }
+};
+
+template <class T, int THREADS, int NV>
+__global__ __launch_bounds__(THREADS) void tokens_kernel(TokenParams p) {
+    __shared__ float scratch[THREADS / 64];
+    __shared__ int counts[THREADS / 64];
+    const uint64_t row = p.first + blockIdx.x;
+    const auto* x = static_cast<const typename T::raw*>(p.x) + row * p.stride;
+    uint64_t* codes = reinterpret_cast<uint64_t*>(p.codes + row * p.pitch);
+    const uint32_t pieces = (uint32_t)(p.pitch / 8);
+    Eight<T> held[NV];
+    float most = 0.0f;
+    bool odd = false;  // a NaN or an infinity
+    for (uint32_t first = 0; first < pieces; first += THREADS * NV) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t at = first + i * THREADS + threadIdx.x;
+            if (at < pieces) held[i].load(x, (uint64_t)at * 8, p.k);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) held[i].v[e] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float a = fabsf(held[i].v[e]);
+                odd |= !(a < __builtin_inff());
+                most = fmaxf(most, a);
+            }
+    }
+    if (__ballot(odd)) most = __builtin_inff();
+    most = reduce_block<THREADS>(most, Max(), scratch);
+    const float scale = most < __builtin_inff() ? most * (1.0f / 127.0f) : __builtin_nanf("");
+    if (threadIdx.x == 0) p.scale[row] = scale;
+    const bool some = scale > 0.0f;
+    for (uint32_t b = 0; b < p.buckets; ++b) {
+        const uint32_t lo = b * (p.bucket / 8), hi = b + 1 == p.buckets ? pieces : lo + p.bucket / 8;
+        int sum = 0;
+        for (uint32_t first = lo / (THREADS * NV) * (THREADS * NV); first < hi; first += THREADS * NV) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const uint32_t at = first + i * THREADS + threadIdx.x;
+                if (at < lo || at >= hi) continue;
+                if (pieces > THREADS * NV) held[i].load(x, (uint64_t)at * 8, p.k);
+                uint32_t word[2] = {0, 0};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float q = fminf(fmaxf(rintf(held[i].v[e] / scale), -127.0f), 127.0f);
+                    const int c = some ? (int)q : 0;
+                    sum += c;
+                    word[e / 4] |= (uint32_t)(c & 0xff) << (e % 4 * 8);
+                }
+                codes[at] = (uint64_t)word[1] << 32 | word[0];
+            }
+        }
+        sum = reduce_block<THREADS>(sum, Add(), counts);
+        if (threadIdx.x == 0) p.sums[row * p.buckets + b] = (float)sum;  // below 2^24: exact
     }
 }
 
@@ -87,6 +138,24 @@ __global__ __launch_bounds__(64) void matmul_kernel(MatmulParams p) {
     for (int c = 0; c < 4; ++c) {
         const uint64_t n = n0 + part * 4 + c;
         if (n < p.n) y[n] = O::put(p.bias ? fmaf(s, acc[c], p.bias[n]) : s * acc[c]);
+    }
+}
+
+// Four consecutive elements, or the first `count` of them, wherever they start.
+template <class O>
+__device__ __forceinline__ void put4(typename O::raw* y, const float* v, int count) {
+    if (count == 4) {
+        if constexpr (sizeof(typename O::raw) == 4) {
+            typedef float anywhere __attribute__((ext_vector_type(4), aligned(4)));
+            *reinterpret_cast<anywhere*>(y) = anywhere{v[0], v[1], v[2], v[3]};
+        } else {
+            typedef uint32_t anywhere __attribute__((ext_vector_type(2), aligned(2)));
+            *reinterpret_cast<anywhere*>(y) = anywhere{O::two(v[0], v[1]), O::two(v[2], v[3])};
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < 3; ++c)
+            if (c < count) y[c] = O::put(v[c]);
     }
 }
 
@@ -195,33 +264,51 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Ma
         multiply(lds[s & 1]);
     }
     // d[a][b][c]: channel wn + a * 16 + part * 4 + c of token wm + b * 16 + r
+    const float* meta = p.meta + 2 * (n0 + wn + part * 4);
+    const float* bias = p.bias ? p.bias + n0 + wn + part * 4 : nullptr;
+    const int64_t left = (int64_t)(p.n - n0) - wn - part * 4;  // channels from the lane's first one on
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-        const uint64_t m = m0 + wm + b * 16 + r;
-        if (m >= p.m) continue;
-        const float scale = p.x_scale[m], sum = p.x_sums[m];
-        auto* y = static_cast<typename O::raw*>(p.y) + m * p.y_stride;
+    for (int a = 0; a < A; ++a) {
+        if (left <= a * 16) continue;
+        const int count = left - a * 16 < 4 ? (int)(left - a * 16) : 4;
+        float step[4], centre[4], add[4];
 #pragma unroll
-        for (int a = 0; a < A; ++a) {
+        for (int c = 0; c < 4; ++c) {
+            const int n = a * 16 + (c < count ? c : 0);
+            step[c] = meta[2 * n + 1];
+            centre[c] = fmaf(128.0f, step[c], meta[2 * n]);
+            add[c] = bias ? bias[n] : 0.0f;
+        }
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint64_t n = n0 + wn + a * 16 + part * 4 + c;
-                if (n >= p.n) continue;
-                const float base = p.meta[2 * n], step = p.meta[2 * n + 1];
-                const float v = fmaf(step, (float)d[a][b][c], fmaf(128.0f, step, base) * sum);
-                y[n] = O::put(p.bias ? fmaf(scale, v, p.bias[n]) : scale * v);
-            }
+        for (int b = 0; b < B; ++b) {
+            const uint64_t m = m0 + wm + b * 16 + r;
+            if (m >= p.m) continue;
+            const float scale = p.x_scale[m], sum = p.x_sums[m];
+            float v[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = fmaf(scale, fmaf(step[c], (float)d[a][b][c], centre[c] * sum), add[c]);
+            put4<O>(static_cast<typename O::raw*>(p.y) + m * p.y_stride + n0 + wn + part * 4 + a * 16, v, count);
         }
     }
 }
 
 }  // namespace
 
+template <class T>
+static hipError_t launch_tokens_of(TokenParams p, hipStream_t s) {
+    for (p.first = 0; p.first < p.rows; p.first += kMaxGrid) {
+        const dim3 grid((unsigned)(p.rows - p.first < kMaxGrid ? p.rows - p.first : kMaxGrid));
+        if (p.pitch <= 8 * 64) hipLaunchKernelGGL((tokens_kernel<T, 64, 1>), grid, dim3(64), 0, s, p);
+        else if (p.pitch <= 8 * 256) hipLaunchKernelGGL((tokens_kernel<T, 256, 1>), grid, dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((tokens_kernel<T, 256, 4>), grid, dim3(256), 0, s, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 hipError_t launch_tokens(qsdp_dtype dtype, const TokenParams& p, hipStream_t s) {
-    const dim3 grid((unsigned)(p.rows < (1u << 20) ? p.rows : (1u << 20)));
-    auto kernel = dtype == QSDP_F32 ? tokens_kernel<F32> : dtype == QSDP_BF16 ? tokens_kernel<BF16> : tokens_kernel<F16>;
-    hipLaunchKernelGGL(kernel, grid, dim3(kTokenThreads), 0, s, p);
-    return hipGetLastError();
+    return dtype == QSDP_F32 ? launch_tokens_of<F32>(p, s) : dtype == QSDP_BF16 ? launch_tokens_of<BF16>(p, s) : launch_tokens_of<F16>(p, s);
 }
 
 template <int TN, int TM, int WN, int WM, class O>

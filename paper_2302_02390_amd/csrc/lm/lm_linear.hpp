@@ -15,6 +15,7 @@ struct TokenParams {
     int8_t* codes;
     uint64_t pitch;  // bytes from a token's codes to the next one's
     float *scale, *sums;
+    uint64_t first;  // token of a launch's first workgroup
 };
 
 struct MatmulParams {
