@@ -676,7 +676,7 @@ int qsdp_distill_loss_backward(const void* logits, qsdp_dtype dtype, uint64_t ro
  * is whole buckets: k a multiple of `bucket` (the flat matrix as one vector), or every channel
  * encoded as a tensor of its own (segmented calls; k <= bucket: one bucket, the rest of its slots
  * unused). So wcodes holds ceil(k / bucket) * bucket bytes per channel, wmeta ceil(k / bucket)
- * pairs. bucket is a multiple of 128 where a channel has more than one; k <= 2^20.
+ * pairs. bucket is a multiple of 128 where a channel has more than one; k <= 2^20, n <= 2^26.
  *
  * qsdp_quantize_tokens rounds each row of x to 8 bits: s = max |x| * (1/127), q = x / s to the
  * nearest whole number (binary32: product with the rounded 1/127, IEEE division; all zero for a

@@ -31,9 +31,9 @@ bool distill_ok(int top, float alpha, const void* index, const void* logit, cons
            (top == 0 || (index && logit)) && (alpha == 1.0f || labels);
 }
 
-// A channel is one bucket, or several buckets of whole steps of the product.
+// A channel is one bucket, or several buckets of whole steps of the product. (2^26 channels of 2^20 codes: 64 TB.)
 bool product_ok(uint64_t m, uint64_t n, uint64_t k, int bucket) {
-    return m <= kMost && n >= 1 && n <= kMost && k >= 1 && k <= (1u << 20) && bucket >= 32 && bucket <= 8192 &&
+    return m <= kMost && n >= 1 && n <= (1u << 26) && k >= 1 && k <= (1u << 20) && bucket >= 32 && bucket <= 8192 &&
            bucket % 32 == 0 && (k <= (uint64_t)bucket || bucket % 128 == 0);
 }
 

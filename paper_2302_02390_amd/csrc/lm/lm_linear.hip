@@ -5,6 +5,8 @@
 //   D_rnb = sum_{k in b} q_rk (c_nk - 128),  Q_rb = sum_{k in b} q_rk
 // D and Q are whole numbers and exact: |D| <= 127 * 128 * 8192 < 2^31 by the largest bucket. c - 128 as a signed byte is c
 // with its top bit flipped, so the packed codes go into the matrix instructions as they are but for one xor.
+#include <type_traits>
+
 #include "lm_common.hpp"
 #include "lm_linear.hpp"
 
@@ -100,47 +102,6 @@ __global__ __launch_bounds__(THREADS) void tokens_kernel(TokenParams p) {
     }
 }
 
-// A wave computes 16 channels x 16 tokens: the codes of a channel and of a token come in pieces of 64, 16 bytes to a lane.
-template <class O>
-__global__ __launch_bounds__(64) void matmul_kernel(MatmulParams p) {
-    const int lane = threadIdx.x, i = lane % 16, part = lane / 16;
-    const uint64_t tiles = (p.n + 15) / 16;
-    const uint64_t n0 = blockIdx.x % tiles * 16, m0 = blockIdx.x / tiles * 16;
-    const uint64_t wn = n0 + i < p.n ? n0 + i : p.n - 1, xm = m0 + i < p.m ? m0 + i : p.m - 1;
-    const uint8_t* w = p.w + wn * p.w_pitch;
-    const int8_t* x = p.x + xm * p.x_pitch;
-    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t b = 0; b < p.buckets; ++b) {
-        // 16 bytes at a time as far as there are tokens' codes: those past k are zero, whatever the weights hold there
-        const uint64_t lo = (uint64_t)b * p.bucket, end = (p.k + 15) / 16 * 16, hi = lo + p.bucket < end ? lo + p.bucket : end;
-        v4i d = {0, 0, 0, 0};
-        for (uint64_t k = lo; k < hi; k += 64) {
-            v4i wv = {0, 0, 0, 0}, xv = {0, 0, 0, 0};
-            if (k + part * 16 < hi) {
-                wv = *reinterpret_cast<const v4i*>(w + k + part * 16);
-                wv = wv ^ (int)0x80808080;
-                xv = *reinterpret_cast<const v4i*>(x + k + part * 16);
-            }
-            d = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, xv, d, 0, 0, 0);
-        }
-        const float q = p.x_sums[xm * p.buckets + b];
-        for (int c = 0; c < 4; ++c) {
-            const uint64_t n = n0 + part * 4 + c;
-            if (n < p.n) {
-                const float base = p.meta[2 * (n * p.buckets + b)], scale = p.meta[2 * (n * p.buckets + b) + 1];
-                acc[c] += fmaf(scale, (float)d[c], fmaf(128.0f, scale, base) * q);
-            }
-        }
-    }
-    if (m0 + i >= p.m) return;
-    const float s = p.x_scale[m0 + i];
-    auto* y = static_cast<typename O::raw*>(p.y) + (m0 + i) * p.y_stride;
-    for (int c = 0; c < 4; ++c) {
-        const uint64_t n = n0 + part * 4 + c;
-        if (n < p.n) y[n] = O::put(p.bias ? fmaf(s, acc[c], p.bias[n]) : s * acc[c]);
-    }
-}
-
 // Four consecutive elements, or the first `count` of them, wherever they start.
 template <class O>
 __device__ __forceinline__ void put4(typename O::raw* y, const float* v, int count) {
@@ -161,7 +122,7 @@ __device__ __forceinline__ void put4(typename O::raw* y, const float* v, int cou
 
 // ---- tiles ----------------------------------------------------------------------------------------------------------------
 // A workgroup computes TN channels x TM tokens in steps of 128 codes. Both operands' codes go straight from memory into LDS,
-// two steps deep: while one is multiplied the next is on its way, and one barrier a step separates them. LDS holds rows of
+// STAGES steps deep: while one is multiplied the next ones are on their way, and one barrier a step separates them. LDS holds rows of
 // 128 bytes whose eight pieces of 16 are permuted by the row (piece c of row r in place c ^ (r % 8)), so that sixteen rows
 // read the same piece from all banks; the permutation is in the addresses that the lanes read from memory. A wave multiplies
 // WN channels (first operand, so that four consecutive channels of a token end up in a lane) by WM tokens.
@@ -169,6 +130,38 @@ constexpr int kStep = 128;
 
 typedef __attribute__((address_space(1))) const void* global_ptr;
 typedef __attribute__((address_space(3))) void* lds_ptr;
+
+// Until at most N of the wave's loads are on their way: those into LDS are not the compiler's to wait for.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    static_assert(N < 64, "six bits");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Until the wave's reads of LDS (and scalar loads) are done, in a form that the compiler counts and does not repeat.
+__device__ __forceinline__ void wait_reads() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// The workgroup's waves meet; unlike __syncthreads, without waiting for the loads that are on their way. What a wave has
+// read from LDS before is in its registers, as it has been multiplied.
+__device__ __forceinline__ void meet_here() { asm volatile("s_barrier" ::: "memory"); }
+
+// Reads of LDS (and loads from memory) go between the matrix instructions of the same stretch of code: a wave whose reads wait
+// for the LDS issues nothing else, and all waves are at the same place.
+template <int READS, int PRODUCTS, int LOADS, int I = 0>
+__device__ __forceinline__ void interleave() {
+    if constexpr (I < READS) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        if constexpr (I < LOADS) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, (I + 1) * PRODUCTS / READS - I * PRODUCTS / READS, 0);
+        interleave<READS, PRODUCTS, LOADS, I + 1>();
+    } else {
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
 
 template <int TN, int TM, int WN, int WM>
 struct Tile {
@@ -191,11 +184,11 @@ __device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_
     m = band * kBand + in % high;
 }
 
-template <int TN, int TM, int WN, int WM, bool BUCKETS, class O>
+template <int TN, int TM, int WN, int WM, int STAGES, bool BUCKETS, class O>
 __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(MatmulParams p, uint32_t n_tiles,
                                                                                  uint32_t m_tiles) {
     typedef Tile<TN, TM, WN, WM> S;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][S::BYTES];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES][S::BYTES];
     constexpr int A = WN / 16, B = WM / 16;
     uint32_t n_tile, m_tile;
     place(blockIdx.x, n_tiles, m_tiles, n_tile, m_tile);
@@ -239,56 +232,287 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Ma
     for (int a = 0; a < A; ++a)
 #pragma unroll
         for (int b = 0; b < B; ++b) d[a][b] = v4i{0, 0, 0, 0};
-    auto multiply = [&](const uint8_t* from) __attribute__((always_inline)) {
+    // a half of a step's codes (64) for the wave's channels and tokens, and their product
+    v4i wv[2][A], xv[2][B];
+    auto read = [&](auto set, const uint8_t* from) __attribute__((always_inline)) {
+        const int at = r * kStep + ((set * 4 + part) ^ (r % 8)) * 16;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int at = r * kStep + ((k * 4 + part) ^ (r % 8)) * 16;
-            v4i wv[A], xv[B];
+        for (int a = 0; a < A; ++a) wv[set][a] = *reinterpret_cast<const v4i*>(from + (wn + a * 16) * kStep + at);
 #pragma unroll
-            for (int a = 0; a < A; ++a)
-                wv[a] = *reinterpret_cast<const v4i*>(from + (wn + a * 16) * kStep + at) ^ (int)0x80808080;
+        for (int b = 0; b < B; ++b) xv[set][b] = *reinterpret_cast<const v4i*>(from + (TN + wm + b * 16) * kStep + at);
+    };
+    auto multiply = [&](auto set) __attribute__((always_inline)) {
 #pragma unroll
-            for (int b = 0; b < B; ++b) xv[b] = *reinterpret_cast<const v4i*>(from + (TN + wm + b * 16) * kStep + at);
+        for (int a = 0; a < A; ++a) {
+            const v4i signed_w = wv[set][a] ^ (int)0x80808080;
 #pragma unroll
-            for (int a = 0; a < A; ++a)
-#pragma unroll
-                for (int b = 0; b < B; ++b) d[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[a], xv[b], d[a][b], 0, 0, 0);
+            for (int b = 0; b < B; ++b) d[a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(signed_w, xv[set][b], d[a][b], 0, 0, 0);
         }
     };
-    const uint32_t steps = (uint32_t)((p.k + kStep - 1) / kStep);
-    fetch(lds[0], 0);
-    for (uint32_t s = 0; s < steps; ++s) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();  // this step's codes are there, and the step before has been multiplied
-        if (s + 1 < steps) fetch(lds[(s + 1) & 1], (s + 1) * kStep);
-        multiply(lds[s & 1]);
-    }
+    const std::integral_constant<int, 0> one;
+    const std::integral_constant<int, 1> other;
     // d[a][b][c]: channel wn + a * 16 + part * 4 + c of token wm + b * 16 + r
-    const float* meta = p.meta + 2 * (n0 + wn + part * 4);
-    const float* bias = p.bias ? p.bias + n0 + wn + part * 4 : nullptr;
     const int64_t left = (int64_t)(p.n - n0) - wn - part * 4;  // channels from the lane's first one on
+    const float* meta = p.meta + 2 * p.buckets * (n0 + wn + part * 4);
+    const uint32_t steps = (uint32_t)((p.k + kStep - 1) / kStep);
+    // of channels in several buckets: the sum over the buckets so far, added to at the end of each
+    float sum_of[BUCKETS ? A : 1][BUCKETS ? B : 1][4];
+    if constexpr (BUCKETS) {
 #pragma unroll
-    for (int a = 0; a < A; ++a) {
-        if (left <= a * 16) continue;
-        const int count = left - a * 16 < 4 ? (int)(left - a * 16) : 4;
-        float step[4], centre[4], add[4];
+        for (int a = 0; a < A; ++a)
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sum_of[a][b][c] = 0.0f;
+    }
+    uint32_t bucket = 0, next = p.bucket / kStep;
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s)
+        if ((uint32_t)s < steps) fetch(lds[s], s * kStep);
+    // Step `at` is there for all waves: its loads are done (those behind it may be on their way), and so is the reading of the
+    // step before, whose place the step STAGES - 1 further takes. While a half is multiplied the next one comes out of LDS,
+    // over the barrier as well: reading and multiplying would otherwise take turns, as the barrier has all waves do the same.
+    constexpr int LOADS = S::W_LOADS + S::X_LOADS;
+    // the buckets that end with step s
+    auto fold = [&](uint32_t s) __attribute__((always_inline)) {
+        if constexpr (BUCKETS) {
+            if (s + 1 != next && s + 1 != steps) return;
+            float sums[B];
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                const uint64_t m = m0 + wm + b * 16 + r;
+                sums[b] = p.x_sums[(m < p.m ? m : p.m - 1) * p.buckets + bucket];
+            }
+#pragma unroll
+            for (int a = 0; a < A; ++a)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int64_t n = a * 16 + c < left ? a * 16 + c : left - 1;  // within the matrix, from the lane's first on
+                    const float2 of = left > 0 ? *reinterpret_cast<const float2*>(meta + 2 * (n * p.buckets + bucket))
+                                               : make_float2(0.0f, 0.0f);
+                    const float centre = fmaf(128.0f, of.y, of.x);
+#pragma unroll
+                    for (int b = 0; b < B; ++b) {
+                        sum_of[a][b][c] += fmaf(of.y, (float)d[a][b][c], centre * sums[b]);
+                        d[a][b][c] = 0;
+                    }
+                }
+            ++bucket;
+            next += p.bucket / kStep;
+        }
+    };
+    auto first_half = [&](uint32_t s) __attribute__((always_inline)) {
+        wait_reads();  // ahead of the next ones: more than fifteen cannot be counted
+        read(other, lds[s % STAGES]);
+        multiply(one);
+        interleave<A + B, A * B, 0>();
+        wait_reads();  // the step is in registers
+    };
+    wait_loads<0>();
+    meet_here();
+    if (STAGES - 1 < steps) fetch(lds[STAGES - 1], (STAGES - 1) * kStep);
+    wait_reads();
+    read(one, lds[0]);
+    uint32_t s = 0;
+    for (; s + STAGES < steps; ++s) {
+        first_half(s);
+        wait_loads<(STAGES - 2) * LOADS>();
+        meet_here();
+        fetch(lds[s % STAGES], (s + STAGES) * kStep);
+        read(one, lds[(s + 1) % STAGES]);
+        multiply(other);
+        interleave<A + B, A * B, LOADS>();
+        fold(s);
+    }
+    for (; s + 1 < steps; ++s) {
+        first_half(s);
+        wait_loads<0>();
+        meet_here();
+        read(one, lds[(s + 1) % STAGES]);
+        multiply(other);
+        interleave<A + B, A * B, 0>();
+        fold(s);
+    }
+    first_half(s);
+    multiply(other);
+    fold(s);
+    // every scale is read before the first output is written: the compiler cannot know them apart
+    const float* bias = p.bias ? p.bias + n0 + wn + part * 4 : nullptr;
+    float scale[B], sums[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        const uint64_t m = m0 + wm + b * 16 + r < p.m ? m0 + wm + b * 16 + r : p.m - 1;
+        scale[b] = p.x_scale[m];
+        sums[b] = BUCKETS ? 0.0f : p.x_sums[m];
+    }
+    float step[A][4], centre[A][4], add[A][4];
+#pragma unroll
+    for (int a = 0; a < A; ++a)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            const int n = a * 16 + (c < count ? c : 0);
-            step[c] = meta[2 * n + 1];
-            centre[c] = fmaf(128.0f, step[c], meta[2 * n]);
-            add[c] = bias ? bias[n] : 0.0f;
+            const int64_t n = a * 16 + c < left ? a * 16 + c : left - 1;  // as in fold
+            const float2 of = BUCKETS || left <= 0 ? make_float2(0.0f, 0.0f) : *reinterpret_cast<const float2*>(meta + 2 * n);
+            step[a][c] = of.y;
+            centre[a][c] = fmaf(128.0f, of.y, of.x);
+            add[a][c] = bias && left > 0 ? bias[n] : 0.0f;
         }
 #pragma unroll
-        for (int b = 0; b < B; ++b) {
-            const uint64_t m = m0 + wm + b * 16 + r;
-            if (m >= p.m) continue;
-            const float scale = p.x_scale[m], sum = p.x_sums[m];
+    for (int b = 0; b < B; ++b) {
+        const uint64_t m = m0 + wm + b * 16 + r;
+        if (m >= p.m) continue;
+        auto* y = static_cast<typename O::raw*>(p.y) + m * p.y_stride + n0 + wn + part * 4;
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+            if (left <= a * 16) continue;
             float v[4];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) v[c] = fmaf(scale, fmaf(step[c], (float)d[a][b][c], centre[c] * sum), add[c]);
-            put4<O>(static_cast<typename O::raw*>(p.y) + m * p.y_stride + n0 + wn + part * 4 + a * 16, v, count);
+            for (int c = 0; c < 4; ++c) {
+                if constexpr (BUCKETS) v[c] = fmaf(scale[b], sum_of[a][b][c], add[a][c]);
+                else v[c] = fmaf(scale[b], fmaf(step[a][c], (float)d[a][b][c], centre[a][c] * sums[b]), add[a][c]);
+            }
+            put4<O>(y + a * 16, v, left - a * 16 < 4 ? (int)(left - a * 16) : 4);
         }
+    }
+}
+
+// ---- few tokens ----------------------------------------------------------------------------------------------------------
+// The weights are read once and bound the time. A workgroup takes 16 channels and all tokens (16 * MT); its waves share the
+// codes of a channel: by buckets, or a bucket's codes among several waves, so that enough loads are on their way. Each wave
+// moves its codes through LDS of its own, as the tiles do, and waits for nobody. Whole numbers meet in LDS before they are
+// scaled; waves that take whole buckets scale their own, and their sums meet in the order of the waves.
+template <int MT, int WAVES, int STAGES, class O>
+__global__ __launch_bounds__(WAVES * 64) void few_kernel(MatmulParams p) {
+    constexpr int ROWS = 16 + 16 * MT, LOADS = 2 + 2 * MT;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[WAVES][STAGES][ROWS * kStep];
+    __shared__ int meet[WAVES][MT][4][64];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const int i = lane % 16, part = lane / 16;
+    const uint64_t n0 = (uint64_t)blockIdx.x * 16;
+    const uint32_t piece = (uint32_t)((lane % 8) ^ (lane / 8)) * 16;
+    const uint8_t* w = p.w + n0 * p.w_pitch;
+    uint32_t w_at[2], x_at[2 * MT];
+#pragma unroll
+    for (int l = 0; l < 2; ++l) {
+        uint64_t row = l * 8 + lane / 8;
+        if (n0 + row >= p.n) row = p.n - 1 - n0;
+        w_at[l] = (uint32_t)(row * p.w_pitch) + piece;
+    }
+#pragma unroll
+    for (int l = 0; l < 2 * MT; ++l) {
+        const uint32_t row = l * 8 + lane / 8;
+        x_at[l] = (uint32_t)((row < p.m ? row : (uint32_t)p.m - 1) * p.x_pitch) + piece;
+    }
+    auto fetch = [&](uint8_t* to, uint32_t k0) __attribute__((always_inline)) {
+        const bool past = k0 + piece >= p.w_pitch;  // as in the tiles
+#pragma unroll
+        for (int l = 0; l < 2; ++l)
+            __builtin_amdgcn_global_load_lds((global_ptr)(w + k0 + (past ? w_at[l] - piece : w_at[l])), (lds_ptr)(to + l * 1024), 16, 0, 0);
+#pragma unroll
+        for (int l = 0; l < 2 * MT; ++l)
+            __builtin_amdgcn_global_load_lds((global_ptr)(p.x + k0 + x_at[l]), (lds_ptr)(to + (2 + l) * 1024), 16, 0, 0);
+    };
+    // steps [from, to) of 128 codes
+    auto multiply = [&](uint32_t from, uint32_t to, v4i (&d)[MT]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s)
+            if (from + s < to) fetch(lds[wave][s], (from + s) * kStep);
+        uint32_t slot = 0;
+        for (uint32_t s = from; s < to; ++s) {
+            if (s + STAGES - 1 < to) {
+                fetch(lds[wave][slot == 0 ? STAGES - 1 : slot - 1], (s + STAGES - 1) * kStep);
+                wait_loads<(STAGES - 1) * LOADS>();
+            } else {
+                wait_loads<0>();
+            }
+            const uint8_t* at = lds[wave][slot] + i * kStep;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int in = ((k * 4 + part) ^ (i % 8)) * 16;
+                const v4i wv = *reinterpret_cast<const v4i*>(at + in) ^ (int)0x80808080;
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    const v4i xv = *reinterpret_cast<const v4i*>(at + (16 + t * 16) * kStep + in);
+                    d[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, xv, d[t], 0, 0, 0);
+                }
+            }
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+            wait_reads();  // the slot has been read before it is filled again
+        }
+    };
+    const bool shared = p.buckets < WAVES;  // several waves to a bucket
+    const uint32_t parts = shared ? WAVES / p.buckets : 1;
+    const uint32_t steps = (uint32_t)((p.k + kStep - 1) / kStep), each_bucket = (p.bucket + kStep - 1) / kStep;
+    const uint64_t first = n0 + part * 4;
+    auto scaled = [&](const int* d, uint32_t bucket, int t, float* v) __attribute__((always_inline)) {
+        const uint64_t m = t * 16 + i < (int)p.m ? t * 16 + i : p.m - 1;
+        const float sum = p.x_sums[m * p.buckets + bucket];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint64_t n = first + c < p.n ? first + c : p.n - 1;
+            const float2 of = *reinterpret_cast<const float2*>(p.meta + 2 * (n * p.buckets + bucket));
+            v[c] += fmaf(of.y, (float)d[c], fmaf(128.0f, of.y, of.x) * sum);
+        }
+    };
+    if (shared) {
+        v4i d[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) d[t] = v4i{0, 0, 0, 0};
+        const uint32_t bucket = wave / parts, at = wave % parts;
+        if (bucket < p.buckets) {
+            const uint32_t lo = bucket * each_bucket, stop = lo + each_bucket < steps ? lo + each_bucket : steps;
+            const uint32_t each = (stop - lo + parts - 1) / parts, from = lo + at * each;
+            if (from < stop) multiply(from, from + each < stop ? from + each : stop, d);
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) meet[wave][t][c][lane] = d[t][c];
+    } else {
+        float v[MT][4];
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[t][c] = 0.0f;
+        for (uint32_t b = wave; b < p.buckets; b += WAVES) {
+            v4i d[MT];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) d[t] = v4i{0, 0, 0, 0};
+            const uint32_t lo = b * each_bucket;
+            multiply(lo, lo + each_bucket < steps ? lo + each_bucket : steps, d);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const int whole[4] = {d[t][0], d[t][1], d[t][2], d[t][3]};
+                scaled(whole, b, t, v[t]);
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) meet[wave][t][c][lane] = __float_as_int(v[t][c]);
+    }
+    __syncthreads();
+    for (int t = wave; t < MT; t += WAVES) {
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (shared) {
+            for (uint32_t b = 0; b < p.buckets; ++b) {
+                int d[4] = {0, 0, 0, 0};
+                for (uint32_t a = 0; a < parts; ++a)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) d[c] += meet[b * parts + a][t][c][lane];
+                scaled(d, b, t, v);
+            }
+        } else {
+            for (int a = 0; a < WAVES; ++a)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] += __int_as_float(meet[a][t][c][lane]);
+        }
+        const uint64_t m = t * 16 + i;
+        if (m >= p.m || first >= p.n) continue;
+        const float s = p.x_scale[m];
+        const int count = p.n - first < 4 ? (int)(p.n - first) : 4;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] = p.bias ? fmaf(s, v[c], p.bias[c < count ? first + c : first]) : s * v[c];
+        put4<O>(static_cast<typename O::raw*>(p.y) + m * p.y_stride + first, v, count);
     }
 }
 
@@ -311,23 +535,74 @@ hipError_t launch_tokens(qsdp_dtype dtype, const TokenParams& p, hipStream_t s) 
     return dtype == QSDP_F32 ? launch_tokens_of<F32>(p, s) : dtype == QSDP_BF16 ? launch_tokens_of<BF16>(p, s) : launch_tokens_of<F16>(p, s);
 }
 
-template <int TN, int TM, int WN, int WM, class O>
+template <int TN, int TM, int WN, int WM, int STAGES, bool BUCKETS, class O>
 static hipError_t launch_tiles(const MatmulParams& p, hipStream_t s) {
     const uint32_t n_tiles = (uint32_t)((p.n + TN - 1) / TN), m_tiles = (uint32_t)((p.m + TM - 1) / TM);
-    hipLaunchKernelGGL((tiles_kernel<TN, TM, WN, WM, false, O>), dim3(n_tiles * m_tiles), dim3(Tile<TN, TM, WN, WM>::THREADS), 0,
-                       s, p, n_tiles, m_tiles);
+    // in several launches where the tiles are more than a grid holds
+    const uint32_t most = kMaxGrid / n_tiles ? kMaxGrid / n_tiles : 1;
+    for (uint32_t done = 0; done < m_tiles; done += most) {
+        const uint32_t now = m_tiles - done < most ? m_tiles - done : most;
+        const uint64_t first = (uint64_t)done * TM;
+        MatmulParams q = p;
+        q.x += first * p.x_pitch;
+        q.x_scale += first;
+        q.x_sums += first * p.buckets;
+        q.m = p.m - first < (uint64_t)now * TM ? p.m - first : (uint64_t)now * TM;
+        q.y = static_cast<typename O::raw*>(p.y) + first * p.y_stride;
+        hipLaunchKernelGGL((tiles_kernel<TN, TM, WN, WM, STAGES, BUCKETS, O>), dim3(n_tiles * now),
+                           dim3(Tile<TN, TM, WN, WM>::THREADS), 0, s, q, n_tiles, now);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <int MT, int WAVES, int STAGES, class O>
+static hipError_t launch_few(const MatmulParams& p, hipStream_t s) {
+    hipLaunchKernelGGL((few_kernel<MT, WAVES, STAGES, O>), dim3((unsigned)((p.n + 15) / 16)), dim3(WAVES * 64), 0, s, p);
     return hipGetLastError();
 }
 
+// Time of a product with tiles of TN x TM by the steps of 128 codes and the tiles that a compute unit gets: us of a step with
+// one workgroup on the compute unit (it waits for its loads), of a step with all of them, and of a tile's start and end.
+struct Cost {
+    uint64_t tn, tm;
+    double alone, packed, tile;
+};
+static double cost_of(const MatmulParams& p, const Cost& c) {
+    const uint64_t tiles = (p.n + c.tn - 1) / c.tn * ((p.m + c.tm - 1) / c.tm), each = (tiles + 255) / 256;
+    const double steps = (double)((p.k + kStep - 1) / kStep), step = c.packed * (double)each;
+    return steps * (step > c.alone ? step : c.alone) + c.tile * (double)each;
+}
+// Measured on products of 8192 x 2048 x 8192, 4096^3, 2048^3, 512 x 8192 x 2048 and 512 x 2048 x 8192 (m x n x k), within a
+// fifth of these sums: us with 256-, 128- and 64-wide tiles 142 / 171 / 251, 68 / 81 / 112, 36 / 18 / 19, 35 / 18 / 18 and
+// 92 / 43 / 22.
+constexpr Cost kCost256 = {256, 256, 1.43, 1.95, 11.0}, kCost128 = {128, 128, 0.66, 0.58, 3.5}, kCost64 = {64, 64, 0.30, 0.21, 1.3};
+
+template <bool BUCKETS, class O>
+static hipError_t launch_small_tiles(const MatmulParams& p, hipStream_t s) {
+    // deeper where no more than two share a compute unit (512 x 2048 x 8192 32 / 22 us), else room for five (2048^3 22 / 19 us)
+    if ((p.n + 63) / 64 * ((p.m + 63) / 64) <= 512) return launch_tiles<64, 64, 32, 32, 4, BUCKETS, O>(p, s);
+    return launch_tiles<64, 64, 32, 32, 2, BUCKETS, O>(p, s);
+}
+
+template <class O>
+static hipError_t launch_matmul_to(const MatmulParams& p, hipStream_t s) {
+    // Few tokens: waves with loads of their own as long as the channels alone do not fill the chip (1 x 8192 x 2048 4.7 us, in
+    // tiles 7.6; 16 x 50257 x 2048 21 us, in tiles 18), more of them to a channel where there are fewer workgroups.
+    const uint64_t groups = (p.n + 15) / 16;
+    if (p.m <= 16 && groups <= 2048) return groups <= 512 ? launch_few<1, 8, 2, O>(p, s) : launch_few<1, 4, 3, O>(p, s);
+    if (p.m <= 32 && groups <= 1024) return groups <= 256 ? launch_few<2, 8, 2, O>(p, s) : launch_few<2, 4, 2, O>(p, s);
+    const double small = cost_of(p, kCost64), middle = cost_of(p, kCost128), large = cost_of(p, kCost256);
+    if (p.buckets > 1)  // the largest tile has no registers for sums over buckets
+        return small < middle ? launch_small_tiles<true, O>(p, s) : launch_tiles<128, 128, 64, 64, 2, true, O>(p, s);
+    if (small < middle && small < large) return launch_small_tiles<false, O>(p, s);
+    if (middle < large) return launch_tiles<128, 128, 64, 64, 2, false, O>(p, s);
+    return launch_tiles<256, 256, 64, 128, 2, false, O>(p, s);
+}
+
 hipError_t launch_matmul(qsdp_dtype out, const MatmulParams& p, hipStream_t s) {
-    if (p.m > 64 && p.buckets == 1)
-        return out == QSDP_F32    ? launch_tiles<256, 256, 64, 128, F32>(p, s)
-               : out == QSDP_BF16 ? launch_tiles<256, 256, 64, 128, BF16>(p, s)
-                                  : launch_tiles<256, 256, 64, 128, F16>(p, s);
-    const dim3 grid((unsigned)((p.n + 15) / 16 * ((p.m + 15) / 16)));
-    auto kernel = out == QSDP_F32 ? matmul_kernel<F32> : out == QSDP_BF16 ? matmul_kernel<BF16> : matmul_kernel<F16>;
-    hipLaunchKernelGGL(kernel, grid, dim3(64), 0, s, p);
-    return hipGetLastError();
+    return out == QSDP_F32 ? launch_matmul_to<F32>(p, s) : out == QSDP_BF16 ? launch_matmul_to<BF16>(p, s) : launch_matmul_to<F16>(p, s);
 }
 
 }  // namespace qsdp_lm
