@@ -48,15 +48,22 @@ __device__ __forceinline__ float exp2_fast(float a) { return __builtin_amdgcn_ex
 
 // ---- a row in pieces -----------------------------------------------------------------------------------------------
 // Piece i of a thread holds elements (first + i * THREADS + thread) * PER ... of the row; what is past the row is -inf.
-// STREAM: the row has more pieces than the workgroup holds and passes through chunk by chunk.
-template <class T, int THREADS, int NV, bool STREAM>
+// The first NV are in registers, up to HELD more in LDS, in places that only their thread uses. STREAM: the row has more
+// pieces than the workgroup holds and passes through chunk by chunk.
+enum class Rest { NONE, HELD, STREAM };
+constexpr uint32_t kHeld = 4736;  // pieces in LDS: two workgroups to a compute unit's 160 KB, with what else they use
+
+template <class T, int THREADS, int NV, Rest REST>
 struct Row {
-    static constexpr uint32_t CHUNK = THREADS * NV;  // pieces
+    static constexpr uint32_t CHUNK = THREADS * NV;  // pieces in registers
+    static constexpr bool STREAM = REST == Rest::STREAM;
+    static constexpr int HELD = REST == Rest::HELD ? (kHeld + THREADS - 1) / THREADS : 0;
     const typename T::raw* z;
+    u32x4* held;
     uint32_t n, pieces, first;
     u32x4 v[NV];
 
-    __device__ __forceinline__ Row(const typename T::raw* z_, uint64_t n_) : z(z_), n((uint32_t)n_) {
+    __device__ __forceinline__ Row(const typename T::raw* z_, uint64_t n_, u32x4* held_) : z(z_), held(held_), n((uint32_t)n_) {
         pieces = (n + T::PER - 1) / T::PER;
         load(0);
     }
@@ -70,6 +77,19 @@ struct Row {
             if (at + thread < whole) v[i] = load16<T>(z + (uint64_t)at * T::PER + thread * T::PER);
         });
         const uint32_t rest = n % T::PER, slot = whole - first;  // of the piece that the row ends in
+        if constexpr (HELD > 0) {
+            u32x4 more[HELD];
+            times<HELD>([&](auto i) QSDP_INLINE {
+                const uint32_t at = CHUNK + i * THREADS;
+                more[i] = u32x4{T::NONE, T::NONE, T::NONE, T::NONE};
+                if (at + thread < whole) more[i] = load16<T>(z + (uint64_t)at * T::PER + thread * T::PER);
+            });
+            times<HELD>([&](auto i) QSDP_INLINE {
+                if (i * THREADS + thread < kHeld) held[i * THREADS + thread] = more[i];
+            });
+            if (rest != 0 && slot >= CHUNK && slot % THREADS == thread)
+                held[slot - CHUNK] = load_part<T>(z + (uint64_t)whole * T::PER, (int)rest);
+        }
         if (rest != 0 && slot < CHUNK && slot % THREADS == thread) {
             const u32x4 last = load_part<T>(z + (uint64_t)whole * T::PER, (int)rest);
             times<NV>([&](auto i) QSDP_INLINE {
@@ -77,16 +97,31 @@ struct Row {
             });
         }
     }
-    // f(i, index of the piece's first element) for the pieces that the thread's wave has any of. The pieces are made opaque:
-    // otherwise the compiler keeps their elements unpacked from one pass to the next, in twice the registers and more.
+    // f(piece, i, index of its first element) for the pieces that the thread's wave has any of. Those in registers are made
+    // opaque: otherwise the compiler keeps their elements unpacked from one pass to the next, in twice the registers and more.
     template <class F>
-    __device__ __forceinline__ void pieces_of_wave(F f) {
+    __device__ __forceinline__ void in_registers(F f) {
         times<NV>([&](auto i) QSDP_INLINE { asm volatile("" : "+v"(v[i])); });
         const uint32_t end = fresh(pieces), wave = (uint32_t)wave_index() * 64, lane = threadIdx.x % 64;
         times<NV>([&](auto i) QSDP_INLINE {
             const uint32_t at = first + i * THREADS + wave;
-            if (at < end) f(i, (at + lane) * T::PER);
+            if (at < end) f(v[i], i, (at + lane) * T::PER);
         });
+    }
+    template <class F>
+    __device__ __forceinline__ void in_lds(F f) {
+        if constexpr (HELD > 0) {
+            const uint32_t end = fresh(pieces), wave = (uint32_t)wave_index() * 64, thread = fresh_thread();
+            times<HELD>([&](auto i) QSDP_INLINE {
+                const uint32_t at = CHUNK + i * THREADS + wave;
+                if (at < end) f(held[i * THREADS + thread], i, (at + thread % 64) * T::PER);
+            });
+        }
+    }
+    template <class F>
+    __device__ __forceinline__ void pieces_of_wave(F f) {
+        in_registers(f);
+        in_lds(f);
     }
     // all chunks in turn; a row of one chunk stays where it is
     template <class F>
@@ -107,43 +142,54 @@ struct Row {
     // to[..] = f(element) for all of them; the piece that the row ends in goes by itself, once for all i
     template <class F>
     __device__ __forceinline__ void write(typename T::raw* to, F f) {
-        const uint32_t whole = fresh(n) / T::PER, thread = fresh_thread();
-        pieces_of_wave([&](auto i, uint32_t) QSDP_INLINE {
+        const uint32_t whole = fresh(n) / T::PER;
+        pieces_of_wave([&](const u32x4& piece, auto, uint32_t index) QSDP_INLINE {
             float d[T::PER];
+            const u32x4 here = piece;
             times<T::PER>([&](auto e) QSDP_INLINE {
-                d[e] = f(T::at(v[i], e));
+                d[e] = f(T::at(here, e));
                 keep_order(e);
             });
-            const uint32_t at = first + i * THREADS;
-            if (at + thread < whole) store16<T>(to + (uint64_t)at * T::PER + thread * T::PER, T::pack(d));
+            if (index < whole * T::PER) store16<T>(to + index, T::pack(d));
         });
-        const uint32_t rest = n % T::PER, slot = whole - first;
-        if (rest != 0 && slot < CHUNK && slot % THREADS == thread) {
+        const uint32_t rest = n % T::PER, slot = whole - first, thread = threadIdx.x;
+        if (rest != 0 && slot < CHUNK + (HELD > 0 ? kHeld : 0) && slot % THREADS == thread) {
             u32x4 last = v[0];
             times<NV>([&](auto i) QSDP_INLINE {
                 if (slot / THREADS == (uint32_t)i) last = v[i];
             });
+            if (HELD > 0 && slot >= CHUNK) last = held[slot - CHUNK];
             float d[T::PER];
             times<T::PER>([&](auto e) QSDP_INLINE { d[e] = f(T::at(last, e)); });
             store_part<T>(to + (uint64_t)whole * T::PER, T::pack(d), (int)rest);
         }
     }
-    // A bit for every element of the thread for which hit(value) holds: bit i * PER + e. -inf past the row counts like any.
-    template <class H>
+    // A bit for every element of the thread in registers, or in LDS, for which hit(value) holds: bit i * PER + e. -inf past the
+    // row counts like any.
+    template <bool LDS, class H>
     __device__ __forceinline__ uint64_t mask(H hit) {
-        static_assert(NV * T::PER <= 64, "a bit for every element");
+        static_assert((NV > HELD ? NV : HELD) * T::PER <= 64, "a bit for every element");
         uint32_t low = 0, high = 0;
-        pieces_of_wave([&](auto i, uint32_t) QSDP_INLINE {
+        auto look = [&](const u32x4& piece, auto i, uint32_t) QSDP_INLINE {
+            const u32x4 here = piece;
             times<T::PER>([&](auto e) QSDP_INLINE {
-                const int bit = i * T::PER + e;
-                if (bit < 32) low |= hit(T::at(v[i], e)) ? 1u << bit : 0u;
-                else high |= hit(T::at(v[i], e)) ? 1u << (bit - 32) : 0u;
+                constexpr int bit = decltype(i)::value * T::PER + decltype(e)::value;
+                if (bit < 32) low |= hit(T::at(here, e)) ? 1u << (bit % 32) : 0u;
+                else high |= hit(T::at(here, e)) ? 1u << (bit % 32) : 0u;
             });
-        });
+        };
+        if constexpr (LDS) in_lds(look);
+        else in_registers(look);
         return (uint64_t)high << 32 | low;
     }
+    template <class H>
+    __device__ __forceinline__ uint32_t count(H hit) {
+        return (uint32_t)__popcll(mask<false>(hit)) + (HELD > 0 ? (uint32_t)__popcll(mask<true>(hit)) : 0u);
+    }
+    // element of a bit of the mask
+    template <bool LDS>
     __device__ __forceinline__ uint32_t index_of(int bit) const {
-        return (first + (uint32_t)bit / T::PER * THREADS + threadIdx.x) * T::PER + (uint32_t)bit % T::PER;
+        return ((LDS ? CHUNK : first) + (uint32_t)bit / T::PER * THREADS + threadIdx.x) * T::PER + (uint32_t)bit % T::PER;
     }
 };
 
@@ -162,46 +208,58 @@ __device__ __forceinline__ void rescale(Sums& a, float top, float scale2) {
     a.m = top;
 }
 
-// A wave's sums over its pieces of every chunk, the maximum its own: no workgroup has to meet for it.
-template <bool MEAN, class R, class T>
-__device__ __forceinline__ void add_chunk(R& row, float scale2, Sums& a, T) {
-    float m = a.m;
-    row.pieces_of_wave([&](auto i, uint32_t) QSDP_INLINE {
-        times<T::PER>([&](auto e) QSDP_INLINE { m = fmaxf(m, T::at(row.v[i], e)); });
+// Adds a chunk to a wave's sums, lane by lane; the maximum is the wave's own, so that no workgroup has to meet for it, and
+// `most` the lane's. MORE: the sum of another power of the same differences as well, of 2^(a * ratio).
+enum class Second { NONE, SQUARE, OTHER };
+
+template <bool MEAN, Second MORE, class R, class T>
+__device__ __forceinline__ void add_chunk(R& row, float scale2, float other2, Sums& a, float& second, float& most, T) {
+    row.pieces_of_wave([&](const u32x4& piece, auto, uint32_t) QSDP_INLINE {
+        const u32x4 here = piece;
+        times<T::PER>([&](auto e) QSDP_INLINE { most = fmaxf(most, T::at(here, e)); });
     });
-    m = reduce64(m, Max());
-    rescale(a, m, scale2);
+    const float m = reduce64(most, Max());
+    if (a.m != m) {
+        if (MORE == Second::SQUARE) second *= exp2_fast(2.0f * shift_of(a.m, m, scale2));
+        if (MORE == Second::OTHER) second *= exp2_fast(shift_of(a.m, m, other2));
+        rescale(a, m, scale2);
+    }
     const float at = m == kNegInf ? 0.0f : m;
-    float s = 0.0f, u = 0.0f;
-    row.pieces_of_wave([&](auto i, uint32_t) QSDP_INLINE {
+    row.pieces_of_wave([&](const u32x4& piece, auto, uint32_t) QSDP_INLINE {
+        const u32x4 here = piece;
         times<T::PER>([&](auto e) QSDP_INLINE {
-            const float d = (T::at(row.v[i], e) - at) * scale2;
-            const float p = exp2_fast(d);
-            s += p;
-            if (MEAN) u = fmaf(p, fmaxf(d, kLeast), u);
+            const float d = T::at(here, e) - at;
+            const float p = exp2_fast(d * scale2);
+            a.s += p;
+            if (MEAN) a.u = fmaf(p, fmaxf(d * scale2, kLeast), a.u);
+            if (MORE == Second::SQUARE) second = fmaf(p, p, second);
+            if (MORE == Second::OTHER) second += exp2_fast(d * other2);
             keep_order(e);
         });
     });
-    a.s += s;  // lane by lane; the wave's lanes are added up by join
-    if (MEAN) a.u += u;
 }
 
-// The workgroup's sums from its waves'; every thread gets them. room: 3 floats for each wave.
-template <int THREADS, bool MEAN>
-__device__ __forceinline__ Sums join(Sums a, float scale2, float (*room)[3]) {
+// The workgroup's sums from its waves'; every thread gets them. room: 4 floats for each wave.
+template <int THREADS, bool MEAN, Second MORE>
+__device__ __forceinline__ Sums join(Sums a, float scale2, float other2, float& second, float (*room)[4]) {
     constexpr int WAVES = THREADS / 64;
     a.s = reduce64(a.s, Add());
     if (MEAN) a.u = reduce64(a.u, Add());
+    if (MORE != Second::NONE) second = reduce64(second, Add());
     if (threadIdx.x % 64 == 0) {
         float* w = room[threadIdx.x / 64];
-        w[0] = a.m, w[1] = a.s, w[2] = a.u;
+        w[0] = a.m, w[1] = a.s, w[2] = a.u, w[3] = second;
     }
     __syncthreads();
     const int w = threadIdx.x % 16;
     Sums b = {kNegInf, 0.0f, 0.0f};
-    if (w < WAVES) b = {room[w][0], room[w][1], room[w][2]};
+    float c = 0.0f;
+    if (w < WAVES) b = {room[w][0], room[w][1], room[w][2]}, c = room[w][3];
     const float m = reduce16(b.m, Max());
+    if (MORE == Second::SQUARE) c *= exp2_fast(b.m == m ? 0.0f : 2.0f * shift_of(b.m, m, scale2));
+    if (MORE == Second::OTHER) c *= exp2_fast(b.m == m ? 0.0f : shift_of(b.m, m, other2));
     rescale(b, m, scale2);
+    if (MORE != Second::NONE) second = reduce16(c, Add());
     return {m, reduce16(b.s, Add()), MEAN ? reduce16(b.u, Add()) : 0.0f};
 }
 
@@ -235,16 +293,17 @@ struct TopRoom {
 // few and read from memory once more: which of its registers a thread needs is not known when the code is compiled.
 template <class T, int THREADS, class R, class H>
 __device__ __forceinline__ void collect(R& row, TopRoom<THREADS>& room, H hit) {
-    row.again();
-    row.each_chunk([&]() QSDP_INLINE {
-        uint64_t mine = row.mask(hit);
+    auto append = [&](uint64_t mine, auto lds) QSDP_INLINE {
         if (mine == 0) return;
         uint32_t to = atomicAdd(&room.count, (uint32_t)__popcll(mine));
         for (; mine != 0 && to < kRoom; mine &= mine - 1, ++to) {
-            const uint32_t index = row.index_of(__ffsll((unsigned long long)mine) - 1);
+            const uint32_t index = row.template index_of<decltype(lds)::value>(__ffsll((unsigned long long)mine) - 1);
             room.list[to] = (uint64_t)value_key(T::get(row.z[index])) << 32 | ~index;
         }
-    });
+    };
+    row.again();
+    row.each_chunk([&]() QSDP_INLINE { append(row.template mask<false>(hit), std::false_type()); });
+    if (R::HELD > 0) append(row.template mask<true>(hit), std::true_type());
 }
 
 // The `top` first elements, as keys in room.list[0 .. return value), in no order and with some more. Threshold: the top-th
@@ -252,17 +311,11 @@ __device__ __forceinline__ void collect(R& row, TopRoom<THREADS>& room, H hit) {
 // -g log(1 - top / g) of g groups: 74 for 64). Where too many reach it (ties, masks, large values in few groups) or a NaN takes
 // part, the top-th value itself is found bit by bit, and of its equals the first by index are taken.
 template <class T, int THREADS, class R>
-__device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, TopRoom<THREADS>& room) {
+__device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, float most, TopRoom<THREADS>& room) {
     constexpr int GROUPS = TopRoom<THREADS>::GROUPS, SHARE = THREADS / GROUPS, LOW = key_low_bits<T>();
     const int lane = threadIdx.x % 64, wave = wave_index();
     if (threadIdx.x == 0) room.count = 0;
-    float m = kNegInf;
-    row.again();
-    row.each_chunk([&]() QSDP_INLINE {
-        row.pieces_of_wave([&](auto i, uint32_t) QSDP_INLINE {
-            times<T::PER>([&](auto e) QSDP_INLINE { m = fmaxf(m, T::at(row.v[i], e)); });
-        });
-    });
+    float m = most;  // the thread's
     if (SHARE >= 2) m = fmaxf(m, dpp<0xB1>(m));
     if (SHARE >= 4) m = fmaxf(m, dpp<0x4E>(m));
     if (threadIdx.x % SHARE == 0) room.group[threadIdx.x / SHARE] = value_key(m);
@@ -298,14 +351,14 @@ __device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, T
         if (!known) {
             uint32_t nans = 0;
             row.again();
-            row.each_chunk([&]() QSDP_INLINE { nans += __popcll(row.mask([](float z) QSDP_INLINE { return z != z; })); });
+            row.each_chunk([&]() QSDP_INLINE { nans += row.count([](float z) QSDP_INLINE { return z != z; }); });
             nans = reduce_block<THREADS>(nans, Add(), room.words);
             least = 0;
             for (int bit = 31; bit >= 0; --bit) {
                 const float trial = key_value(least | 1u << bit);  // nothing reaches a NaN but NaNs
                 uint32_t reach = 0;
                 row.again();
-                row.each_chunk([&]() QSDP_INLINE { reach += __popcll(row.mask([&](float z) QSDP_INLINE { return z >= trial; })); });
+                row.each_chunk([&]() QSDP_INLINE { reach += row.count([&](float z) QSDP_INLINE { return z >= trial; }); });
                 if (reduce_block<THREADS>(reach, Add(), room.words) + nans >= top) least |= 1u << bit;
             }
             least = least < kKeyNegInf ? kKeyNegInf : least;
@@ -323,12 +376,10 @@ __device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, T
     // of the equal ones the first by index: a piece of every thread at a time, which is the order of the row
     uint32_t found = above;
     const uint64_t below = (1ull << lane) - 1;
-    row.again();
-    for (uint32_t c = 0; c < row.chunks() && found < top; ++c) {
-        if (c > 0) row.load(c);
-        uint64_t mine = row.mask([&](float z) QSDP_INLINE { return z == bound || (z != z && bound != bound); });
-        for (uint32_t i = 0; i < R::CHUNK / THREADS && found < top; ++i, mine >>= T::PER) {
-            const uint32_t index = row.index_of(i * T::PER);
+    auto equal = [&](float z) QSDP_INLINE { return z == bound || (z != z && bound != bound); };
+    auto take = [&](uint64_t mine, auto lds, uint32_t rounds) QSDP_INLINE {
+        for (uint32_t i = 0; i < rounds && found < top; ++i, mine >>= T::PER) {
+            const uint32_t index = row.template index_of<decltype(lds)::value>((int)i * T::PER);
             uint32_t bits = (uint32_t)mine & ((1u << T::PER) - 1);
             if (index + T::PER > row.n) bits &= index < row.n ? (1u << (row.n - index)) - 1 : 0u;
             const uint32_t many = __popc(bits);
@@ -350,20 +401,29 @@ __device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, T
             for (; bits != 0 && to < top; bits &= bits - 1, ++to)
                 room.list[to] = (uint64_t)least << 32 | ~(index + (uint32_t)(__ffs((int)bits) - 1));
         }
+    };
+    row.again();
+    for (uint32_t c = 0; c < row.chunks() && found < top; ++c) {
+        if (c > 0) row.load(c);
+        take(row.template mask<false>(equal), std::false_type(), R::CHUNK / THREADS);
     }
+    if (R::HELD > 0 && found < top) take(row.template mask<true>(equal), std::true_type(), R::HELD);
     __syncthreads();
     return top;
 }
 
-template <class T, int THREADS, int NV, bool STREAM, bool TOP>
-__device__ __forceinline__ void score_row(const ScoreParams& p, uint64_t r) {
-    __shared__ float waves[THREADS / 64][3];
+template <class T, int THREADS, int NV, Rest REST, bool TOP>
+__global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void score_kernel(ScoreParams p) {
+    __shared__ float waves[THREADS / 64][4];
+    __shared__ u32x4 held[REST == Rest::HELD ? kHeld : 1];
+    const uint64_t r = p.in.first + blockIdx.x;
     const auto* z = static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride;
     const float scale2 = p.in.inv_temperature * kLog2e;
-    Row<T, THREADS, NV, STREAM> row(z, p.in.vocab);
+    Row<T, THREADS, NV, REST> row(z, p.in.vocab, held);
     Sums a = {kNegInf, 0.0f, 0.0f};
-    row.each_chunk([&]() QSDP_INLINE { add_chunk<true>(row, scale2, a, T()); });
-    a = join<THREADS, true>(a, scale2, waves);
+    float most = kNegInf, none = 0.0f;
+    row.each_chunk([&]() QSDP_INLINE { add_chunk<true, Second::NONE>(row, scale2, 0.0f, a, none, most, T()); });
+    a = join<THREADS, true, Second::NONE>(a, scale2, 0.0f, none, waves);
     const bool empty = a.s == 0.0f;
     const float log_total = logf(a.s);
     if (threadIdx.x == 0) {
@@ -383,7 +443,7 @@ __device__ __forceinline__ void score_row(const ScoreParams& p, uint64_t r) {
     if constexpr (TOP) {
         __shared__ TopRoom<THREADS> room;
         const uint32_t top = (uint32_t)p.top;
-        const uint32_t count = top_list<T>(row, top, a.s == a.s, room);
+        const uint32_t count = top_list<T>(row, top, a.s == a.s, most, room);
         for (uint32_t i = threadIdx.x; i < count; i += THREADS) {
             const uint64_t key = room.list[i];
             uint32_t rank = 0;
@@ -395,11 +455,6 @@ __device__ __forceinline__ void score_row(const ScoreParams& p, uint64_t r) {
             }
         }
     }
-}
-
-template <class T, int THREADS, int NV, bool STREAM, bool TOP>
-__global__ __launch_bounds__(THREADS, STREAM ? 4 : 8) void score_kernel(ScoreParams p) {
-    score_row<T, THREADS, NV, STREAM, TOP>(p, p.in.first + blockIdx.x);
 }
 
 // ---- gradient of log probability and entropy --------------------------------------------------------------------------
@@ -427,13 +482,14 @@ struct Segment {
             else if (at == n / T::PER) v[i] = load_part<T>(z + (uint64_t)at * T::PER, (int)(n % T::PER));
         });
     }
-    // dz[j] = f(z[j], j)
+    // dz[j] = f(z[j], j), and `more` on top at one place (~0: nowhere)
     template <class F>
-    __device__ __forceinline__ void write(const u32x4* v, typename T::raw* dz, F f) const {
+    __device__ __forceinline__ void write(const u32x4* v, typename T::raw* dz, F f, uint32_t place, float more) const {
         times<kSegment>([&](auto i) QSDP_INLINE {
             const uint32_t at = first + i * 256 + threadIdx.x;
             float d[T::PER];
             times<T::PER>([&](auto e) QSDP_INLINE { d[e] = f(T::at(v[i], e), at * T::PER + e); });
+            if (place / T::PER == at) times<T::PER>([&](auto e) QSDP_INLINE { d[e] += place % T::PER == e ? more : 0.0f; });
             if (at < n / T::PER) store16<T>(dz + (uint64_t)at * T::PER, T::pack(d));
             else if (at == n / T::PER) store_part<T>(dz + (uint64_t)at * T::PER, T::pack(d), (int)(n % T::PER));
         });
@@ -450,18 +506,20 @@ __global__ __launch_bounds__(256) void score_backward_kernel(ScoreBackwardParams
     u32x4 v[kSegment];
     part.load(static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride, v);
     const float m = p.stats[2 * r], log_total = p.stats[2 * r + 1], log2_total = log_total * kLog2e;
-    const bool empty = log_total == kNegInf;
+    auto* dz = static_cast<typename T::raw*>(p.d_logits) + r * p.d_stride;
+    if (log_total == kNegInf) {
+        part.write(v, dz, [](float, uint32_t) QSDP_INLINE { return 0.0f; }, ~0u, 0.0f);
+        return;
+    }
     const int64_t asked = p.d_logprob && p.tokens ? p.tokens[r] : -1;
-    const uint32_t token = (uint64_t)asked < (uint64_t)n && !empty ? (uint32_t)asked : ~0u;  // ~0: none
+    const uint32_t token = (uint64_t)asked < (uint64_t)n ? (uint32_t)asked : ~0u;  // ~0: none
     const float g = token != ~0u ? p.d_logprob[r] * p.in.inv_temperature : 0.0f;
     const float h = ENTROPY ? p.d_entropy[r] * p.in.inv_temperature * kLn2 : 0.0f;  // entropies in bits below
-    const float entropy = ENTROPY ? p.entropy[r] * kLog2e : 0.0f;
-    part.write(v, static_cast<typename T::raw*>(p.d_logits) + r * p.d_stride, [&](float z, uint32_t j) QSDP_INLINE {
+    const float off = ENTROPY ? fmaf(h, p.entropy[r] * kLog2e, g) : g;
+    part.write(v, dz, [&](float z, uint32_t) QSDP_INLINE {
         const float a = fmaf(z - m, scale2, -log2_total);
-        const float prob = exp2_fast(a);
-        const float d = -prob * (ENTROPY ? fmaf(h, fmaxf(a, kLeast) + entropy, g) : g);
-        return empty ? 0.0f : j == token ? d + g : d;
-    });
+        return -exp2_fast(a) * (ENTROPY ? fmaf(h, fmaxf(a, kLeast), off) : off);
+    }, token, g);
 }
 
 // ---- distillation ------------------------------------------------------------------------------------------------------
@@ -481,9 +539,9 @@ __device__ __forceinline__ uint32_t label_of(int64_t asked, uint32_t n) {  // ~0
 }
 
 // One exponential: at 1 where the list has no part, else at the temperature.
-template <bool BOTH>
+template <Second MORE>
 __device__ __forceinline__ float one_scale2(const DistillParams& p) {
-    return !BOTH && p.alpha == 0.0f ? kLog2e : p.in.inv_temperature * kLog2e;
+    return MORE == Second::NONE && p.alpha == 0.0f ? kLog2e : p.in.inv_temperature * kLog2e;
 }
 
 template <class T, int THREADS>
@@ -515,10 +573,11 @@ __device__ __forceinline__ bool fill_list(const DistillParams& p, const typename
 }
 
 // What the gradient of a row's loss is made of: d z_v = soft 2^(...) + hard 2^(...), less the targets at the list's places and
-// at the label. BOTH: the temperature's exponentials and those at 1 are two; otherwise one serves (scale2).
-template <bool BOTH>
+// at the label. MORE: the exponentials at 1 are others than the
+// temperature's (scale2), or their squares at temperature 2; otherwise one serves.
+template <Second MORE>
 struct Slope {
-    float m, scale2, soft_log, hard_log, soft, hard, one;
+    float m, scale2, soft_log, hard_log, soft, hard, one, square;
     uint32_t label;  // ~0: none
     __device__ __forceinline__ Slope(const DistillParams& p, float scale2_, float m_, float soft_log_, float hard_log_, bool taught,
                                      uint32_t label_, float g)
@@ -526,12 +585,16 @@ struct Slope {
         soft = same(taught ? g * p.alpha * p.temperature : 0.0f);
         hard = same(label != ~0u ? g * (1.0f - p.alpha) : 0.0f);
         one = same(soft + hard);
+        // p^2 = 2^(2 (...) - 2 soft_log): what it takes to have hard_log there
+        square = same(MORE == Second::SQUARE && hard != 0.0f ? hard * exp2f(2.0f * soft_log - hard_log) : 0.0f);
     }
     __device__ __forceinline__ bool nothing() const { return soft_log == kNegInf || (soft == 0.0f && hard == 0.0f); }
     __device__ __forceinline__ float operator()(float v) const {
         const float d = v - m;
-        if (!BOTH) return one * exp2_fast(fmaf(d, scale2, -soft_log));
-        return fmaf(hard, exp2_fast(fmaf(d, kLog2e, -hard_log)), soft * exp2_fast(fmaf(d, scale2, -soft_log)));
+        const float p = exp2_fast(fmaf(d, scale2, -soft_log));
+        if (MORE == Second::NONE) return one * p;
+        if (MORE == Second::SQUARE) return fmaf(square * p, p, soft * p);
+        return fmaf(hard, exp2_fast(fmaf(d, kLog2e, -hard_log)), soft * p);
     }
     __device__ __forceinline__ float target(const List& list, int top, uint32_t j) const {
         float sum = 0.0f;
@@ -554,28 +617,26 @@ struct Slope {
 };
 
 // Loss, and in the same pass the gradient if it is asked for.
-template <class T, int THREADS, int NV, bool STREAM, bool BOTH>
-__global__ __launch_bounds__(THREADS, STREAM ? 4 : 8) void distill_kernel(DistillParams p) {
-    __shared__ float waves[THREADS / 64][3], waves1[THREADS / 64][3], scratch[THREADS / 64];
+template <class T, int THREADS, int NV, Rest REST, Second MORE>
+__global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void distill_kernel(DistillParams p) {
+    __shared__ float waves[THREADS / 64][4], scratch[THREADS / 64];
+    __shared__ u32x4 held[REST == Rest::HELD ? kHeld : 1];
     __shared__ List list;
     const uint64_t r = p.in.first + blockIdx.x;
     const uint32_t n = (uint32_t)p.in.vocab;
     const auto* z = static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride;
-    const float scale2 = one_scale2<BOTH>(p);
-    Row<T, THREADS, NV, STREAM> row(z, n);
+    const float scale2 = one_scale2<MORE>(p);
+    Row<T, THREADS, NV, REST> row(z, n, held);
     const bool taught = fill_list<T, THREADS>(p, z, r, list, scratch);
     const int64_t asked = p.labels && p.alpha < 1.0f ? p.labels[r] : -1;
     const uint32_t label = label_of(asked, n);
     const float z_label = same(label != ~0u ? T::get(z[label]) : 0.0f);
-    Sums a = {kNegInf, 0.0f, 0.0f}, b = a;
-    row.each_chunk([&]() QSDP_INLINE {
-        add_chunk<false>(row, scale2, a, T());
-        if (BOTH) add_chunk<false>(row, kLog2e, b, T());
-    });
-    a = join<THREADS, false>(a, scale2, waves);
+    Sums a = {kNegInf, 0.0f, 0.0f};
+    float most = kNegInf, second = 0.0f;
+    row.each_chunk([&]() QSDP_INLINE { add_chunk<false, MORE>(row, scale2, kLog2e, a, second, most, T()); });
+    a = join<THREADS, false, MORE>(a, scale2, kLog2e, second, waves);
     // maximum, log2 of the sums at the temperature and at 1
-    const float m = same(a.m), soft_log = same(log2f(a.s));
-    const float hard_log = BOTH ? same(log2f(join<THREADS, false>(b, kLog2e, waves1).s)) : soft_log;
+    const float m = same(a.m), soft_log = same(log2f(a.s)), hard_log = MORE == Second::NONE ? soft_log : same(log2f(second));
     const bool empty = soft_log == kNegInf;
     const int k = (int)threadIdx.x;
     float kl = 0.0f;
@@ -599,7 +660,7 @@ __global__ __launch_bounds__(THREADS, STREAM ? 4 : 8) void distill_kernel(Distil
     }
     if (!p.d_logits) return;
     auto* dz = static_cast<typename T::raw*>(p.d_logits) + r * p.d_stride;
-    const Slope<BOTH> slope(p, scale2, m, soft_log, hard_log, taught, label, same(p.row_scale ? p.row_scale[r] : 1.0f));
+    const Slope<MORE> slope(p, scale2, m, soft_log, hard_log, taught, label, same(p.row_scale ? p.row_scale[r] : 1.0f));
     row.again();
     __syncthreads();  // the list is there, and what is read outside the own pieces has been read
     if (slope.nothing()) {
@@ -612,7 +673,7 @@ __global__ __launch_bounds__(THREADS, STREAM ? 4 : 8) void distill_kernel(Distil
 }
 
 // The gradient alone, from the row's statistics: rows are cut into pieces as for the gradient of log probabilities.
-template <class T, bool BOTH>
+template <class T, Second MORE>
 __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p) {
     __shared__ float scratch[4];
     __shared__ List list;
@@ -626,11 +687,11 @@ __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p) 
     const bool taught = fill_list<T, 256>(p, z, r, list, scratch);
     const uint32_t label = label_of(p.labels && p.alpha < 1.0f ? p.labels[r] : -1, n);
     const float z_label = same(label != ~0u ? T::get(z[label]) : 0.0f);
-    const Slope<BOTH> slope(p, one_scale2<BOTH>(p), same(p.stats[3 * r]), same(p.stats[3 * r + 1] * kLog2e),
+    const Slope<MORE> slope(p, one_scale2<MORE>(p), same(p.stats[3 * r]), same(p.stats[3 * r + 1] * kLog2e),
                             same(p.stats[3 * r + 2] * kLog2e), taught, label, same(p.d_loss[r]));
     const bool nothing = slope.nothing();
     __syncthreads();  // the list is there
-    part.write(v, dz, [&](float v, uint32_t) QSDP_INLINE { return nothing ? 0.0f : slope(v); });
+    part.write(v, dz, [&](float v, uint32_t) QSDP_INLINE { return nothing ? 0.0f : slope(v); }, ~0u, 0.0f);
     if (nothing) return;
     __syncthreads();
     slope.template aim<T>(list, p.top, z_label, dz, part.lo(), part.hi());
@@ -653,17 +714,22 @@ hipError_t go(void (*kernel)(P), int threads, uint64_t work, P p, hipStream_t s)
 }
 
 // Threads and pieces per thread by the row's length: the smallest team that holds it, as 64 registers to a lane keep a
-// compute unit's 2048 threads; longer rows take fewer, larger threads, and the longest pass chunk by chunk.
+// compute unit's 2048 threads; then with LDS, and the longest pass chunk by chunk.
+template <Rest REST>
+using RestOf = std::integral_constant<Rest, REST>;
+
 template <class T, class F>
 hipError_t by_length(uint64_t n, F f) {
     const uint64_t pieces = (n + T::PER - 1) / T::PER;
-    std::integral_constant<int, 2> two;
-    std::integral_constant<int, 8> eight;
-    if (pieces <= 128 * 2) return f(std::integral_constant<int, 128>(), two, std::false_type());
-    if (pieces <= 256 * 8) return f(std::integral_constant<int, 256>(), eight, std::false_type());
-    if (pieces <= 512 * 8) return f(std::integral_constant<int, 512>(), eight, std::false_type());
-    if (pieces <= 1024 * 8) return f(std::integral_constant<int, 1024>(), eight, std::false_type());
-    return f(std::integral_constant<int, 1024>(), eight, std::true_type());
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 8> eight;
+    const std::integral_constant<int, 1024> most;
+    if (pieces <= 128 * 2) return f(std::integral_constant<int, 128>(), two, RestOf<Rest::NONE>());
+    if (pieces <= 256 * 8) return f(std::integral_constant<int, 256>(), eight, RestOf<Rest::NONE>());
+    if (pieces <= 512 * 8) return f(std::integral_constant<int, 512>(), eight, RestOf<Rest::NONE>());
+    if (pieces <= 1024 * 8) return f(most, eight, RestOf<Rest::NONE>());
+    if (pieces <= 1024 * 8 + kHeld) return f(most, eight, RestOf<Rest::HELD>());
+    return f(most, eight, RestOf<Rest::STREAM>());
 }
 
 template <class F>
@@ -676,9 +742,9 @@ hipError_t by_format(qsdp_dtype dtype, F f) {
 hipError_t launch_score(qsdp_dtype dtype, const ScoreParams& p, hipStream_t s) {
     return by_format(dtype, [&](auto t) {
         using T = decltype(t);
-        return by_length<T>(p.in.vocab, [&](auto threads, auto nv, auto stream) {
-            if (p.top) return go(score_kernel<T, threads, nv, stream, true>, threads, p.in.rows, p, s);
-            return go(score_kernel<T, threads, nv, stream, false>, threads, p.in.rows, p, s);
+        return by_length<T>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+            if (p.top) return go(score_kernel<T, threads, nv, rest, true>, threads, p.in.rows, p, s);
+            return go(score_kernel<T, threads, nv, rest, false>, threads, p.in.rows, p, s);
         });
     });
 }
@@ -694,16 +760,18 @@ hipError_t launch_score_backward(qsdp_dtype dtype, const ScoreBackwardParams& p,
 
 hipError_t launch_distill(qsdp_dtype dtype, const DistillParams& p, hipStream_t s) {
     const bool both = p.alpha > 0.0f && p.alpha < 1.0f && p.temperature != 1.0f;
+    auto by_second = [&](auto f) {
+        if (!both) return f(std::integral_constant<Second, Second::NONE>());
+        if (p.temperature == 2.0f) return f(std::integral_constant<Second, Second::SQUARE>());
+        return f(std::integral_constant<Second, Second::OTHER>());
+    };
     return by_format(dtype, [&](auto t) {
         using T = decltype(t);
-        if (!p.loss) {
-            const uint64_t work = p.in.rows * Segment<T>::of(p.in.vocab);
-            return both ? go(distill_backward_kernel<T, true>, 256, work, p, s)
-                        : go(distill_backward_kernel<T, false>, 256, work, p, s);
-        }
-        return by_length<T>(p.in.vocab, [&](auto threads, auto nv, auto stream) {
-            if (both) return go(distill_kernel<T, threads, nv, stream, true>, threads, p.in.rows, p, s);
-            return go(distill_kernel<T, threads, nv, stream, false>, threads, p.in.rows, p, s);
+        return by_second([&](auto more) {
+            if (!p.loss) return go(distill_backward_kernel<T, more>, 256, p.in.rows * Segment<T>::of(p.in.vocab), p, s);
+            return by_length<T>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+                return go(distill_kernel<T, threads, nv, rest, more>, threads, p.in.rows, p, s);
+            });
         });
     });
 }
