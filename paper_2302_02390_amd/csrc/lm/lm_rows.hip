@@ -51,13 +51,15 @@ __device__ __forceinline__ float exp2_fast(float a) { return __builtin_amdgcn_ex
 // The first NV are in registers, up to HELD more in LDS, in places that only their thread uses. STREAM: the row has more
 // pieces than the workgroup holds and passes through chunk by chunk.
 enum class Rest { NONE, HELD, STREAM };
-constexpr uint32_t kHeld = 4736;  // pieces in LDS: two workgroups to a compute unit's 160 KB, with what else they use
+// Pieces in LDS: two workgroups of 1024 threads, four of 512, to a compute unit's 160 KB, with what else they use.
+constexpr uint32_t held_pieces(int threads) { return threads == 1024 ? 4800 : 2240; }
 
 template <class T, int THREADS, int NV, Rest REST>
 struct Row {
     static constexpr uint32_t CHUNK = THREADS * NV;  // pieces in registers
     static constexpr bool STREAM = REST == Rest::STREAM;
-    static constexpr int HELD = REST == Rest::HELD ? (kHeld + THREADS - 1) / THREADS : 0;
+    static constexpr uint32_t ROOM = REST == Rest::HELD ? held_pieces(THREADS) : 0;
+    static constexpr int HELD = (int)((ROOM + THREADS - 1) / THREADS);
     const typename T::raw* z;
     u32x4* held;
     uint32_t n, pieces, first;
@@ -85,7 +87,7 @@ struct Row {
                 if (at + thread < whole) more[i] = load16<T>(z + (uint64_t)at * T::PER + thread * T::PER);
             });
             times<HELD>([&](auto i) QSDP_INLINE {
-                if (i * THREADS + thread < kHeld) held[i * THREADS + thread] = more[i];
+                if (i * THREADS + thread < ROOM) held[i * THREADS + thread] = more[i];
             });
             if (rest != 0 && slot >= CHUNK && slot % THREADS == thread)
                 held[slot - CHUNK] = load_part<T>(z + (uint64_t)whole * T::PER, (int)rest);
@@ -153,7 +155,7 @@ struct Row {
             if (index < whole * T::PER) store16<T>(to + index, T::pack(d));
         });
         const uint32_t rest = n % T::PER, slot = whole - first, thread = threadIdx.x;
-        if (rest != 0 && slot < CHUNK + (HELD > 0 ? kHeld : 0) && slot % THREADS == thread) {
+        if (rest != 0 && slot < CHUNK + ROOM && slot % THREADS == thread) {
             u32x4 last = v[0];
             times<NV>([&](auto i) QSDP_INLINE {
                 if (slot / THREADS == (uint32_t)i) last = v[i];
@@ -283,8 +285,10 @@ constexpr uint32_t kRoom = 512;  // candidates that are ranked
 template <int THREADS>
 struct TopRoom {
     static constexpr int GROUPS = THREADS < 256 ? THREADS : 256;
-    uint32_t group[GROUPS];
-    uint64_t list[kRoom];
+    union {
+        uint32_t group[GROUPS];  // until the threshold is known
+        uint64_t list[kRoom];
+    };
     uint32_t words[THREADS / 64];
     uint32_t count, least;
 };
@@ -415,7 +419,7 @@ __device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, f
 template <class T, int THREADS, int NV, Rest REST, bool TOP>
 __global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void score_kernel(ScoreParams p) {
     __shared__ float waves[THREADS / 64][4];
-    __shared__ u32x4 held[REST == Rest::HELD ? kHeld : 1];
+    __shared__ u32x4 held[REST == Rest::HELD ? held_pieces(THREADS) : 1];
     const uint64_t r = p.in.first + blockIdx.x;
     const auto* z = static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride;
     const float scale2 = p.in.inv_temperature * kLog2e;
@@ -620,7 +624,7 @@ struct Slope {
 template <class T, int THREADS, int NV, Rest REST, Second MORE>
 __global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void distill_kernel(DistillParams p) {
     __shared__ float waves[THREADS / 64][4], scratch[THREADS / 64];
-    __shared__ u32x4 held[REST == Rest::HELD ? kHeld : 1];
+    __shared__ u32x4 held[REST == Rest::HELD ? held_pieces(THREADS) : 1];
     __shared__ List list;
     const uint64_t r = p.in.first + blockIdx.x;
     const uint32_t n = (uint32_t)p.in.vocab;
@@ -726,9 +730,11 @@ hipError_t by_length(uint64_t n, F f) {
     const std::integral_constant<int, 1024> most;
     if (pieces <= 128 * 2) return f(std::integral_constant<int, 128>(), two, RestOf<Rest::NONE>());
     if (pieces <= 256 * 8) return f(std::integral_constant<int, 256>(), eight, RestOf<Rest::NONE>());
-    if (pieces <= 512 * 8) return f(std::integral_constant<int, 512>(), eight, RestOf<Rest::NONE>());
+    const std::integral_constant<int, 512> half;
+    if (pieces <= 512 * 8) return f(half, eight, RestOf<Rest::NONE>());
+    if (pieces <= 512 * 8 + held_pieces(512)) return f(half, eight, RestOf<Rest::HELD>());
     if (pieces <= 1024 * 8) return f(most, eight, RestOf<Rest::NONE>());
-    if (pieces <= 1024 * 8 + kHeld) return f(most, eight, RestOf<Rest::HELD>());
+    if (pieces <= 1024 * 8 + held_pieces(1024)) return f(most, eight, RestOf<Rest::HELD>());
     return f(most, eight, RestOf<Rest::STREAM>());
 }
 
