@@ -72,25 +72,25 @@ template <class T>
 __device__ __forceinline__ void store16(typename T::raw* p, u32x4 v) {
     __builtin_nontemporal_store(v, reinterpret_cast<u32x4_anywhere*>(p));
 }
-// The first `count` elements of 16 bytes, the others -inf.
+// Elements [from, to) of 16 bytes, the others -inf; and back.
 template <class T>
-__device__ __forceinline__ u32x4 load_part(const typename T::raw* p, int count) {
+__device__ __forceinline__ u32x4 load_part(const typename T::raw* p, int from, int to) {
     typename T::raw e[T::PER];
     u32x4 v = {T::NONE, T::NONE, T::NONE, T::NONE};
     __builtin_memcpy(e, &v, 16);
 #pragma unroll
     for (int k = 0; k < T::PER; ++k)
-        if (k < count) e[k] = p[k];
+        if (k >= from && k < to) e[k] = p[k];
     __builtin_memcpy(&v, e, 16);
     return v;
 }
 template <class T>
-__device__ __forceinline__ void store_part(typename T::raw* p, u32x4 v, int count) {
+__device__ __forceinline__ void store_part(typename T::raw* p, u32x4 v, int from, int to) {
     typename T::raw e[T::PER];
     __builtin_memcpy(e, &v, 16);
 #pragma unroll
     for (int k = 0; k < T::PER; ++k)
-        if (k < count) p[k] = e[k];
+        if (k >= from && k < to) p[k] = e[k];
 }
 
 // ---- reductions -------------------------------------------------------------------------------------------------------
