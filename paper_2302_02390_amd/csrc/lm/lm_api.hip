@@ -48,8 +48,7 @@ using namespace qsdp_lm;
 extern "C" {
 
 size_t qsdp_token_logprobs_bytes(uint64_t rows, uint64_t vocab, int top) {
-    (void)rows, (void)vocab, (void)top;
-    return 0;
+    return top < 0 || top > kMostTop ? 0 : parts_bytes(rows, vocab, top);
 }
 
 int qsdp_token_logprobs(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab, uint64_t row_stride,
@@ -64,8 +63,14 @@ int qsdp_token_logprobs(const void* logits, qsdp_dtype dtype, uint64_t rows, uin
     if (!aligned(logits, width(dtype)) || !aligned(tokens, 8) || !aligned(logprob, 4) || !aligned(entropy, 4) ||
         !aligned(stats, 4) || !aligned(top_logprob, 4) || !aligned(top_index, 4) || !aligned(workspace, 16))
         return QSDP_EALIGN;
-    const ScoreParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, tokens, top, logprob, entropy, stats,
-                           top_logprob, top_index};
+    ScoreParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, tokens, top, logprob, entropy, stats,
+                     top_logprob, top_index, 0, nullptr, nullptr};
+    const uint64_t parts = parts_bytes(rows, vocab, top);
+    if (workspace && parts && workspace_bytes >= parts) {
+        p.per = ((vocab + kParts - 1) / kParts + 7) / 8 * 8;  // the last part has at least a seventh of that, and the top
+        p.heads = static_cast<float4*>(workspace);
+        p.keys = reinterpret_cast<uint64_t*>(p.heads + rows * kParts);
+    }
     return status_of(launch_score(dtype, p, static_cast<hipStream_t>(stream)));
 }
 

@@ -76,7 +76,8 @@ __global__ __launch_bounds__(THREADS) void tokens_kernel(TokenParams p) {
     most = reduce_block<THREADS>(most, Max(), scratch);
     const float scale = most < __builtin_inff() ? most * (1.0f / 127.0f) : __builtin_nanf("");
     if (threadIdx.x == 0) p.scale[row] = scale;
-    const bool some = scale > 0.0f;
+    const float inv = 1.0f / scale;
+    const bool some = scale > 0.0f, plain = inv < 0x1p100f && inv > 0x1p-100f;  // the product is as good as the quotient
     for (uint32_t b = 0; b < p.buckets; ++b) {
         const uint32_t lo = b * (p.bucket / 8), hi = b + 1 == p.buckets ? pieces : lo + p.bucket / 8;
         int sum = 0;
@@ -86,14 +87,25 @@ __global__ __launch_bounds__(THREADS) void tokens_kernel(TokenParams p) {
                 const uint32_t at = first + i * THREADS + threadIdx.x;
                 if (at < lo || at >= hi) continue;
                 if (pieces > THREADS * NV) held[i].load(x, (uint64_t)at * 8, p.k);
-                uint32_t word[2] = {0, 0};
+                // x times 1 / s is within 2^-15 of x / s: unless it is that near to a tie, both round to the same code
+                float q[8], near = 1.0f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float q = fminf(fmaxf(rintf(held[i].v[e] / scale), -127.0f), 127.0f);
-                    const int c = some ? (int)q : 0;
-                    sum += c;
-                    word[e / 4] |= (uint32_t)(c & 0xff) << (e % 4 * 8);
+                    const float about = held[i].v[e] * inv;
+                    q[e] = rintf(about);
+                    near = fminf(near, fabsf(fabsf(about - q[e]) - 0.5f));
                 }
+                if (!(near > 0x1p-14f) || !plain)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) q[e] = rintf(held[i].v[e] / scale);
+                uint32_t word[2] = {0, 0};
+#pragma unroll
+                for (int e = 0; e < 8; ++e)  // as unsigned bytes about 128, turned into signed ones below
+                    word[e / 4] = __builtin_amdgcn_cvt_pk_u8_f32(fminf(fmaxf(q[e], -127.0f), 127.0f) + 128.0f, e % 4, word[e / 4]);
+                word[0] = some ? word[0] ^ 0x80808080u : 0u;
+                word[1] = some ? word[1] ^ 0x80808080u : 0u;
+                sum = __builtin_amdgcn_sdot4((int)word[0], 0x01010101, sum, false);
+                sum = __builtin_amdgcn_sdot4((int)word[1], 0x01010101, sum, false);
                 codes[at] = (uint64_t)word[1] << 32 | word[0];
             }
         }

@@ -46,6 +46,11 @@ __device__ __forceinline__ void keep_order(int e) {
 
 __device__ __forceinline__ float exp2_fast(float a) { return __builtin_amdgcn_exp2f(a); }  // 1 ulp, 0 below 2^-126
 
+// A value that is the same for all threads, in a scalar register.
+__device__ __forceinline__ float same(float v) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+}
+
 // ---- a row in pieces -----------------------------------------------------------------------------------------------
 // Piece i of a thread holds elements (first + i * THREADS + thread) * PER - lead ... of the row; what is not of the row is
 // -inf. Pieces start at multiples of four bytes: a row of 16-bit elements that does not has a lead of one (loads of 16 bytes at
@@ -209,6 +214,27 @@ struct Row {
     }
 };
 
+// ---- exponents -------------------------------------------------------------------------------------------------------------
+// (z - m) slope for many z, m the largest of them, by one multiply-add: z slope - back, with back = m slope rounded. `rest` is
+// what that rounding leaves, the same for all z: the true exponent is the multiply-add's plus rest, of a magnitude of 2^-24 of
+// back's. Where that is large (rows of the format's lowest value or highest) two different z are so far apart that only m's own
+// exponential is not zero: any power of two for slope keeps it so, and with it back is exact.
+struct Line {
+    float slope, back, rest;
+    __device__ __forceinline__ Line(float m, float slope_) : slope(slope_) {
+        m = m == kNegInf ? 0.0f : m;
+        back = m * slope;
+        rest = -fmaf(m, slope, -back);
+        if (!(fabsf(back) < 536870912.0f)) {
+            slope = ldexpf(1.0f, 59 - __builtin_amdgcn_frexp_expf(m));
+            back = m * slope;
+            rest = 0.0f;
+        }
+        slope = same(slope), back = same(back), rest = same(rest);
+    }
+    __device__ __forceinline__ float at(float z) const { return fmaf(z, slope, -back); }
+};
+
 // ---- sums of exponentials --------------------------------------------------------------------------------------------
 // The maximum m and, with a = (z - m) * scale2, the sums s of 2^a and u of 2^a a, over part of a row. Where nothing is
 // above -inf all three stay at their start; a NaN or +inf makes the sums NaN.
@@ -224,35 +250,81 @@ __device__ __forceinline__ void rescale(Sums& a, float top, float scale2) {
     a.m = top;
 }
 
+// The lane's maximum over the pieces of a chunk. A NaN may win or lose: the sums of its wave are NaN either way.
+template <class R>
+__device__ __forceinline__ float lane_max(R& row, F32) {
+    float most = kNegInf;
+    row.pieces_of_wave([&](const u32x4& piece, auto, uint32_t) QSDP_INLINE {
+        const u32x4 here = piece;
+        times<4>([&](auto e) QSDP_INLINE { most = fmaxf(most, F32::at(here, e)); });
+    });
+    return most;
+}
+template <class R>
+__device__ __forceinline__ float lane_max(R& row, F16) {  // two at a time
+    F16::pair most = {(_Float16)kNegInf, (_Float16)kNegInf};
+    row.pieces_of_wave([&](const u32x4& piece, auto, uint32_t) QSDP_INLINE {
+        const u32x4 here = piece;
+        times<4>([&](auto k) QSDP_INLINE {
+            const uint32_t word = here[(int)k];
+            most = __builtin_elementwise_max(most, __builtin_bit_cast(F16::pair, word));
+        });
+    });
+    return fmaxf((float)most[0], (float)most[1]);
+}
+template <class R>
+__device__ __forceinline__ float lane_max(R& row, BF16) {
+    // Two at a time as 16-bit integers: the largest signed one is the maximum unless it is negative; then all are, and the
+    // smallest unsigned one is.
+    typedef short two __attribute__((ext_vector_type(2)));
+    typedef unsigned short two_u __attribute__((ext_vector_type(2)));
+    two top = {-32768, -32768};
+    two_u low = {0xffff, 0xffff};
+    row.pieces_of_wave([&](const u32x4& piece, auto, uint32_t) QSDP_INLINE {
+        const u32x4 here = piece;
+        times<4>([&](auto k) QSDP_INLINE {
+            const uint32_t word = here[(int)k];
+            top = __builtin_elementwise_max(top, __builtin_bit_cast(two, word));
+            low = __builtin_elementwise_min(low, __builtin_bit_cast(two_u, word));
+        });
+    });
+    const int larger = top[0] > top[1] ? top[0] : top[1];
+    const uint32_t smaller = low[0] < low[1] ? low[0] : low[1];
+    const float most = __uint_as_float((larger >= 0 ? (uint32_t)larger : smaller) << 16);
+    return most == most ? most : kNegInf;  // of a lane with nothing, or a NaN
+}
+
 // Adds a chunk to a wave's sums, lane by lane; the maximum is the wave's own, so that no workgroup has to meet for it, and
 // `most` the lane's. MORE: the sum of another power of the same differences as well, of 2^(a * ratio).
 enum class Second { NONE, SQUARE, OTHER };
 
 template <bool MEAN, Second MORE, class R, class T>
-__device__ __forceinline__ void add_chunk(R& row, float scale2, float other2, Sums& a, float& second, float& most, T) {
-    row.pieces_of_wave([&](const u32x4& piece, auto, uint32_t) QSDP_INLINE {
-        const u32x4 here = piece;
-        times<T::PER>([&](auto e) QSDP_INLINE { most = fmaxf(most, T::at(here, e)); });
-    });
-    const float m = reduce64(most, Max());
+__device__ __forceinline__ void add_chunk(R& row, float scale2, float other2, Sums& a, float& second, float& most, T tag) {
+    most = fmaxf(most, lane_max(row, tag));
+    const float m = same(reduce64(most, Max()));
     if (a.m != m) {
         if (MORE == Second::SQUARE) second *= exp2_fast(2.0f * shift_of(a.m, m, scale2));
         if (MORE == Second::OTHER) second *= exp2_fast(shift_of(a.m, m, other2));
         rescale(a, m, scale2);
     }
-    const float at = m == kNegInf ? 0.0f : m;
+    const Line line(m, scale2), other(m, MORE == Second::OTHER ? other2 : 0.0f);
+    float s = 0.0f, u = 0.0f, o = 0.0f;
     row.pieces_of_wave([&](const u32x4& piece, auto, uint32_t) QSDP_INLINE {
         const u32x4 here = piece;
         times<T::PER>([&](auto e) QSDP_INLINE {
-            const float d = T::at(here, e) - at;
-            const float p = exp2_fast(d * scale2);
-            a.s += p;
-            if (MEAN) a.u = fmaf(p, fmaxf(d * scale2, kLeast), a.u);
-            if (MORE == Second::SQUARE) second = fmaf(p, p, second);
-            if (MORE == Second::OTHER) second += exp2_fast(d * other2);
+            const float z = T::at(here, e), d = line.at(z), p = exp2_fast(d);
+            s += p;
+            if (MEAN) u = fmaf(p, fmaxf(d, kLeast), u);
+            if (MORE == Second::SQUARE) o = fmaf(p, p, o);
+            if (MORE == Second::OTHER) o += exp2_fast(other.at(z));
             keep_order(e);
         });
     });
+    const float f = exp2_fast(line.rest);
+    a.s = fmaf(f, s, a.s);
+    if (MEAN) a.u = fmaf(f, fmaf(line.rest, s, u), a.u);
+    if (MORE == Second::SQUARE) second = fmaf(f * f, o, second);
+    if (MORE == Second::OTHER) second = fmaf(exp2_fast(other.rest), o, second);
 }
 
 // The workgroup's sums from its waves'; every thread gets them. room: 4 floats for each wave.
@@ -304,7 +376,7 @@ struct TopRoom {
         uint64_t list[kRoom];
     };
     uint32_t words[THREADS / 64];
-    uint32_t count, least;
+    uint32_t count, least, exact;
 };
 
 // Appends the row's elements for which hit(value) holds to the list, as far as it has room, and counts all of them. They are
@@ -349,13 +421,19 @@ __device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, f
 #pragma unroll
             for (int g = 0; g < GROUPS / 64; ++g) reach += __popcll(__ballot(key[g] >= trial));
             if (reach >= top) high = trial;
+            if (reach == top) break;  // the bits below need not be known
         }
         high <<= LOW;
         if ((int32_t)high >= 0) high |= (1u << LOW) - 1;  // a negative value's low bits
-        if (lane == 0) room.least = high;
+        high = high > kKeyNegInf ? high : kKeyNegInf;
+        uint32_t reach = 0;  // a group's maximum, not only a bound
+#pragma unroll
+        for (int g = 0; g < GROUPS / 64; ++g) reach |= __ballot(key[g] == high >> LOW) != 0;
+        if (lane == 0) room.least = high, room.exact = reach;
     }
     __syncthreads();
     uint32_t least = room.least;
+    bool known = plain && room.exact;
     float bound = key_value(least);
     if (plain && bound != kNegInf) {
         collect<T>(row, room, [&](float z) QSDP_INLINE { return z >= bound; });
@@ -363,7 +441,6 @@ __device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, f
         if (room.count <= kRoom) return room.count;
     }
     // the value bit by bit, unless the threshold is it already: fewer than `top` are above it
-    bool known = plain;
     uint32_t above;
     for (;;) {
         if (!known) {
@@ -433,48 +510,106 @@ __device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, f
     return top;
 }
 
-template <class T, int THREADS, int NV, Rest REST, bool TOP>
+// A row's results from its sums; one thread's work.
+__device__ __forceinline__ void put_score(const ScoreParams& p, uint64_t r, const Sums& a, float log_total, int64_t token,
+                                          float z_token) {
+    const bool empty = a.s == 0.0f;
+    if (p.logprob) {
+        float v = 0.0f;
+        if (token >= 0) v = empty ? kNegInf : __builtin_nanf("");
+        if ((uint64_t)token < p.in.vocab && !empty) v = (z_token - a.m) * p.in.inv_temperature - log_total;
+        p.logprob[r] = v;
+    }
+    if (p.entropy) p.entropy[r] = empty ? 0.0f : log_total - a.u / a.s * kLn2;
+    if (p.stats) {
+        p.stats[2 * r] = a.m;
+        p.stats[2 * r + 1] = log_total;
+    }
+}
+__device__ __forceinline__ void put_top(const ScoreParams& p, uint64_t r, uint32_t rank, uint64_t key, const Sums& a, float log_total) {
+    p.top_index[r * p.top + rank] = (int32_t)~(uint32_t)key;
+    p.top_logprob[r * p.top + rank] =
+        a.s == 0.0f ? kNegInf : (key_value((uint32_t)(key >> 32)) - a.m) * p.in.inv_temperature - log_total;
+}
+
+// PART: one of kParts parts of a row, to be joined.
+template <class T, int THREADS, int NV, Rest REST, bool TOP, bool PART>
 __global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void score_kernel(ScoreParams p) {
     __shared__ float waves[THREADS / 64][4];
     __shared__ u32x4 held[REST == Rest::HELD ? held_pieces(THREADS) : 1];
-    const uint64_t r = p.in.first + blockIdx.x;
-    const auto* z = static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride;
+    const uint64_t item = p.in.first + blockIdx.x, r = PART ? item / kParts : item;
+    const uint64_t lo = PART ? item % kParts * p.per : 0, left = p.in.vocab - lo;
+    const auto* z = static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride + lo;
     const float scale2 = p.in.inv_temperature * kLog2e;
-    Row<T, THREADS, NV, REST> row(z, p.in.vocab, held);
+    // the token is asked for ahead of the row, its logit right behind it
+    const int64_t token = !PART && p.logprob ? p.tokens[r] : -1;
+    Row<T, THREADS, NV, REST> row(z, PART && left > p.per ? p.per : left, held);
+    const float z_token = PART ? 0.0f : T::get(z[(uint64_t)token < p.in.vocab ? token : 0]);
     Sums a = {kNegInf, 0.0f, 0.0f};
     float most = kNegInf, none = 0.0f;
     row.each_chunk([&]() QSDP_INLINE { add_chunk<true, Second::NONE>(row, scale2, 0.0f, a, none, most, T()); });
     a = join<THREADS, true, Second::NONE>(a, scale2, 0.0f, none, waves);
-    const bool empty = a.s == 0.0f;
     const float log_total = logf(a.s);
     if (threadIdx.x == 0) {
-        if (p.logprob) {
-            const int64_t t = p.tokens[r];
-            float v = 0.0f;
-            if (t >= 0) v = empty ? kNegInf : __builtin_nanf("");
-            if (t >= 0 && (uint64_t)t < p.in.vocab && !empty) v = (T::get(z[t]) - a.m) * p.in.inv_temperature - log_total;
-            p.logprob[r] = v;
-        }
-        if (p.entropy) p.entropy[r] = empty ? 0.0f : log_total - a.u / a.s * kLn2;
-        if (p.stats) {
-            p.stats[2 * r] = a.m;
-            p.stats[2 * r + 1] = log_total;
-        }
+        if (PART) p.heads[item] = make_float4(a.m, a.s, a.u, 0.0f);
+        else put_score(p, r, a, log_total, token, z_token);
     }
     if constexpr (TOP) {
         __shared__ TopRoom<THREADS> room;
         const uint32_t top = (uint32_t)p.top;
         const uint32_t count = top_list<T>(row, top, a.s == a.s, most, room);
-        for (uint32_t i = threadIdx.x; i < count; i += THREADS) {
+        // eight lanes count for a candidate how many are before it
+        for (uint32_t i = threadIdx.x / 8; i < count; i += THREADS / 8) {
             const uint64_t key = room.list[i];
             uint32_t rank = 0;
-            for (uint32_t o = 0; o < count; ++o) rank += room.list[o] > key;
-            if (rank < top) {
-                p.top_index[r * top + rank] = (int32_t)~(uint32_t)key;
-                p.top_logprob[r * top + rank] =
-                    empty ? kNegInf : (key_value((uint32_t)(key >> 32)) - a.m) * p.in.inv_temperature - log_total;
+            for (uint32_t o = threadIdx.x % 8; o < count; o += 8) rank += room.list[o] > key;
+            rank = reduce4(rank, Add());
+            rank += dpp<0x141>(rank);
+            if (rank < top && threadIdx.x % 8 == 0) {
+                if (PART) p.keys[item * top + rank] = key - lo;  // its low word is the complement of the index
+                else put_top(p, r, rank, key, a, log_total);
             }
         }
+    }
+}
+
+// The parts of a row: their sums by one maximum; their alternatives, each list in order, by how many of the other lists are
+// before each.
+template <class T>
+__global__ __launch_bounds__(256) void score_join_kernel(ScoreParams p) {
+    __shared__ uint64_t keys[kParts * kMostTop];
+    const uint64_t r = p.in.first + blockIdx.x;
+    const uint32_t top = (uint32_t)p.top, all = top * (uint32_t)kParts;
+    const auto* z = static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride;
+    const int64_t token = p.logprob ? p.tokens[r] : -1;
+    for (uint32_t i = threadIdx.x; i < all; i += 256) keys[i] = p.keys[r * all + i];
+    const uint32_t part = threadIdx.x % 16;
+    Sums a = {kNegInf, 0.0f, 0.0f};
+    if (part < kParts) {
+        const float4 head = p.heads[r * kParts + part];
+        a = {head.x, head.y, head.z};
+    }
+    const float z_token = T::get(z[(uint64_t)token < p.in.vocab ? token : 0]);
+    const float m = reduce16(a.m, Max());
+    rescale(a, m, p.in.inv_temperature * kLog2e);
+    a = {m, reduce16(a.s, Add()), reduce16(a.u, Add())};
+    const float log_total = logf(a.s);
+    if (threadIdx.x == 0) put_score(p, r, a, log_total, token, z_token);
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < all; i += 256) {
+        const uint64_t key = keys[i];
+        uint32_t rank = i % top;
+        for (uint32_t q = 0; q < kParts; ++q) {
+            if (q == i / top) continue;
+            uint32_t from = 0, to = top;
+            while (from < to) {
+                const uint32_t mid = (from + to) / 2;
+                if (keys[q * top + mid] > key) from = mid + 1;
+                else to = mid;
+            }
+            rank += from;
+        }
+        if (rank < top) put_top(p, r, rank, key, a, log_total);
     }
 }
 
@@ -526,7 +661,7 @@ __global__ __launch_bounds__(256) void score_backward_kernel(ScoreBackwardParams
     const uint64_t r = part.row;
     u32x4 v[kSegment];
     part.load(static_cast<const typename T::raw*>(p.in.logits) + r * p.in.stride, v);
-    const float m = p.stats[2 * r], log_total = p.stats[2 * r + 1], log2_total = log_total * kLog2e;
+    const float m = same(p.stats[2 * r]), log_total = same(p.stats[2 * r + 1]), log2_total = log_total * kLog2e;
     auto* dz = static_cast<typename T::raw*>(p.d_logits) + r * p.d_stride;
     if (log_total == kNegInf) {
         part.write(v, dz, [](float, uint32_t) QSDP_INLINE { return 0.0f; }, ~0u, 0.0f);
@@ -536,10 +671,13 @@ __global__ __launch_bounds__(256) void score_backward_kernel(ScoreBackwardParams
     const uint32_t token = (uint64_t)asked < (uint64_t)n ? (uint32_t)asked : ~0u;  // ~0: none
     const float g = token != ~0u ? p.d_logprob[r] * p.in.inv_temperature : 0.0f;
     const float h = ENTROPY ? p.d_entropy[r] * p.in.inv_temperature * kLn2 : 0.0f;  // entropies in bits below
-    const float off = ENTROPY ? fmaf(h, p.entropy[r] * kLog2e, g) : g;
+    // p = f e, log2 p = a + rest - log2_total, e = 2^a
+    const Line line(m, scale2);
+    const float f = exp2f(line.rest - log2_total);
+    const float off = -f * (ENTROPY ? fmaf(h, fmaf(p.entropy[r], kLog2e, line.rest - log2_total), g) : g), times_a = -f * h;
     part.write(v, dz, [&](float z, uint32_t) QSDP_INLINE {
-        const float a = fmaf(z - m, scale2, -log2_total);
-        return -exp2_fast(a) * (ENTROPY ? fmaf(h, fmaxf(a, kLeast), off) : off);
+        const float a = line.at(z);
+        return exp2_fast(a) * (ENTROPY ? fmaf(times_a, fmaxf(a, kLeast), off) : off);
     }, token, g);
 }
 
@@ -549,11 +687,6 @@ struct List {
     float p[kMostTop], log2_p[kMostTop], z[kMostTop];
     int32_t index[kMostTop];
 };
-
-// A value that is the same for all threads, in a scalar register.
-__device__ __forceinline__ float same(float v) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
-}
 
 __device__ __forceinline__ uint32_t label_of(int64_t asked, uint32_t n) {  // ~0: none
     return __builtin_amdgcn_readfirstlane((uint64_t)asked < (uint64_t)n ? (uint32_t)asked : ~0u);
@@ -598,24 +731,25 @@ __device__ __forceinline__ bool fill_list(const DistillParams& p, const typename
 // temperature's (scale2), or their squares at temperature 2; otherwise one serves.
 template <Second MORE>
 struct Slope {
-    float m, scale2, soft_log, hard_log, soft, hard, one, square;
-    uint32_t label;  // ~0: none
-    __device__ __forceinline__ Slope(const DistillParams& p, float scale2_, float m_, float soft_log_, float hard_log_, bool taught,
+    Line line, other;  // exponents at the temperature (or the only ones), and at 1
+    float soft, hard;  // of the targets
+    float p1, p2;      // d z_v = p1 e + p2 f, f = e^2 at temperature 2: the sums and the lines' rests are in them
+    uint32_t label;    // ~0: none
+    bool none;
+    __device__ __forceinline__ Slope(const DistillParams& p, float scale2, float m, float soft_log, float hard_log, bool taught,
                                      uint32_t label_, float g)
-        : m(m_), scale2(scale2_), soft_log(soft_log_), hard_log(hard_log_), label(label_) {
+        : line(m, scale2), other(m, MORE == Second::OTHER ? kLog2e : 0.0f), label(label_) {
         soft = same(taught ? g * p.alpha * p.temperature : 0.0f);
         hard = same(label != ~0u ? g * (1.0f - p.alpha) : 0.0f);
-        one = same(soft + hard);
-        // p^2 = 2^(2 (...) - 2 soft_log): what it takes to have hard_log there
-        square = same(MORE == Second::SQUARE && hard != 0.0f ? hard * exp2f(2.0f * soft_log - hard_log) : 0.0f);
+        none = soft_log == kNegInf || (soft == 0.0f && hard == 0.0f);
+        p1 = same((MORE == Second::NONE ? soft + hard : soft) * exp2f(line.rest - soft_log));
+        p2 = MORE == Second::NONE ? 0.0f : same(hard * exp2f((MORE == Second::SQUARE ? 2.0f * line.rest : other.rest) - hard_log));
     }
-    __device__ __forceinline__ bool nothing() const { return soft_log == kNegInf || (soft == 0.0f && hard == 0.0f); }
-    __device__ __forceinline__ float operator()(float v) const {
-        const float d = v - m;
-        const float p = exp2_fast(fmaf(d, scale2, -soft_log));
-        if (MORE == Second::NONE) return one * p;
-        if (MORE == Second::SQUARE) return fmaf(square * p, p, soft * p);
-        return fmaf(hard, exp2_fast(fmaf(d, kLog2e, -hard_log)), soft * p);
+    __device__ __forceinline__ float operator()(float z) const {
+        const float e = exp2_fast(line.at(z));
+        if (MORE == Second::NONE) return p1 * e;
+        if (MORE == Second::SQUARE) return e * fmaf(p2, e, p1);
+        return fmaf(p2, exp2_fast(other.at(z)), p1 * e);
     }
     __device__ __forceinline__ float target(const List& list, int top, uint32_t j) const {
         float sum = 0.0f;
@@ -684,7 +818,7 @@ __global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void distill
     const Slope<MORE> slope(p, scale2, m, soft_log, hard_log, taught, label, same(p.row_scale ? p.row_scale[r] : 1.0f));
     row.again();
     __syncthreads();  // the list is there, and what is read outside the own pieces has been read
-    if (slope.nothing()) {
+    if (slope.none) {
         for (uint32_t j = threadIdx.x; j < n; j += THREADS) dz[j] = T::put(0.0f);
         return;
     }
@@ -710,7 +844,7 @@ __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p) 
     const float z_label = same(label != ~0u ? T::get(z[label]) : 0.0f);
     const Slope<MORE> slope(p, one_scale2<MORE>(p), same(p.stats[3 * r]), same(p.stats[3 * r + 1] * kLog2e),
                             same(p.stats[3 * r + 2] * kLog2e), taught, label, same(p.d_loss[r]));
-    const bool nothing = slope.nothing();
+    const bool nothing = slope.none;
     __syncthreads();  // the list is there
     part.write(v, dz, [&](float v, uint32_t) QSDP_INLINE { return nothing ? 0.0f : slope(v); }, ~0u, 0.0f);
     if (nothing) return;
@@ -739,7 +873,9 @@ hipError_t go(void (*kernel)(P), int threads, uint64_t work, P p, hipStream_t s)
 template <Rest REST>
 using RestOf = std::integral_constant<Rest, REST>;
 
-template <class T, class F>
+// FOUR: four workgroups of 512 threads to a compute unit, with LDS, rather than two of 1024 with registers alone: for what
+// writes as much as it reads (distillation of 8192 rows of 50257 bf16 logits 332 / 354 us; sums alone of 4096 rows 75 / 70).
+template <class T, bool FOUR, class F>
 hipError_t by_length(uint64_t n, F f) {
     const uint64_t pieces = (n + T::PER - 1 + (sizeof(typename T::raw) == 2)) / T::PER;  // with a lead
     const std::integral_constant<int, 2> two;
@@ -749,7 +885,8 @@ hipError_t by_length(uint64_t n, F f) {
     if (pieces <= 256 * 8) return f(std::integral_constant<int, 256>(), eight, RestOf<Rest::NONE>());
     const std::integral_constant<int, 512> half;
     if (pieces <= 512 * 8) return f(half, eight, RestOf<Rest::NONE>());
-    if (pieces <= 512 * 8 + held_pieces(512)) return f(half, eight, RestOf<Rest::HELD>());
+    if constexpr (FOUR)
+        if (pieces <= 512 * 8 + held_pieces(512)) return f(half, eight, RestOf<Rest::HELD>());
     if (pieces <= 1024 * 8) return f(most, eight, RestOf<Rest::NONE>());
     if (pieces <= 1024 * 8 + held_pieces(1024)) return f(most, eight, RestOf<Rest::HELD>());
     return f(most, eight, RestOf<Rest::STREAM>());
@@ -765,10 +902,24 @@ hipError_t by_format(qsdp_dtype dtype, F f) {
 hipError_t launch_score(qsdp_dtype dtype, const ScoreParams& p, hipStream_t s) {
     return by_format(dtype, [&](auto t) {
         using T = decltype(t);
-        return by_length<T>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
-            if (p.top) return go(score_kernel<T, threads, nv, rest, true>, threads, p.in.rows, p, s);
-            return go(score_kernel<T, threads, nv, rest, false>, threads, p.in.rows, p, s);
-        });
+        auto rows = [&](auto top) {
+            if (p.heads)
+                return by_length<T, false>(p.per, [&](auto threads, auto nv, auto rest) {
+                    return go(score_kernel<T, threads, nv, rest, top, true>, threads, p.in.rows * kParts, p, s);
+                });
+            // many rows with alternatives gain by four workgroups (4096 rows of 50257 bf16 logits, eight alternatives, 119 / 96 us),
+            // few lose (48 rows 10.5 / 12 us)
+            if (top && p.in.rows >= 512)
+                return by_length<T, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+                    return go(score_kernel<T, threads, nv, rest, top, false>, threads, p.in.rows, p, s);
+                });
+            return by_length<T, false>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+                return go(score_kernel<T, threads, nv, rest, top, false>, threads, p.in.rows, p, s);
+            });
+        };
+        const hipError_t e = p.top ? rows(std::true_type()) : rows(std::false_type());
+        if (e != hipSuccess || !p.heads) return e;
+        return go(score_join_kernel<T>, 256, p.in.rows, p, s);
     });
 }
 
@@ -792,7 +943,7 @@ hipError_t launch_distill(qsdp_dtype dtype, const DistillParams& p, hipStream_t 
         using T = decltype(t);
         return by_second([&](auto more) {
             if (!p.loss) return go(distill_backward_kernel<T, more>, 256, p.in.rows * Segment<T>::of(p.in.vocab), p, s);
-            return by_length<T>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+            return by_length<T, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
                 return go(distill_kernel<T, threads, nv, rest, more>, threads, p.in.rows, p, s);
             });
         });

@@ -21,7 +21,20 @@ struct ScoreParams {
     int top;
     float *logprob, *entropy, *stats, *top_logprob;
     int32_t* top_index;
+    // Rows shared among workgroups: each takes `per` elements (the last one what is left) and leaves its sums and its first
+    // alternatives, [rows, kParts] and [rows, kParts, top].
+    uint64_t per;
+    float4* heads;
+    uint64_t* keys;
 };
+
+// Few rows are cut into eight parts where they are long: the bytes of workspace that takes, 0 for other calls. From 65536
+// logits on it pays (us without / with, 20 alternatives: one row of 65536 bf16 12 / 11, of 131072 19 / 12, of 262144 float 43 /
+// 13; 64 of 65536 12.7 / 12.7, of 131072 21 / 15); below, the second launch costs more than a workgroup alone (50257: 10.2 / 10.8).
+constexpr uint64_t kParts = 8;
+inline uint64_t parts_bytes(uint64_t rows, uint64_t vocab, int top) {
+    return rows <= 64 && vocab >= 65536 ? rows * kParts * (sizeof(float4) + sizeof(uint64_t) * (uint64_t)top) : 0;
+}
 
 struct ScoreBackwardParams {
     Rows in;

@@ -282,3 +282,30 @@ def test_refusals_of_the_binding():
         qb.qsdp_token_logprobs_backward(z, t, 1.0, torch.zeros((3, 2), device=lu.DEV), None, out, None, z.half())
     with pytest.raises(qb.QsdpError):  # nothing to differentiate
         qb.qsdp_token_logprobs_backward(z, t, 1.0, torch.zeros((3, 2), device=lu.DEV), None, None, None, z)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [65536, 70001, 150003])
+def test_rows_cut_into_parts(vocab, dtype):
+    """Long rows shared among workgroups, parts without anything, equal values across parts: the results of whole rows."""
+    dt = lu.DTYPES[dtype]
+    assert qb.token_logprobs_bytes(9, vocab, 100) > 0
+    z = lu.make_rows(9, vocab, dt, 3, seed=vocab, offset=1)
+    z[1] = -math.inf
+    z[2] = -math.inf
+    z[2, vocab - 2] = 1.0                       # all but the last part empty
+    z[3] = 0.25                                 # equal throughout
+    z[4, ::1000] = 20.0                         # equal ones in every part
+    z[5] = torch.finfo(dt).min
+    z[6, 5000:60000] = torch.finfo(dt).min
+    z[7, :vocab // 2] = -math.inf
+    tokens = torch.tensor([vocab - 1, 4, vocab - 2, 7, 1000, 9, -5, vocab - 9, vocab // 2])
+    check(z, tokens, 1.0, 100, True)
+    check(z, tokens, 0.7, 1, True)
+    zg = lu.to_gpu(z)
+    zg[8, 66] = math.nan
+    out = run_score(zg, tokens.to(lu.DEV), 1.0, 20, full_workspace(zg, 20))
+    whole = run_score(zg, tokens.to(lu.DEV), 1.0, 20)
+    assert torch.equal(out[4], whole[4]) and out[0][8].isnan() and out[1][8].isnan() and out[3][8].isnan().all()
+    short = torch.empty(qb.token_logprobs_bytes(9, vocab, 20) - 1, dtype=torch.uint8, device=lu.DEV)
+    assert all(torch.equal(a.nan_to_num(9), b.nan_to_num(9)) for a, b in zip(run_score(zg, tokens.to(lu.DEV), 1.0, 20, short), whole))
