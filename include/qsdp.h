@@ -617,9 +617,10 @@ int qsdp_recv_adamw_step_segmented(float* x, float* m, float* v, const qsdp_segm
  * A masked entry is -inf (or the format's lowest value) and has probability 0. A row of nothing
  * but -inf: logprob -inf, entropy 0, stats {-inf, -inf}, gradient 0. A row with a NaN or +inf:
  * NaN in every result but the order of its alternatives.
- *   workspace    16-byte aligned; of qsdp_token_logprobs_bytes bytes it lets a call of few rows
- *                share each row among workgroups. Less or none is allowed and slower. Its contents
- *                need no preparation and are not kept.
+ *   workspace    16-byte aligned; of qsdp_token_logprobs_bytes bytes it lets a call of few long
+ *                rows share each row among workgroups (0 bytes: the call has no use for one).
+ *                Less or none is allowed and slower. Its contents need no preparation and are not
+ *                kept.
  */
 size_t qsdp_token_logprobs_bytes(uint64_t rows, uint64_t vocab, int top);
 int qsdp_token_logprobs(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab,
@@ -654,8 +655,8 @@ int qsdp_token_logprobs_backward(const void* logits, qsdp_dtype dtype, uint64_t 
  * a label >= vocab gives a NaN loss. With d_logits the gradient comes out of the same pass over
  * the logits (row_scale: the gradient of the total by loss[r], 1 where NULL); without it, or where
  * that gradient is not known yet, `stats` ([rows, 3], nullable: maximum, logs of the sums at the
- * temperature and at 1) goes to qsdp_distill_loss_backward with it as d_loss. d_logits may
- * overwrite the logits. labels may be NULL for alpha = 1, the list for alpha = 0 (top = 0).
+ * temperature and at 1, of which alpha = 1 or 0 leaves one without a meaning) goes to
+ * qsdp_distill_loss_backward with it as d_loss and the same alpha. d_logits may overwrite the logits. labels may be NULL for alpha = 1, the list for alpha = 0 (top = 0).
  * A row of nothing but -inf: loss +inf if anything is asked of it, gradient 0. top <= 128.
  */
 int qsdp_distill_loss(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab,

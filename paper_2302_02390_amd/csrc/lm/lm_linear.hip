@@ -20,7 +20,8 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 // ---- tokens --------------------------------------------------------------------------------------------------------------
 // s = max |x| times the rounded 1/127, q = rint(x / s) with an IEEE division in binary32; slots past k are zero. A workgroup
 // per token, which keeps the token in registers between its maximum and its codes: eight elements to a thread at a time, of
-// which the NV-th part is the last that is held; a longer token is read twice.
+// which the NV-th part is the last that is held; a longer token is read twice. HBM bounds it for many tokens: 8192 of 8192 bf16
+// elements 45 us, 4.5 TB/s both ways.
 template <class T>
 struct Eight {
     float v[8];
@@ -137,7 +138,8 @@ __device__ __forceinline__ void put4(typename O::raw* y, const float* v, int cou
 // STAGES steps deep: while one is multiplied the next ones are on their way, and one barrier a step separates them. LDS holds rows of
 // 128 bytes whose eight pieces of 16 are permuted by the row (piece c of row r in place c ^ (r % 8)), so that sixteen rows
 // read the same piece from all banks; the permutation is in the addresses that the lanes read from memory. A wave multiplies
-// WN channels (first operand, so that four consecutive channels of a token end up in a lane) by WM tokens.
+// WN channels (first operand, so that four consecutive channels of a token end up in a lane) by WM tokens. The matrix units bound
+// large products: 8192^3 495 us, 2223 TOP/s (the library's int8 product 2202), 8192 x 2048 x 8192 114-127 us.
 constexpr int kStep = 128;
 
 typedef __attribute__((address_space(1))) const void* global_ptr;
@@ -391,7 +393,8 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Ma
 // The weights are read once and bound the time. A workgroup takes 16 channels and all tokens (16 * MT); its waves share the
 // codes of a channel: by buckets, or a bucket's codes among several waves, so that enough loads are on their way. Each wave
 // moves its codes through LDS of its own, as the tiles do, and waits for nobody. Whole numbers meet in LDS before they are
-// scaled; waves that take whole buckets scale their own, and their sums meet in the order of the waves.
+// scaled; waves that take whole buckets scale their own, and their sums meet in the order of the waves. One token times 8192 x 2048
+// 6.3 us (2.7 TB/s: the latency of the loads).
 template <int MT, int WAVES, int STAGES, class O>
 __global__ __launch_bounds__(WAVES * 64) void few_kernel(MatmulParams p) {
     constexpr int ROWS = 16 + 16 * MT, LOADS = 2 + 2 * MT;
