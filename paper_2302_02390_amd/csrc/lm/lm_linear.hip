@@ -198,15 +198,19 @@ __device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_
     m = band * kBand + in % high;
 }
 
-template <int TN, int TM, int WN, int WM, int STAGES, bool BUCKETS, class O>
-__global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(MatmulParams p, uint32_t n_tiles,
+// GROUPS of such teams share a tile where there are fewer tiles than compute units: each takes a run of the steps, and their sums
+// meet in LDS in the order of the groups. All make the same number of steps; those past a group's run multiply by zero.
+template <int TN, int TM, int WN, int WM, int STAGES, bool BUCKETS, int GROUPS, class O>
+__global__ __launch_bounds__((TN / WN) * (TM / WM) * GROUPS * 64, 2) void tiles_kernel(MatmulParams p, uint32_t n_tiles,
                                                                                  uint32_t m_tiles) {
     typedef Tile<TN, TM, WN, WM> S;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES][S::BYTES];
+    __shared__ __attribute__((aligned(1024))) uint8_t all[GROUPS][STAGES][S::BYTES];
     constexpr int A = WN / 16, B = WM / 16;
     uint32_t n_tile, m_tile;
     place(blockIdx.x, n_tiles, m_tiles, n_tile, m_tile);
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const int lane = threadIdx.x % 64, team = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 64);
+    const int wave = GROUPS == 1 ? team : team % S::WAVES, group = GROUPS == 1 ? 0 : team / S::WAVES;
+    uint8_t(*lds)[S::BYTES] = all[group];
     const uint64_t n0 = (uint64_t)n_tile * TN, m0 = (uint64_t)m_tile * TM;
     // what the lane loads: a piece of 16 bytes of a row of eight; rows past the matrix are its last one
     const uint32_t piece = (uint32_t)((lane % 8) ^ (lane / 8)) * 16;
@@ -225,7 +229,10 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Ma
     }
     const uint8_t* w = p.w + n0 * p.w_pitch;
     const int8_t* x = p.x + m0 * p.x_pitch;
-    auto fetch = [&](uint8_t* to, uint32_t k0) __attribute__((always_inline)) {
+    const uint32_t total = (uint32_t)((p.k + kStep - 1) / kStep), steps = (total + GROUPS - 1) / GROUPS;
+    const uint32_t begin = group * steps, mine = begin >= total ? 0 : total - begin < steps ? total - begin : steps;
+    auto fetch = [&](uint8_t* to, uint32_t at) __attribute__((always_inline)) {
+        const uint32_t k0 = (GROUPS == 1 || begin + at < total ? begin + at : total - 1) * kStep;
         const uint8_t* wk = w + k0;
         const int8_t* xk = x + k0;
         // a channel's codes end at a multiple of 32: pieces past that are read from its start, the tokens' codes there are zero
@@ -255,7 +262,12 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Ma
 #pragma unroll
         for (int b = 0; b < B; ++b) xv[set][b] = *reinterpret_cast<const v4i*>(from + (TN + wm + b * 16) * kStep + at);
     };
-    auto multiply = [&](auto set) __attribute__((always_inline)) {
+    auto multiply = [&](auto set, uint32_t s) __attribute__((always_inline)) {
+        if constexpr (GROUPS > 1) {
+            const int keep = s < mine ? -1 : 0;
+#pragma unroll
+            for (int b = 0; b < B; ++b) xv[set][b] &= keep;
+        }
 #pragma unroll
         for (int a = 0; a < A; ++a) {
             const v4i signed_w = wv[set][a] ^ (int)0x80808080;
@@ -268,7 +280,6 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Ma
     // d[a][b][c]: channel wn + a * 16 + part * 4 + c of token wm + b * 16 + r
     const int64_t left = (int64_t)(p.n - n0) - wn - part * 4;  // channels from the lane's first one on
     const float* meta = p.meta + 2 * p.buckets * (n0 + wn + part * 4);
-    const uint32_t steps = (uint32_t)((p.k + kStep - 1) / kStep);
     // of channels in several buckets: the sum over the buckets so far, added to at the end of each
     float sum_of[BUCKETS ? A : 1][BUCKETS ? B : 1][4];
     if constexpr (BUCKETS) {
@@ -279,23 +290,25 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Ma
 #pragma unroll
                 for (int c = 0; c < 4; ++c) sum_of[a][b][c] = 0.0f;
     }
-    uint32_t bucket = 0, next = p.bucket / kStep;
+    const uint32_t per = p.bucket / kStep;  // where there are several buckets
+    uint32_t bucket = BUCKETS ? begin / per : 0, next = (bucket + 1) * per;
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s)
-        if ((uint32_t)s < steps) fetch(lds[s], s * kStep);
+        if ((uint32_t)s < steps) fetch(lds[s], s);
     // Step `at` is there for all waves: its loads are done (those behind it may be on their way), and so is the reading of the
     // step before, whose place the step STAGES - 1 further takes. While a half is multiplied the next one comes out of LDS,
     // over the barrier as well: reading and multiplying would otherwise take turns, as the barrier has all waves do the same.
     constexpr int LOADS = S::W_LOADS + S::X_LOADS;
-    // the buckets that end with step s
+    // the bucket that ends with step s, or the part of it that ends with the group's run; the last step adds the tokens' sum
     auto fold = [&](uint32_t s) __attribute__((always_inline)) {
         if constexpr (BUCKETS) {
-            if (s + 1 != next && s + 1 != steps) return;
+            const bool ends = begin + s + 1 == next || begin + s + 1 == total;
+            if (GROUPS == 1 ? !ends : s >= mine || (!ends && s + 1 != mine)) return;
             float sums[B];
 #pragma unroll
             for (int b = 0; b < B; ++b) {
                 const uint64_t m = m0 + wm + b * 16 + r;
-                sums[b] = p.x_sums[(m < p.m ? m : p.m - 1) * p.buckets + bucket];
+                sums[b] = ends ? p.x_sums[(m < p.m ? m : p.m - 1) * p.buckets + bucket] : 0.0f;
             }
 #pragma unroll
             for (int a = 0; a < A; ++a)
@@ -312,19 +325,19 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Ma
                     }
                 }
             ++bucket;
-            next += p.bucket / kStep;
+            next += per;
         }
     };
     auto first_half = [&](uint32_t s) __attribute__((always_inline)) {
         wait_reads();  // ahead of the next ones: more than fifteen cannot be counted
         read(other, lds[s % STAGES]);
-        multiply(one);
+        multiply(one, s);
         interleave<A + B, A * B, 0>();
         wait_reads();  // the step is in registers
     };
     wait_loads<0>();
     meet_here();
-    if (STAGES - 1 < steps) fetch(lds[STAGES - 1], (STAGES - 1) * kStep);
+    if (STAGES - 1 < steps) fetch(lds[STAGES - 1], STAGES - 1);
     wait_reads();
     read(one, lds[0]);
     uint32_t s = 0;
@@ -332,9 +345,9 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Ma
         first_half(s);
         wait_loads<(STAGES - 2) * LOADS>();
         meet_here();
-        fetch(lds[s % STAGES], (s + STAGES) * kStep);
+        fetch(lds[s % STAGES], s + STAGES);
         read(one, lds[(s + 1) % STAGES]);
-        multiply(other);
+        multiply(other, s);
         interleave<A + B, A * B, LOADS>();
         fold(s);
     }
@@ -343,13 +356,47 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Ma
         wait_loads<0>();
         meet_here();
         read(one, lds[(s + 1) % STAGES]);
-        multiply(other);
+        multiply(other, s);
         interleave<A + B, A * B, 0>();
         fold(s);
     }
     first_half(s);
-    multiply(other);
+    multiply(other, s);
     fold(s);
+    if constexpr (GROUPS > 1) {
+        static_assert((GROUPS - 1) * TN * TM * 4 <= GROUPS * STAGES * S::BYTES, "the sums of the other groups");
+        v4i* meet = reinterpret_cast<v4i*>(&all[0][0][0]);
+        auto place_of = [&](int g, int a, int b) { return ((g - 1) * A * B + a * B + b) * S::THREADS + wave * 64 + lane; };
+        __syncthreads();
+        if (group) {
+#pragma unroll
+            for (int a = 0; a < A; ++a)
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    if constexpr (BUCKETS)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) d[a][b][c] = __float_as_int(sum_of[a][b][c]);
+                    meet[place_of(group, a, b)] = d[a][b];
+                }
+        }
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int g = 1; g < GROUPS; ++g)
+#pragma unroll
+            for (int a = 0; a < A; ++a)
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    const v4i more = meet[place_of(g, a, b)];
+                    if constexpr (BUCKETS)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const int word = more[c];
+                            sum_of[a][b][c] += __int_as_float(word);
+                        }
+                    else d[a][b] += more;
+                }
+    }
     // every scale is read before the first output is written: the compiler cannot know them apart
     const float* bias = p.bias ? p.bias + n0 + wn + part * 4 : nullptr;
     float scale[B], sums[B];
@@ -550,7 +597,7 @@ hipError_t launch_tokens(qsdp_dtype dtype, const TokenParams& p, hipStream_t s) 
     return dtype == QSDP_F32 ? launch_tokens_of<F32>(p, s) : dtype == QSDP_BF16 ? launch_tokens_of<BF16>(p, s) : launch_tokens_of<F16>(p, s);
 }
 
-template <int TN, int TM, int WN, int WM, int STAGES, bool BUCKETS, class O>
+template <int TN, int TM, int WN, int WM, int STAGES, bool BUCKETS, int GROUPS, class O>
 static hipError_t launch_tiles(const MatmulParams& p, hipStream_t s) {
     const uint32_t n_tiles = (uint32_t)((p.n + TN - 1) / TN), m_tiles = (uint32_t)((p.m + TM - 1) / TM);
     // in several launches where the tiles are more than a grid holds
@@ -564,8 +611,8 @@ static hipError_t launch_tiles(const MatmulParams& p, hipStream_t s) {
         q.x_sums += first * p.buckets;
         q.m = p.m - first < (uint64_t)now * TM ? p.m - first : (uint64_t)now * TM;
         q.y = static_cast<typename O::raw*>(p.y) + first * p.y_stride;
-        hipLaunchKernelGGL((tiles_kernel<TN, TM, WN, WM, STAGES, BUCKETS, O>), dim3(n_tiles * now),
-                           dim3(Tile<TN, TM, WN, WM>::THREADS), 0, s, q, n_tiles, now);
+        hipLaunchKernelGGL((tiles_kernel<TN, TM, WN, WM, STAGES, BUCKETS, GROUPS, O>), dim3(n_tiles * now),
+                           dim3(Tile<TN, TM, WN, WM>::THREADS * GROUPS), 0, s, q, n_tiles, now);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -597,8 +644,12 @@ constexpr Cost kCost256 = {256, 256, 1.43, 1.95, 11.0}, kCost128 = {128, 128, 0.
 template <bool BUCKETS, class O>
 static hipError_t launch_small_tiles(const MatmulParams& p, hipStream_t s) {
     // deeper where no more than two share a compute unit (512 x 2048 x 8192 32 / 22 us), else room for five (2048^3 22 / 19 us)
-    if ((p.n + 63) / 64 * ((p.m + 63) / 64) <= 512) return launch_tiles<64, 64, 32, 32, 4, BUCKETS, O>(p, s);
-    return launch_tiles<64, 64, 32, 32, 2, BUCKETS, O>(p, s);
+    const uint64_t tiles = (p.n + 63) / 64 * ((p.m + 63) / 64);
+    // No more tiles than compute units: four teams to a tile where the steps are long enough to share (125 x 2048 x 8192 19 / 16 us,
+    // in eight buckets 30 / 20; 512 x 2048 x 8192 22 / 21, in eight buckets 33 / 25; 125 x 2048 x 2048 8.1 / 7.6, x 1024 6.1 / 6.4).
+    if (tiles <= 256 && p.k >= 2048) return launch_tiles<64, 64, 32, 32, 2, BUCKETS, 4, O>(p, s);
+    if (tiles <= 512) return launch_tiles<64, 64, 32, 32, 4, BUCKETS, 1, O>(p, s);
+    return launch_tiles<64, 64, 32, 32, 2, BUCKETS, 1, O>(p, s);
 }
 
 template <class O>
@@ -610,10 +661,10 @@ static hipError_t launch_matmul_to(const MatmulParams& p, hipStream_t s) {
     if (p.m <= 32 && groups <= 1024) return groups <= 256 ? launch_few<2, 8, 2, O>(p, s) : launch_few<2, 4, 2, O>(p, s);
     const double small = cost_of(p, kCost64), middle = cost_of(p, kCost128), large = cost_of(p, kCost256);
     if (p.buckets > 1)  // the largest tile has no registers for sums over buckets
-        return small < middle ? launch_small_tiles<true, O>(p, s) : launch_tiles<128, 128, 64, 64, 2, true, O>(p, s);
+        return small < middle ? launch_small_tiles<true, O>(p, s) : launch_tiles<128, 128, 64, 64, 2, true, 1, O>(p, s);
     if (small < middle && small < large) return launch_small_tiles<false, O>(p, s);
-    if (middle < large) return launch_tiles<128, 128, 64, 64, 2, false, O>(p, s);
-    return launch_tiles<256, 256, 64, 128, 2, false, O>(p, s);
+    if (middle < large) return launch_tiles<128, 128, 64, 64, 2, false, 1, O>(p, s);
+    return launch_tiles<256, 256, 64, 128, 2, false, 1, O>(p, s);
 }
 
 hipError_t launch_matmul(qsdp_dtype out, const MatmulParams& p, hipStream_t s) {

@@ -92,6 +92,14 @@ def test_buckets(m, n, k, bucket):
     check(m, n, k, bucket, "bf16", "f32", bias=n % 2 == 0, seed=k + m)
 
 
+@pytest.mark.parametrize("m", [33, 100, 200])
+@pytest.mark.parametrize("n,k,bucket", [(130, 2047, 2048), (130, 2049, 2080), (63, 2176, 128), (100, 2177, 128), (66, 3200, 640),
+                                        (66, 5000, 1024), (5, 5000, 8192), (2000, 2500, 2560)])
+def test_teams_that_share_a_tile(m, n, k, bucket):
+    """Few tiles and long sums: teams take runs of steps that are not equally long and end inside a bucket."""
+    check(m, n, k, bucket, "bf16", "f32", bias=n % 2 == 0, seed=k + m)
+
+
 @pytest.mark.parametrize("m", [2, 40, 200])
 def test_rows_of_zeros_nan_and_infinity(m):
     x = make_x(m, 500, torch.float32, 3)
