@@ -646,7 +646,8 @@ static hipError_t launch_small_tiles(const MatmulParams& p, hipStream_t s) {
     // deeper where no more than two share a compute unit (512 x 2048 x 8192 32 / 22 us), else room for five (2048^3 22 / 19 us)
     const uint64_t tiles = (p.n + 63) / 64 * ((p.m + 63) / 64);
     // No more tiles than compute units: four teams to a tile where the steps are long enough to share (125 x 2048 x 8192 19 / 16 us,
-    // in eight buckets 30 / 20; 512 x 2048 x 8192 22 / 21, in eight buckets 33 / 25; 125 x 2048 x 2048 8.1 / 7.6, x 1024 6.1 / 6.4).
+    // in eight buckets 30 / 20; 512 x 2048 x 8192 22 / 21, in eight buckets 33 / 25; 125 x 2048 x 2048 8.1 / 7.6, x 1024 6.1 / 6.4;
+    // operands in the caches).
     if (tiles <= 256 && p.k >= 2048) return launch_tiles<64, 64, 32, 32, 2, BUCKETS, 4, O>(p, s);
     if (tiles <= 512) return launch_tiles<64, 64, 32, 32, 4, BUCKETS, 1, O>(p, s);
     return launch_tiles<64, 64, 32, 32, 2, BUCKETS, 1, O>(p, s);
