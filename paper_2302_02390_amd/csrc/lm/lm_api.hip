@@ -1,5 +1,6 @@
 // C entry points of the operators on logits and on packed weights: arguments are looked at, nothing else.
 #include <cmath>
+#include <type_traits>
 
 #include "lm_linear.hpp"
 #include "lm_rows.hpp"
@@ -13,6 +14,12 @@ constexpr int kMostTop = 128;
 bool aligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 bool known(qsdp_dtype t) { return t == QSDP_F32 || t == QSDP_BF16 || t == QSDP_F16; }
 size_t width(qsdp_dtype t) { return t == QSDP_F32 ? 4 : 2; }
+
+// f with a null pointer to the format's type.
+template <class F>
+hipError_t by_format(qsdp_dtype t, F f) {
+    return t == QSDP_F32 ? f((F32*)nullptr) : t == QSDP_BF16 ? f((BF16*)nullptr) : f((F16*)nullptr);
+}
 
 int status_of(hipError_t e) { return e == hipSuccess ? QSDP_OK : QSDP_ELAUNCH; }
 
@@ -71,7 +78,9 @@ int qsdp_token_logprobs(const void* logits, qsdp_dtype dtype, uint64_t rows, uin
         p.heads = static_cast<float4*>(workspace);
         p.keys = reinterpret_cast<uint64_t*>(p.heads + rows * kParts);
     }
-    return status_of(launch_score(dtype, p, static_cast<hipStream_t>(stream)));
+    return status_of(by_format(dtype, [&](auto* t) {
+        return launch_score<std::remove_pointer_t<decltype(t)>>(p, static_cast<hipStream_t>(stream));
+    }));
 }
 
 int qsdp_token_logprobs_backward(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab, uint64_t row_stride,
@@ -87,7 +96,9 @@ int qsdp_token_logprobs_backward(const void* logits, qsdp_dtype dtype, uint64_t 
         return QSDP_EALIGN;
     const ScoreBackwardParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, tokens, stats, entropy,
                                    d_logprob, d_entropy, d_logits, d_row_stride};
-    return status_of(launch_score_backward(dtype, p, static_cast<hipStream_t>(stream)));
+    return status_of(by_format(dtype, [&](auto* t) {
+        return launch_score_backward<std::remove_pointer_t<decltype(t)>>(p, static_cast<hipStream_t>(stream));
+    }));
 }
 
 int qsdp_distill_loss(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab, uint64_t row_stride,
@@ -103,7 +114,9 @@ int qsdp_distill_loss(const void* logits, qsdp_dtype dtype, uint64_t rows, uint6
         return QSDP_EALIGN;
     const DistillParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, teacher_index, teacher_logit, top,
                              labels, temperature, alpha, row_scale, nullptr, loss, stats, d_logits, d_row_stride};
-    return status_of(launch_distill(dtype, p, static_cast<hipStream_t>(stream)));
+    return status_of(by_format(dtype, [&](auto* t) {
+        return launch_distill<std::remove_pointer_t<decltype(t)>>(p, static_cast<hipStream_t>(stream));
+    }));
 }
 
 int qsdp_distill_loss_backward(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab, uint64_t row_stride,
@@ -120,7 +133,9 @@ int qsdp_distill_loss_backward(const void* logits, qsdp_dtype dtype, uint64_t ro
     const DistillParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, teacher_index, teacher_logit, top,
                              labels, temperature, alpha, nullptr, d_loss, nullptr, const_cast<float*>(stats), d_logits,
                              d_row_stride};
-    return status_of(launch_distill(dtype, p, static_cast<hipStream_t>(stream)));
+    return status_of(by_format(dtype, [&](auto* t) {
+        return launch_distill<std::remove_pointer_t<decltype(t)>>(p, static_cast<hipStream_t>(stream));
+    }));
 }
 
 int qsdp_quantize_tokens(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k, uint64_t row_stride, int bucket,

@@ -900,62 +900,54 @@ hipError_t by_length(uint64_t n, F f) {
     return f(most, eight, RestOf<Rest::STREAM>());
 }
 
-template <class F>
-hipError_t by_format(qsdp_dtype dtype, F f) {
-    return dtype == QSDP_F32 ? f(F32()) : dtype == QSDP_BF16 ? f(BF16()) : f(F16());
-}
-
 }  // namespace
 
-hipError_t launch_score(qsdp_dtype dtype, const ScoreParams& p, hipStream_t s) {
-    return by_format(dtype, [&](auto t) {
-        using T = decltype(t);
-        auto rows = [&](auto top) {
-            if (p.heads)
-                return by_length<T, false>(p.per, [&](auto threads, auto nv, auto rest) {
-                    return go(score_kernel<T, threads, nv, rest, top, true>, threads, p.in.rows * kParts, p, s);
-                });
-            // many rows with alternatives gain by four workgroups (4096 rows of 50257 bf16 logits, eight alternatives, 119 / 96 us),
-            // few lose (48 rows 10.5 / 12 us)
-            if (top && p.in.rows >= 512)
-                return by_length<T, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
-                    return go(score_kernel<T, threads, nv, rest, top, false>, threads, p.in.rows, p, s);
-                });
-            return by_length<T, false>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+template <class T>
+hipError_t launch_score(const ScoreParams& p, hipStream_t s) {
+    auto rows = [&](auto top) {
+        if (p.heads)
+            return by_length<T, false>(p.per, [&](auto threads, auto nv, auto rest) {
+                return go(score_kernel<T, threads, nv, rest, top, true>, threads, p.in.rows * kParts, p, s);
+            });
+        // many rows with alternatives gain by four workgroups (4096 rows of 50257 bf16 logits, eight alternatives, 119 / 96 us),
+        // few lose (48 rows 10.5 / 12 us)
+        if (top && p.in.rows >= 512)
+            return by_length<T, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
                 return go(score_kernel<T, threads, nv, rest, top, false>, threads, p.in.rows, p, s);
             });
-        };
-        const hipError_t e = p.top ? rows(std::true_type()) : rows(std::false_type());
-        if (e != hipSuccess || !p.heads) return e;
-        return go(score_join_kernel<T>, 256, p.in.rows, p, s);
-    });
-}
-
-hipError_t launch_score_backward(qsdp_dtype dtype, const ScoreBackwardParams& p, hipStream_t s) {
-    return by_format(dtype, [&](auto t) {
-        using T = decltype(t);
-        const uint64_t work = p.in.rows * Segment<T>::of(p.in.vocab);
-        return p.d_entropy ? go(score_backward_kernel<T, true>, 256, work, p, s)
-                           : go(score_backward_kernel<T, false>, 256, work, p, s);
-    });
-}
-
-hipError_t launch_distill(qsdp_dtype dtype, const DistillParams& p, hipStream_t s) {
-    const bool both = p.alpha > 0.0f && p.alpha < 1.0f && p.temperature != 1.0f;
-    auto by_second = [&](auto f) {
-        if (!both) return f(std::integral_constant<Second, Second::NONE>());
-        if (p.temperature == 2.0f) return f(std::integral_constant<Second, Second::SQUARE>());
-        return f(std::integral_constant<Second, Second::OTHER>());
-    };
-    return by_format(dtype, [&](auto t) {
-        using T = decltype(t);
-        return by_second([&](auto more) {
-            if (!p.loss) return go(distill_backward_kernel<T, more>, 256, p.in.rows * Segment<T>::of(p.in.vocab), p, s);
-            return by_length<T, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
-                return go(distill_kernel<T, threads, nv, rest, more>, threads, p.in.rows, p, s);
-            });
+        return by_length<T, false>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+            return go(score_kernel<T, threads, nv, rest, top, false>, threads, p.in.rows, p, s);
         });
-    });
+    };
+    const hipError_t e = p.top ? rows(std::true_type()) : rows(std::false_type());
+    if (e != hipSuccess || !p.heads) return e;
+    return go(score_join_kernel<T>, 256, p.in.rows, p, s);
 }
+
+template <class T>
+hipError_t launch_score_backward(const ScoreBackwardParams& p, hipStream_t s) {
+    const uint64_t work = p.in.rows * Segment<T>::of(p.in.vocab);
+    return p.d_entropy ? go(score_backward_kernel<T, true>, 256, work, p, s)
+                       : go(score_backward_kernel<T, false>, 256, work, p, s);
+}
+
+template <class T>
+hipError_t launch_distill(const DistillParams& p, hipStream_t s) {
+    const bool both = p.alpha > 0.0f && p.alpha < 1.0f && p.temperature != 1.0f;
+    auto launch = [&](auto more) {
+        if (!p.loss) return go(distill_backward_kernel<T, more>, 256, p.in.rows * Segment<T>::of(p.in.vocab), p, s);
+        return by_length<T, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+            return go(distill_kernel<T, threads, nv, rest, more>, threads, p.in.rows, p, s);
+        });
+    };
+    if (!both) return launch(std::integral_constant<Second, Second::NONE>());
+    if (p.temperature == 2.0f) return launch(std::integral_constant<Second, Second::SQUARE>());
+    return launch(std::integral_constant<Second, Second::OTHER>());
+}
+
+// an object for each format
+template hipError_t launch_score<QSDP_LM_FORMAT>(const ScoreParams&, hipStream_t);
+template hipError_t launch_score_backward<QSDP_LM_FORMAT>(const ScoreBackwardParams&, hipStream_t);
+template hipError_t launch_distill<QSDP_LM_FORMAT>(const DistillParams&, hipStream_t);
 
 }  // namespace qsdp_lm

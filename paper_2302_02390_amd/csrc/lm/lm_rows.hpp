@@ -57,8 +57,15 @@ struct DistillParams {
     uint64_t d_stride;
 };
 
-hipError_t launch_score(qsdp_dtype dtype, const ScoreParams& p, hipStream_t s);
-hipError_t launch_score_backward(qsdp_dtype dtype, const ScoreBackwardParams& p, hipStream_t s);
-hipError_t launch_distill(qsdp_dtype dtype, const DistillParams& p, hipStream_t s);
+// T: a format of lm_common.hpp.
+struct F32;
+struct BF16;
+struct F16;
+template <class T>
+hipError_t launch_score(const ScoreParams& p, hipStream_t s);
+template <class T>
+hipError_t launch_score_backward(const ScoreBackwardParams& p, hipStream_t s);
+template <class T>
+hipError_t launch_distill(const DistillParams& p, hipStream_t s);
 
 }  // namespace qsdp_lm

@@ -1,0 +1,33 @@
+"""Rows of logits with what is no number, no token or no teacher in them, and masks of the format's lowest value."""
+import math
+
+import pytest
+import torch
+
+import lm_util as lu
+from paper_2302_02390_amd import binding as qb
+from test_gpu_distill import lists
+from test_gpu_scoring import full_workspace, run_score
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [5, 3001, 50257, 70001, 131073])
+def test_statistics_of_rows_with_a_nan_or_infinity(vocab, dtype):
+    """Neither the maximum nor the sum of such a row is a number, whole or in parts."""
+    z = lu.make_rows(4, vocab, lu.DTYPES[dtype], 1, seed=vocab)
+    z[0, vocab // 2] = math.nan
+    z[1, vocab - 1] = math.inf
+    z[2] = math.nan
+    zg = lu.to_gpu(z)
+    tokens = torch.tensor([0, vocab - 1, -1, 2], device=lu.DEV)
+    for workspace in (None, full_workspace(zg, 3)):
+        logprob, entropy, stats, _, _ = run_score(zg, tokens, 1.0, 3, workspace)
+        assert stats.isnan().tolist() == [[True, True]] * 3 + [[False, False]]
+        # a row without a token has no log probability to be wrong
+        assert logprob[:2].isnan().all() and float(logprob[2]) == 0.0 and entropy[:3].isnan().all()
+        d = torch.empty_like(zg)
+        one = torch.ones(4, device=lu.DEV)
+        qb.qsdp_token_logprobs_backward(zg, tokens, 1.0, stats, entropy, one, one, d)
+        assert d[:3].isnan().all() and d[3].isfinite().all()
