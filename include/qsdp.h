@@ -616,7 +616,7 @@ int qsdp_recv_adamw_step_segmented(float* x, float* m, float* v, const qsdp_segm
  * logprob, entropy and stats are each left out where NULL; tokens may be NULL where logprob is.
  * A masked entry is -inf (or the format's lowest value) and has probability 0. A row of nothing
  * but -inf: logprob -inf, entropy 0, stats {-inf, -inf}, gradient 0. A row with a NaN or +inf:
- * NaN in every result but the order of its alternatives.
+ * NaN in every result but the order of its alternatives, and the 0 of a row without a token.
  *   workspace    16-byte aligned; of qsdp_token_logprobs_bytes bytes it lets a call of few long
  *                rows share each row among workgroups (0 bytes: the call has no use for one).
  *                Less or none is allowed and slower. Its contents need no preparation and are not

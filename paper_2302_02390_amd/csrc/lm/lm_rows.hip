@@ -522,7 +522,7 @@ __device__ __forceinline__ void put_score(const ScoreParams& p, uint64_t r, cons
     }
     if (p.entropy) p.entropy[r] = empty ? 0.0f : log_total - a.u / a.s * kLn2;
     if (p.stats) {
-        p.stats[2 * r] = a.m;
+        p.stats[2 * r] = a.s == a.s ? a.m : a.s;  // of a NaN or +inf: no maximum either
         p.stats[2 * r + 1] = log_total;
     }
 }
