@@ -607,7 +607,8 @@ int qsdp_recv_adamw_step_segmented(float* x, float* m, float* v, const qsdp_segm
  *
  * Log probabilities of given tokens, entropy and top alternatives of every row z of logits. With
  * m = max z, t = (z - m) / temperature, S = sum exp(t):
- *   logprob[r]   t[tokens[r]] - log S; 0 where tokens[r] < 0 (no token), NaN where it is >= vocab
+ *   logprob[r]   t[tokens[r]] - log S; 0 where tokens[r] < 0 (no token), NaN where it is >= vocab,
+ *                whatever the row holds
  *   entropy[r]   log S - (sum t exp(t)) / S
  *   stats[2r..]  {m, log S}, what the gradient needs; m / temperature + log S is the row's
  *                log-sum-exp

@@ -516,8 +516,8 @@ __device__ __forceinline__ void put_score(const ScoreParams& p, uint64_t r, cons
     const bool empty = a.s == 0.0f;
     if (p.logprob) {
         float v = 0.0f;
-        if (token >= 0) v = empty ? kNegInf : __builtin_nanf("");
-        if ((uint64_t)token < p.in.vocab && !empty) v = (z_token - a.m) * p.in.inv_temperature - log_total;
+        if (token >= 0) v = __builtin_nanf("");
+        if ((uint64_t)token < p.in.vocab) v = empty ? kNegInf : (z_token - a.m) * p.in.inv_temperature - log_total;
         p.logprob[r] = v;
     }
     if (p.entropy) p.entropy[r] = empty ? 0.0f : log_total - a.u / a.s * kLn2;

@@ -31,3 +31,15 @@ def test_statistics_of_rows_with_a_nan_or_infinity(vocab, dtype):
         one = torch.ones(4, device=lu.DEV)
         qb.qsdp_token_logprobs_backward(zg, tokens, 1.0, stats, entropy, one, one, d)
         assert d[:3].isnan().all() and d[3].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [7, 3001, 70001])
+def test_tokens_past_the_vocabulary_of_a_masked_row(vocab, dtype):
+    """A token that does not exist is NaN in every row, one that is not asked for 0."""
+    z = lu.to_gpu(torch.full((4, vocab), -math.inf, dtype=lu.DTYPES[dtype]))
+    tokens = torch.tensor([vocab, vocab - 1, -1, 1 << 40], device=lu.DEV)
+    for workspace in (None, full_workspace(z, 0)):
+        logprob, entropy, stats, _, _ = run_score(z, tokens, 1.0, 0, workspace)
+        assert logprob[0].isnan() and float(logprob[1]) == -math.inf and float(logprob[2]) == 0.0 and logprob[3].isnan()
+        assert bool((entropy == 0).all()) and bool((stats == -math.inf).all())
