@@ -657,7 +657,9 @@ int qsdp_token_logprobs_backward(const void* logits, qsdp_dtype dtype, uint64_t 
  * the logits (row_scale: the gradient of the total by loss[r], 1 where NULL); without it, or where
  * that gradient is not known yet, `stats` ([rows, 3], nullable: maximum, logs of the sums at the
  * temperature and at 1, of which alpha = 1 or 0 leaves one without a meaning) goes to
- * qsdp_distill_loss_backward with it as d_loss and the same alpha. d_logits may overwrite the logits. labels may be NULL for alpha = 1, the list for alpha = 0 (top = 0).
+ * qsdp_distill_loss_backward with it as d_loss and the same alpha. d_logits may overwrite the logits
+ * (same pointer and stride). The labels are not looked at for alpha = 1 (NULL allowed), the list
+ * not for alpha = 0 (top = 0 allowed).
  * A row of nothing but -inf: loss +inf if anything is asked of it, gradient 0. top <= 128.
  */
 int qsdp_distill_loss(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab,

@@ -38,6 +38,9 @@ bool distill_ok(int top, float alpha, const void* index, const void* logit, cons
            (top == 0 || (index && logit)) && (alpha == 1.0f || labels);
 }
 
+// Entries of a list of no weight are not read: what they hold would come into the gradient as a NaN.
+int looked_at(int top, float alpha) { return alpha > 0.0f ? top : 0; }
+
 // A channel is one bucket, or several buckets of whole steps of the product. (2^26 channels of 2^20 codes: 64 TB.)
 bool product_ok(uint64_t m, uint64_t n, uint64_t k, int bucket) {
     return m <= kMost && n >= 1 && n <= (1u << 26) && k >= 1 && k <= (1u << 20) && bucket >= 32 && bucket <= 8192 &&
@@ -112,8 +115,9 @@ int qsdp_distill_loss(const void* logits, qsdp_dtype dtype, uint64_t rows, uint6
     if (!aligned(logits, width(dtype)) || !aligned(teacher_index, 4) || !aligned(teacher_logit, 4) || !aligned(labels, 8) ||
         !aligned(row_scale, 4) || !aligned(loss, 4) || !aligned(stats, 4) || !aligned(d_logits, width(dtype)))
         return QSDP_EALIGN;
-    const DistillParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, teacher_index, teacher_logit, top,
-                             labels, temperature, alpha, row_scale, nullptr, loss, stats, d_logits, d_row_stride};
+    const DistillParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, teacher_index, teacher_logit,
+                             looked_at(top, alpha), labels, temperature, alpha, row_scale, nullptr, loss, stats, d_logits,
+                             d_row_stride};
     return status_of(by_format(dtype, [&](auto* t) {
         return launch_distill<std::remove_pointer_t<decltype(t)>>(p, static_cast<hipStream_t>(stream));
     }));
@@ -130,9 +134,9 @@ int qsdp_distill_loss_backward(const void* logits, qsdp_dtype dtype, uint64_t ro
     if (!aligned(logits, width(dtype)) || !aligned(teacher_index, 4) || !aligned(teacher_logit, 4) || !aligned(labels, 8) ||
         !aligned(stats, 4) || !aligned(d_loss, 4) || !aligned(d_logits, width(dtype)))
         return QSDP_EALIGN;
-    const DistillParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, teacher_index, teacher_logit, top,
-                             labels, temperature, alpha, nullptr, d_loss, nullptr, const_cast<float*>(stats), d_logits,
-                             d_row_stride};
+    const DistillParams p = {{logits, rows, vocab, row_stride, 1.0f / temperature, 0}, teacher_index, teacher_logit,
+                             looked_at(top, alpha), labels, temperature, alpha, nullptr, d_loss, nullptr,
+                             const_cast<float*>(stats), d_logits, d_row_stride};
     return status_of(by_format(dtype, [&](auto* t) {
         return launch_distill<std::remove_pointer_t<decltype(t)>>(p, static_cast<hipStream_t>(stream));
     }));

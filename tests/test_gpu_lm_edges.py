@@ -43,3 +43,22 @@ def test_tokens_past_the_vocabulary_of_a_masked_row(vocab, dtype):
         logprob, entropy, stats, _, _ = run_score(z, tokens, 1.0, 0, workspace)
         assert logprob[0].isnan() and float(logprob[1]) == -math.inf and float(logprob[2]) == 0.0 and logprob[3].isnan()
         assert bool((entropy == 0).all()) and bool((stats == -math.inf).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [9, 5003, 50257])
+def test_a_list_of_weight_zero_is_not_looked_at(vocab, dtype):
+    """alpha = 0: whatever the list holds, loss and gradient are the labels' alone."""
+    z = lu.to_gpu(lu.make_rows(3, vocab, lu.DTYPES[dtype], 0, seed=vocab))
+    index, logit = (t.to(lu.DEV) for t in lists(3, vocab, 5, vocab))
+    logit[0, 2], logit[1, 1], logit[2] = math.nan, math.inf, -math.inf
+    labels = torch.tensor([3, -1, 0], device=lu.DEV)
+    found = []
+    for i, t in ((None, None), (index, logit)):
+        loss, stats = torch.empty(3, device=lu.DEV), torch.empty((3, 3), device=lu.DEV)
+        d, after = torch.empty_like(z), torch.empty_like(z)
+        qb.qsdp_distill_loss(z, i, t, labels, 2.0, 0.0, None, loss, stats, d)
+        qb.qsdp_distill_loss_backward(z, i, t, labels, 2.0, 0.0, stats, torch.ones(3, device=lu.DEV), after)
+        assert loss.isfinite().all() and d.isfinite().all() and after.isfinite().all()
+        found.append((loss, stats, d, after))
+    assert all(torch.equal(a, b) for a, b in zip(*found))
