@@ -802,17 +802,17 @@ __global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void distill
     const float m = same(a.m), soft_log = same(log2f(a.s)), hard_log = MORE == Second::NONE ? soft_log : same(log2f(second));
     const bool empty = soft_log == kNegInf;
     const int k = (int)threadIdx.x;
-    float kl = 0.0f;
+    float kl = 0.0f;  // the temperature times the sum, in natural units: the lowest logit divided by it may be past the format
     if (k < p.top) {
         const float prob = list.p[k];
         if (prob > 0.0f || prob != prob) {
-            const float log2_q = empty ? kNegInf : (list.z[k] - m) * (p.in.inv_temperature * kLog2e) - soft_log;
-            kl = prob * (list.log2_p[k] - log2_q);
+            const float scaled_q = empty ? kNegInf : (list.z[k] - m) - p.temperature * (soft_log * kLn2);
+            kl = prob * (p.temperature * (list.log2_p[k] * kLn2) - scaled_q);
         }
     }
-    kl = reduce_block<THREADS>(kl, Add(), scratch) * kLn2;
+    kl = reduce_block<THREADS>(kl, Add(), scratch);
     if (k == 0) {
-        float loss = p.alpha > 0.0f ? p.alpha * p.temperature * p.temperature * kl : 0.0f;
+        float loss = p.alpha > 0.0f ? p.alpha * p.temperature * kl : 0.0f;
         if (label != ~0u) loss -= (1.0f - p.alpha) * (empty ? kNegInf : (z_label - m) - hard_log * kLn2);
         p.loss[r] = asked >= (int64_t)n ? __builtin_nanf("") : loss;
         if (p.stats) {

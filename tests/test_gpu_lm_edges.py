@@ -62,3 +62,31 @@ def test_a_list_of_weight_zero_is_not_looked_at(vocab, dtype):
         assert loss.isfinite().all() and d.isfinite().all() and after.isfinite().all()
         found.append((loss, stats, d, after))
     assert all(torch.equal(a, b) for a, b in zip(*found))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 0.75, 3.0])
+def test_lists_on_tokens_masked_with_the_lowest_value(tau, dtype):
+    """The student's logit at places of the list is the format's lowest: its log probability there is a large number and not
+    -inf, and so is the loss as far as binary32 holds it. Error: a probability of the list has an exponent of a magnitude below
+    16 with four roundings, an exponential, a sum of eight and a division, below 100 roundings; the terms and their sum have
+    twenty."""
+    dt, vocab = lu.DTYPES[dtype], 3001
+    z = lu.make_rows(3, vocab, dt, 0, seed=7)
+    index, logit = lists(3, vocab, 8, 7, 1.0)
+    z[0, int(index[0, 3])] = torch.finfo(dt).min
+    z[1, 100:] = torch.finfo(dt).min
+    index[1] = torch.arange(96, 104)
+    z[2] = torch.finfo(dt).min
+    z[2, 5] = 1.0
+    index[2] = torch.arange(3, 11)
+    labels = torch.tensor([1, 2, 5])
+    limit = torch.finfo(torch.float32).max
+    for alpha in (1.0, 0.5, 0.25):
+        want, want_d, _, off = lu.distill(z, index, logit, labels, tau, alpha)
+        zg, d, loss = lu.to_gpu(z), torch.empty((3, vocab), dtype=dt, device=lu.DEV), torch.empty(3, device=lu.DEV)
+        qb.qsdp_distill_loss(zg, index.to(lu.DEV), logit.to(lu.DEV), labels.to(lu.DEV), tau, alpha, None, loss, None, d)
+        got = loss.cpu().double()
+        assert bool(((got - want).abs() <= 128 * lu.EPS * want.abs())[want < 0.99 * limit].all())
+        assert bool((got == math.inf)[want > 1.01 * limit].all())
+        assert bool((want < 0.99 * limit)[0]) and lu.near(d, want_d, off)
