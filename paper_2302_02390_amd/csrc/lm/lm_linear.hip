@@ -9,6 +9,7 @@
 
 #include "lm_common.hpp"
 #include "lm_linear.hpp"
+#include "lm_plan.hpp"
 
 namespace qsdp_lm {
 namespace {
@@ -140,8 +141,6 @@ __device__ __forceinline__ void put4(typename O::raw* y, const float* v, int cou
 // read the same piece from all banks; the permutation is in the addresses that the lanes read from memory. A wave multiplies
 // WN channels (first operand, so that four consecutive channels of a token end up in a lane) by WM tokens. The matrix units bound
 // large products: 8192^3 495 us, 2223 TOP/s (the library's int8 product 2202), 8192 x 2048 x 8192 114-127 us.
-constexpr int kStep = 128;
-
 typedef __attribute__((address_space(1))) const void* global_ptr;
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
@@ -598,7 +597,7 @@ hipError_t launch_tokens(qsdp_dtype dtype, const TokenParams& p, hipStream_t s) 
 }
 
 template <int TN, int TM, int WN, int WM, int STAGES, bool BUCKETS, int GROUPS, class O>
-static hipError_t launch_tiles(const MatmulParams& p, hipStream_t s) {
+static hipError_t launch_tiles_of(const MatmulParams& p, hipStream_t s) {
     const uint32_t n_tiles = (uint32_t)((p.n + TN - 1) / TN), m_tiles = (uint32_t)((p.m + TM - 1) / TM);
     // in several launches where the tiles are more than a grid holds
     const uint32_t most = kMaxGrid / n_tiles ? kMaxGrid / n_tiles : 1;
@@ -625,47 +624,27 @@ static hipError_t launch_few(const MatmulParams& p, hipStream_t s) {
     return hipGetLastError();
 }
 
-// Time of a product with tiles of TN x TM by the steps of 128 codes and the tiles that a compute unit gets: us of a step with
-// one workgroup on the compute unit (it waits for its loads), of a step with all of them, and of a tile's start and end.
-struct Cost {
-    uint64_t tn, tm;
-    double alone, packed, tile;
-};
-static double cost_of(const MatmulParams& p, const Cost& c) {
-    const uint64_t tiles = (p.n + c.tn - 1) / c.tn * ((p.m + c.tm - 1) / c.tm), each = (tiles + 255) / 256;
-    const double steps = (double)((p.k + kStep - 1) / kStep), step = c.packed * (double)each;
-    return steps * (step > c.alone ? step : c.alone) + c.tile * (double)each;
-}
-// Measured on products of 8192 x 2048 x 8192, 4096^3, 2048^3, 512 x 8192 x 2048 and 512 x 2048 x 8192 (m x n x k), within a
-// fifth of these sums: us with 256-, 128- and 64-wide tiles 142 / 171 / 251, 68 / 81 / 112, 36 / 18 / 19, 35 / 18 / 18 and
-// 92 / 43 / 22.
-constexpr Cost kCost256 = {256, 256, 1.43, 1.95, 11.0}, kCost128 = {128, 128, 0.66, 0.58, 3.5}, kCost64 = {64, 64, 0.30, 0.21, 1.3};
-
-template <bool BUCKETS, class O>
-static hipError_t launch_small_tiles(const MatmulParams& p, hipStream_t s) {
-    // deeper where no more than two share a compute unit (512 x 2048 x 8192 32 / 22 us), else room for five (2048^3 22 / 19 us)
-    const uint64_t tiles = (p.n + 63) / 64 * ((p.m + 63) / 64);
-    // No more tiles than compute units: four teams to a tile where the steps are long enough to share (125 x 2048 x 8192 19 / 16 us,
-    // in eight buckets 30 / 20; 512 x 2048 x 8192 22 / 21, in eight buckets 33 / 25; 125 x 2048 x 2048 8.1 / 7.6, x 1024 6.1 / 6.4;
-    // operands in the caches).
-    if (tiles <= 256 && p.k >= 2048) return launch_tiles<64, 64, 32, 32, 2, BUCKETS, 4, O>(p, s);
-    if (tiles <= 512) return launch_tiles<64, 64, 32, 32, 4, BUCKETS, 1, O>(p, s);
-    return launch_tiles<64, 64, 32, 32, 2, BUCKETS, 1, O>(p, s);
+// The tile with one bucket to a channel, or with several.
+template <int TN, int TM, int WN, int WM, int STAGES, int GROUPS, class O>
+static hipError_t launch_tiles(const MatmulParams& p, hipStream_t s) {
+    return p.buckets > 1 ? launch_tiles_of<TN, TM, WN, WM, STAGES, true, GROUPS, O>(p, s)
+                         : launch_tiles_of<TN, TM, WN, WM, STAGES, false, GROUPS, O>(p, s);
 }
 
 template <class O>
 static hipError_t launch_matmul_to(const MatmulParams& p, hipStream_t s) {
-    // Few tokens: waves with loads of their own as long as the channels alone do not fill the chip (1 x 8192 x 2048 4.7 us, in
-    // tiles 7.6; 16 x 50257 x 2048 21 us, in tiles 18), more of them to a channel where there are fewer workgroups.
-    const uint64_t groups = (p.n + 15) / 16;
-    if (p.m <= 16 && groups <= 2048) return groups <= 512 ? launch_few<1, 8, 2, O>(p, s) : launch_few<1, 4, 3, O>(p, s);
-    if (p.m <= 32 && groups <= 1024) return groups <= 256 ? launch_few<2, 8, 2, O>(p, s) : launch_few<2, 4, 2, O>(p, s);
-    const double small = cost_of(p, kCost64), middle = cost_of(p, kCost128), large = cost_of(p, kCost256);
-    if (p.buckets > 1)  // the largest tile has no registers for sums over buckets
-        return small < middle ? launch_small_tiles<true, O>(p, s) : launch_tiles<128, 128, 64, 64, 2, true, 1, O>(p, s);
-    if (small < middle && small < large) return launch_small_tiles<false, O>(p, s);
-    if (middle < large) return launch_tiles<128, 128, 64, 64, 2, false, 1, O>(p, s);
-    return launch_tiles<256, 256, 64, 128, 2, false, 1, O>(p, s);
+    switch (choose_product(p.m, p.n, p.k, p.buckets)) {
+        case Product::FEW_16_8: return launch_few<1, 8, 2, O>(p, s);
+        case Product::FEW_16_4: return launch_few<1, 4, 3, O>(p, s);
+        case Product::FEW_32_8: return launch_few<2, 8, 2, O>(p, s);
+        case Product::FEW_32_4: return launch_few<2, 4, 2, O>(p, s);
+        case Product::TILE_64_TEAMS: return launch_tiles<64, 64, 32, 32, 2, 4, O>(p, s);
+        case Product::TILE_64_DEEP: return launch_tiles<64, 64, 32, 32, 4, 1, O>(p, s);
+        case Product::TILE_64: return launch_tiles<64, 64, 32, 32, 2, 1, O>(p, s);
+        case Product::TILE_128: return launch_tiles<128, 128, 64, 64, 2, 1, O>(p, s);
+        case Product::TILE_256: return launch_tiles_of<256, 256, 64, 128, 2, false, 1, O>(p, s);
+    }
+    return hipErrorInvalidValue;
 }
 
 hipError_t launch_matmul(qsdp_dtype out, const MatmulParams& p, hipStream_t s) {

@@ -5,6 +5,7 @@
 #include <type_traits>
 
 #include "lm_common.hpp"
+#include "lm_plan.hpp"
 #include "lm_rows.hpp"
 
 // A lambda is part of the function that calls it: what it refers to has to stay in registers.
@@ -58,8 +59,6 @@ __device__ __forceinline__ float same(float v) {
 // The first NV are in registers, up to HELD more in LDS, in places that only their thread uses. STREAM: the row has more
 // pieces than the workgroup holds and passes through chunk by chunk.
 enum class Rest { NONE, HELD, STREAM };
-// Pieces in LDS: two workgroups of 1024 threads, four of 512, to a compute unit's 160 KB, with what else they use.
-constexpr uint32_t held_pieces(int threads) { return threads == 1024 ? 4800 : 2240; }
 
 template <class T, int THREADS, int NV, Rest REST>
 struct Row {
@@ -876,28 +875,26 @@ hipError_t go(void (*kernel)(P), int threads, uint64_t work, P p, hipStream_t s)
     return hipSuccess;
 }
 
-// Threads and pieces per thread by the row's length: the smallest team that holds it, as 64 registers to a lane keep a
-// compute unit's 2048 threads; then with LDS, and the longest pass chunk by chunk.
-template <Rest REST>
-using RestOf = std::integral_constant<Rest, REST>;
-
-// FOUR: four workgroups of 512 threads to a compute unit, with LDS, rather than two of 1024 with registers alone: for what
-// writes as much as it reads (distillation of 8192 rows of 50257 bf16 logits 332 / 354 us; sums alone of 4096 rows 75 / 70).
+// f with the threads, pieces per thread and Rest of the team for rows of n elements (see choose_row).
 template <class T, bool FOUR, class F>
 hipError_t by_length(uint64_t n, F f) {
-    const uint64_t pieces = (n + T::PER - 1 + (sizeof(typename T::raw) == 2)) / T::PER;  // with a lead
-    const std::integral_constant<int, 2> two;
     const std::integral_constant<int, 8> eight;
-    const std::integral_constant<int, 1024> most;
-    if (pieces <= 128 * 2) return f(std::integral_constant<int, 128>(), two, RestOf<Rest::NONE>());
-    if (pieces <= 256 * 8) return f(std::integral_constant<int, 256>(), eight, RestOf<Rest::NONE>());
     const std::integral_constant<int, 512> half;
-    if (pieces <= 512 * 8) return f(half, eight, RestOf<Rest::NONE>());
-    if constexpr (FOUR)
-        if (pieces <= 512 * 8 + held_pieces(512)) return f(half, eight, RestOf<Rest::HELD>());
-    if (pieces <= 1024 * 8) return f(most, eight, RestOf<Rest::NONE>());
-    if (pieces <= 1024 * 8 + held_pieces(1024)) return f(most, eight, RestOf<Rest::HELD>());
-    return f(most, eight, RestOf<Rest::STREAM>());
+    const std::integral_constant<int, 1024> most;
+    const std::integral_constant<Rest, Rest::NONE> none;
+    const std::integral_constant<Rest, Rest::HELD> held;
+    switch (choose_row(row_pieces(n, T::PER), FOUR)) {
+        case RowTeam::T128: return f(std::integral_constant<int, 128>(), std::integral_constant<int, 2>(), none);
+        case RowTeam::T256: return f(std::integral_constant<int, 256>(), eight, none);
+        case RowTeam::T512: return f(half, eight, none);
+        case RowTeam::T512_LDS:
+            if constexpr (FOUR) return f(half, eight, held);
+            break;
+        case RowTeam::T1024: return f(most, eight, none);
+        case RowTeam::T1024_LDS: return f(most, eight, held);
+        case RowTeam::STREAM: return f(most, eight, std::integral_constant<Rest, Rest::STREAM>());
+    }
+    return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -909,9 +906,7 @@ hipError_t launch_score(const ScoreParams& p, hipStream_t s) {
             return by_length<T, false>(p.per, [&](auto threads, auto nv, auto rest) {
                 return go(score_kernel<T, threads, nv, rest, top, true>, threads, p.in.rows * kParts, p, s);
             });
-        // many rows with alternatives gain by four workgroups (4096 rows of 50257 bf16 logits, eight alternatives, 119 / 96 us),
-        // few lose (48 rows 10.5 / 12 us)
-        if (top && p.in.rows >= 512)
+        if (score_by_four(p.in.rows, p.top))
             return by_length<T, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
                 return go(score_kernel<T, threads, nv, rest, top, false>, threads, p.in.rows, p, s);
             });
