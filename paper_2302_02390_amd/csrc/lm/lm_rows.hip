@@ -875,8 +875,9 @@ hipError_t go(void (*kernel)(P), int threads, uint64_t work, P p, hipStream_t s)
     return hipSuccess;
 }
 
-// f with the threads, pieces per thread and Rest of the team for rows of n elements (see choose_row).
-template <class T, bool FOUR, class F>
+// f with the threads, pieces per thread and Rest of the team for rows of n elements (see choose_row). SHORT: there are rows for
+// the smallest team (parts of rows are longer).
+template <class T, bool FOUR, bool SHORT, class F>
 hipError_t by_length(uint64_t n, F f) {
     const std::integral_constant<int, 8> eight;
     const std::integral_constant<int, 512> half;
@@ -884,7 +885,9 @@ hipError_t by_length(uint64_t n, F f) {
     const std::integral_constant<Rest, Rest::NONE> none;
     const std::integral_constant<Rest, Rest::HELD> held;
     switch (choose_row(row_pieces(n, T::PER), FOUR)) {
-        case RowTeam::T128: return f(std::integral_constant<int, 128>(), std::integral_constant<int, 2>(), none);
+        case RowTeam::T128:
+            if constexpr (SHORT) return f(std::integral_constant<int, 128>(), std::integral_constant<int, 2>(), none);
+            break;
         case RowTeam::T256: return f(std::integral_constant<int, 256>(), eight, none);
         case RowTeam::T512: return f(half, eight, none);
         case RowTeam::T512_LDS:
@@ -903,14 +906,15 @@ template <class T>
 hipError_t launch_score(const ScoreParams& p, hipStream_t s) {
     auto rows = [&](auto top) {
         if (p.heads)
-            return by_length<T, false>(p.per, [&](auto threads, auto nv, auto rest) {
+            return by_length<T, false, false>(p.per, [&](auto threads, auto nv, auto rest) {
                 return go(score_kernel<T, threads, nv, rest, top, true>, threads, p.in.rows * kParts, p, s);
             });
-        if (score_by_four(p.in.rows, p.top))
-            return by_length<T, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
-                return go(score_kernel<T, threads, nv, rest, top, false>, threads, p.in.rows, p, s);
-            });
-        return by_length<T, false>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+        if constexpr (top)
+            if (score_by_four(p.in.rows, p.top))
+                return by_length<T, true, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+                    return go(score_kernel<T, threads, nv, rest, top, false>, threads, p.in.rows, p, s);
+                });
+        return by_length<T, false, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
             return go(score_kernel<T, threads, nv, rest, top, false>, threads, p.in.rows, p, s);
         });
     };
@@ -931,7 +935,7 @@ hipError_t launch_distill(const DistillParams& p, hipStream_t s) {
     const bool both = p.alpha > 0.0f && p.alpha < 1.0f && p.temperature != 1.0f;
     auto launch = [&](auto more) {
         if (!p.loss) return go(distill_backward_kernel<T, more>, 256, p.in.rows * Segment<T>::of(p.in.vocab), p, s);
-        return by_length<T, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
+        return by_length<T, true, true>(p.in.vocab, [&](auto threads, auto nv, auto rest) {
             return go(distill_kernel<T, threads, nv, rest, more>, threads, p.in.rows, p, s);
         });
     };
