@@ -509,15 +509,22 @@ __device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, f
     return top;
 }
 
+// The logit of a row's token, NaN where it has none.
+template <class T>
+__device__ __forceinline__ float logit_of(const typename T::raw* z, int64_t token, uint64_t vocab) {
+    const bool exists = (uint64_t)token < vocab;
+    const float v = T::get(z[exists ? token : 0]);  // asked for in any case, so that nothing waits here
+    return exists ? v : __builtin_nanf("");
+}
+
 // A row's results from its sums; one thread's work.
 __device__ __forceinline__ void put_score(const ScoreParams& p, uint64_t r, const Sums& a, float log_total, int64_t token,
                                           float z_token) {
     const bool empty = a.s == 0.0f;
     if (p.logprob) {
-        float v = 0.0f;
-        if (token >= 0) v = __builtin_nanf("");
-        if ((uint64_t)token < p.in.vocab) v = empty ? kNegInf : (z_token - a.m) * p.in.inv_temperature - log_total;
-        p.logprob[r] = v;
+        float v = (z_token - a.m) * p.in.inv_temperature - log_total;
+        if (empty && z_token == z_token) v = kNegInf;
+        p.logprob[r] = token < 0 ? 0.0f : v;
     }
     if (p.entropy) p.entropy[r] = empty ? 0.0f : log_total - a.u / a.s * kLn2;
     if (p.stats) {
@@ -535,7 +542,7 @@ __device__ __forceinline__ void put_top(const ScoreParams& p, uint64_t r, uint32
 // Alternatives: the `top`-th largest of the threads' group maxima is a threshold that at least `top` logits reach; the few that
 // do are collected and each is ranked by how many come before it.
 // HBM bounds calls of many rows: 4096 rows of 50257 bf16 logits 72 us (5.7 TB/s of reads), of fp32 ones with 64 alternatives
-// 185 us (4.5 TB/s). A call of one row is bound by its workgroup's chain of reductions: 50257 logits 10 us.
+// 158 us (5.2 TB/s). A call of one row is bound by its workgroup's chain of reductions: 50257 logits 10 us.
 // PART: one of kParts parts of a row, to be joined.
 template <class T, int THREADS, int NV, Rest REST, bool TOP, bool PART>
 __global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void score_kernel(ScoreParams p) {
@@ -548,12 +555,16 @@ __global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void score_k
     // the token is asked for ahead of the row, its logit right behind it
     const int64_t token = !PART && p.logprob ? p.tokens[r] : -1;
     Row<T, THREADS, NV, REST> row(z, PART && left > p.per ? p.per : left, held);
-    const float z_token = PART ? 0.0f : T::get(z[(uint64_t)token < p.in.vocab ? token : 0]);
+    const float z_token = PART ? 0.0f : logit_of<T>(z, token, p.in.vocab);
     Sums a = {kNegInf, 0.0f, 0.0f};
     float most = kNegInf, none = 0.0f;
     row.each_chunk([&]() QSDP_INLINE { add_chunk<true, Second::NONE>(row, scale2, 0.0f, a, none, most, T()); });
     a = join<THREADS, true, Second::NONE>(a, scale2, 0.0f, none, waves);
-    const float log_total = logf(a.s);
+    float log_total = logf(a.s);
+    if constexpr (TOP) {  // scalars: the search leaves no vector register to spare (fp32, 64 alternatives 192 us without, 158 with)
+        a = {same(a.m), same(a.s), same(a.u)};
+        log_total = same(log_total);
+    }
     if (threadIdx.x == 0) {
         if (PART) p.heads[item] = make_float4(a.m, a.s, a.u, 0.0f);
         else put_score(p, r, a, log_total, token, z_token);
@@ -593,7 +604,7 @@ __global__ __launch_bounds__(256) void score_join_kernel(ScoreParams p) {
         const float4 head = p.heads[r * kParts + part];
         a = {head.x, head.y, head.z};
     }
-    const float z_token = T::get(z[(uint64_t)token < p.in.vocab ? token : 0]);
+    const float z_token = logit_of<T>(z, token, p.in.vocab);
     const float m = reduce16(a.m, Max());
     rescale(a, m, p.in.inv_temperature * kLog2e);
     a = {m, reduce16(a.s, Add()), reduce16(a.u, Add())};

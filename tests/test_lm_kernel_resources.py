@@ -49,3 +49,27 @@ def test_every_kernel_on_rows_is_one_that_calls_reach(kernels):
     distill = {_row(args) for name, args in rows if name == "distill_kernel"}
     assert distill == {(t, f"LNS0_6SecondE{more}E") for t, more in product(TEAMS, range(3))}
     assert len([1 for name, _ in rows if name not in ("score_kernel", "distill_kernel")]) == 3 + 2 + 1
+
+
+def test_rows_stay_in_registers(kernels):
+    """64 registers to a lane, so that a compute unit has 2048 threads, and LDS for two workgroups of 1024 or four of 512. The search
+    for alternatives spills two registers at most, of what is the same for all rows' elements."""
+    rows, _ = kernels
+    for (name, args), (registers, spilled, lds) in rows.items():
+        assert spilled <= (2 if name == "score_kernel" and "ELb1ELb" in args else 0), (name, args, spilled)
+        if name in ("score_kernel", "distill_kernel"):
+            (threads, _, rest), _ = _row(args)
+            assert registers <= (128 if rest == STREAM else 64), (name, args, registers)
+            assert lds <= 160 * 1024 * threads // 2048, (name, args, lds)
+
+
+def test_registers_of_the_tiles(kernels):
+    """256 registers to a lane for 256-wide tiles and 128-wide ones of several buckets, which spill some outside the loop over the
+    codes; nothing else does."""
+    _, linear = kernels
+    for (name, args), (registers, spilled, lds) in linear.items():
+        wide = name == "tiles_kernel" and args.startswith("Li256E")
+        buckets = name == "tiles_kernel" and args.startswith("Li128E") and "ELb1E" in args
+        assert spilled <= (16 if wide else 2 if buckets else 0), (name, args, spilled)
+        assert registers <= 256 and lds <= 128 * 1024, (name, args, registers, lds)
+    assert len(linear) == 9 + 12 + 27
