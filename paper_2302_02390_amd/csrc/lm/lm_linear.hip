@@ -197,8 +197,8 @@ __device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_
     m = band * kBand + in % high;
 }
 
-// GROUPS of such teams share a tile where there are fewer tiles than compute units: each takes a run of the steps, and their sums
-// meet in LDS in the order of the groups. All make the same number of steps; those past a group's run multiply by zero.
+// GROUPS of such teams share a tile of several buckets where there are fewer tiles than compute units: each takes a run of the steps,
+// and their sums meet in LDS in the order of the groups. All make the same number of steps; those past a group's run multiply by zero.
 template <int TN, int TM, int WN, int WM, int STAGES, bool BUCKETS, int GROUPS, class O>
 __global__ __launch_bounds__((TN / WN) * (TM / WM) * GROUPS * 64, 2) void tiles_kernel(MatmulParams p, uint32_t n_tiles,
                                                                                  uint32_t m_tiles) {
@@ -363,6 +363,7 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * GROUPS * 64, 2) void tiles_
     multiply(other, s);
     fold(s);
     if constexpr (GROUPS > 1) {
+        static_assert(BUCKETS, "sums of whole numbers are not shared");
         static_assert((GROUPS - 1) * TN * TM * 4 <= GROUPS * STAGES * S::BYTES, "the sums of the other groups");
         v4i* meet = reinterpret_cast<v4i*>(&all[0][0][0]);
         auto place_of = [&](int g, int a, int b) { return ((g - 1) * A * B + a * B + b) * S::THREADS + wave * 64 + lane; };
@@ -372,9 +373,8 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * GROUPS * 64, 2) void tiles_
             for (int a = 0; a < A; ++a)
 #pragma unroll
                 for (int b = 0; b < B; ++b) {
-                    if constexpr (BUCKETS)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) d[a][b][c] = __float_as_int(sum_of[a][b][c]);
+                    for (int c = 0; c < 4; ++c) d[a][b][c] = __float_as_int(sum_of[a][b][c]);
                     meet[place_of(group, a, b)] = d[a][b];
                 }
         }
@@ -387,13 +387,11 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * GROUPS * 64, 2) void tiles_
 #pragma unroll
                 for (int b = 0; b < B; ++b) {
                     const v4i more = meet[place_of(g, a, b)];
-                    if constexpr (BUCKETS)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const int word = more[c];
-                            sum_of[a][b][c] += __int_as_float(word);
-                        }
-                    else d[a][b] += more;
+                    for (int c = 0; c < 4; ++c) {
+                        const int word = more[c];
+                        sum_of[a][b][c] += __int_as_float(word);
+                    }
                 }
     }
     // every scale is read before the first output is written: the compiler cannot know them apart
@@ -625,10 +623,10 @@ static hipError_t launch_few(const MatmulParams& p, hipStream_t s) {
 }
 
 // The tile with one bucket to a channel, or with several.
-template <int TN, int TM, int WN, int WM, int STAGES, int GROUPS, class O>
+template <int TN, int TM, int WN, int WM, int STAGES, class O>
 static hipError_t launch_tiles(const MatmulParams& p, hipStream_t s) {
-    return p.buckets > 1 ? launch_tiles_of<TN, TM, WN, WM, STAGES, true, GROUPS, O>(p, s)
-                         : launch_tiles_of<TN, TM, WN, WM, STAGES, false, GROUPS, O>(p, s);
+    return p.buckets > 1 ? launch_tiles_of<TN, TM, WN, WM, STAGES, true, 1, O>(p, s)
+                         : launch_tiles_of<TN, TM, WN, WM, STAGES, false, 1, O>(p, s);
 }
 
 template <class O>
@@ -638,10 +636,10 @@ static hipError_t launch_matmul_to(const MatmulParams& p, hipStream_t s) {
         case Product::FEW_16_4: return launch_few<1, 4, 3, O>(p, s);
         case Product::FEW_32_8: return launch_few<2, 8, 2, O>(p, s);
         case Product::FEW_32_4: return launch_few<2, 4, 2, O>(p, s);
-        case Product::TILE_64_TEAMS: return launch_tiles<64, 64, 32, 32, 2, 4, O>(p, s);
-        case Product::TILE_64_DEEP: return launch_tiles<64, 64, 32, 32, 4, 1, O>(p, s);
-        case Product::TILE_64: return launch_tiles<64, 64, 32, 32, 2, 1, O>(p, s);
-        case Product::TILE_128: return launch_tiles<128, 128, 64, 64, 2, 1, O>(p, s);
+        case Product::TILE_64_TEAMS: return launch_tiles_of<64, 64, 32, 32, 2, true, 4, O>(p, s);
+        case Product::TILE_64_DEEP: return launch_tiles<64, 64, 32, 32, 4, O>(p, s);
+        case Product::TILE_64: return launch_tiles<64, 64, 32, 32, 2, O>(p, s);
+        case Product::TILE_128: return launch_tiles<128, 128, 64, 64, 2, O>(p, s);
         case Product::TILE_256: return launch_tiles_of<256, 256, 64, 128, 2, false, 1, O>(p, s);
     }
     return hipErrorInvalidValue;

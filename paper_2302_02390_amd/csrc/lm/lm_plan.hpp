@@ -55,13 +55,15 @@ constexpr double cost_of(uint64_t m, uint64_t n, uint64_t k, const Cost& c) {
 // 92 / 43 / 22.
 constexpr Cost kCost256 = {256, 256, 1.43, 1.95, 11.0}, kCost128 = {128, 128, 0.66, 0.58, 3.5}, kCost64 = {64, 64, 0.30, 0.21, 1.3};
 
-constexpr Product choose_small_tile(uint64_t m, uint64_t n, uint64_t k) {
+constexpr Product choose_small_tile(uint64_t m, uint64_t n, uint64_t k, uint64_t buckets) {
     // deeper where no more than two share a compute unit (512 x 2048 x 8192 32 / 22 us), else room for five (2048^3 22 / 19 us)
     const uint64_t tiles = (n + 63) / 64 * ((m + 63) / 64);
-    // No more tiles than compute units: four teams to a tile where the steps are long enough to share (125 x 2048 x 8192 19 / 16 us,
-    // in eight buckets 30 / 20; 512 x 2048 x 8192 22 / 21, in eight buckets 33 / 25; 125 x 2048 x 2048 8.1 / 7.6, x 1024 6.1 / 6.4;
-    // operands in the caches).
-    if (tiles <= 256 && k >= 2048) return Product::TILE_64_TEAMS;
+    // Several buckets and no more tiles than compute units: four teams to a tile where the steps are long enough to share (us without /
+    // with, weights from memory: 125 x 2048 x 8192 in eight buckets 35.2 / 31.1, 512 x 2048 x 8192 35.0 / 30.1, 100 x 1024 x 4096 in
+    // four 18.3 / 16.2, 125 x 2048 x 2048 in two 11.6 / 11.3; out of the caches 31.8 / 23.3, 31.9 / 24.0). With one bucket, whose sums
+    // take nothing in between, teams lose as soon as the weights come from memory (125 x 2048 x 8192 23.1 / 27.4, 40 x 16384 x 2048
+    // 11.9 / 13.3; out of the caches 19.8 / 18.9, 9.8 / 11.3).
+    if (buckets > 1 && tiles <= 256 && k >= 2048) return Product::TILE_64_TEAMS;
     return tiles <= 512 ? Product::TILE_64_DEEP : Product::TILE_64;
 }
 
@@ -73,8 +75,8 @@ constexpr Product choose_product(uint64_t m, uint64_t n, uint64_t k, uint64_t bu
     if (m <= 32 && groups <= 1024) return groups <= 256 ? Product::FEW_32_8 : Product::FEW_32_4;
     const double small = cost_of(m, n, k, kCost64), middle = cost_of(m, n, k, kCost128), large = cost_of(m, n, k, kCost256);
     if (buckets > 1)  // the largest tile has no registers for sums over buckets
-        return small < middle ? choose_small_tile(m, n, k) : Product::TILE_128;
-    if (small < middle && small < large) return choose_small_tile(m, n, k);
+        return small < middle ? choose_small_tile(m, n, k, buckets) : Product::TILE_128;
+    if (small < middle && small < large) return choose_small_tile(m, n, k, buckets);
     return middle < large ? Product::TILE_128 : Product::TILE_256;
 }
 

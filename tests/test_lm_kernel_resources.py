@@ -72,4 +72,4 @@ def test_registers_of_the_tiles(kernels):
         buckets = name == "tiles_kernel" and args.startswith("Li128E") and "ELb1E" in args
         assert spilled <= (16 if wide else 2 if buckets else 0), (name, args, spilled)
         assert registers <= 256 and lds <= 128 * 1024, (name, args, registers, lds)
-    assert len(linear) == 9 + 12 + 27
+    assert len(linear) == 9 + 12 + 24

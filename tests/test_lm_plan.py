@@ -45,8 +45,15 @@ def test_products_of_the_gpu_tests(ask):
     got = [PRODUCTS[v] for v in ask("p", asked)]
     assert got == [c[0] for c in gpu.PRODUCTS]
     reached = {(name, c[3] > 1) for name, c in zip(got, asked)}
-    every = {(name, several) for name in PRODUCTS for several in (False, True)} - {("TILE_256", True)}
-    assert every - reached <= {("TILE_64_TEAMS", False)}
+    assert reached == {(name, several) for name in PRODUCTS for several in (False, True)} - {("TILE_256", True),
+                                                                                             ("TILE_64_TEAMS", False)}
+
+
+def test_teams_share_a_tile_of_several_buckets_only(ask):
+    """A tile of one bucket is faster without, but for weights that are in the caches."""
+    sizes = [(m, n, k) for m in (33, 125, 512, 900) for n in (64, 1000, 2048, 16384) for k in (2048, 5000, 8192, 1 << 20)]
+    assert all(PRODUCTS[v] != "TILE_64_TEAMS" for v in ask("p", [(m, n, k, 1) for m, n, k in sizes]))
+    assert PRODUCTS[ask("p", [(125, 2048, 8192, 8)])[0]] == "TILE_64_TEAMS"
 
 
 def test_rows_of_the_gpu_tests(ask):
