@@ -597,8 +597,9 @@ int qsdp_recv_adamw_step_segmented(float* x, float* m, float* v, const qsdp_segm
 
 /* ---------------------------------------------------------------------------------------------
  * Operators on logits and on packed weights: what a run that trains or serves quantized weights
- * does next to the codec. Conventions as above but for alignment: matrices of logits, tokens and
- * outputs need the alignment of their elements only, 16 bytes are needed where said. A matrix is
+ * does next to the codec (losses with their gradients, products for serving). Conventions as above
+ * but for alignment: matrices of logits, tokens and outputs need the alignment of their elements
+ * only, 16 bytes are needed where said. A matrix is
  * rows of consecutive elements, `row_stride` elements apart (at least the row's length; not looked
  * at for a single row). Formats QSDP_F32, QSDP_BF16, QSDP_F16 in and out, binary32 (or exact whole
  * numbers) inside, one rounding at the end. No rows (rows or m = 0): QSDP_OK, nothing is done.
@@ -635,7 +636,7 @@ int qsdp_token_logprobs(const void* logits, qsdp_dtype dtype, uint64_t rows, uin
  * NULL; stats, and with h the entropy, as qsdp_token_logprobs gave them):
  *   d_logits[r, j] = (g ([j = tokens[r]] - p_j) - h p_j (log p_j + entropy)) / temperature
  * in the format of the logits, which d_logits may overwrite (same pointer and stride). A row
- * without a token has no part from g.
+ * without a token, or with one >= vocab, has no part from g.
  */
 int qsdp_token_logprobs_backward(const void* logits, qsdp_dtype dtype, uint64_t rows,
                                  uint64_t vocab, uint64_t row_stride, const int64_t* tokens,
@@ -657,10 +658,14 @@ int qsdp_token_logprobs_backward(const void* logits, qsdp_dtype dtype, uint64_t 
  * the logits (row_scale: the gradient of the total by loss[r], 1 where NULL); without it, or where
  * that gradient is not known yet, `stats` ([rows, 3], nullable: maximum, logs of the sums at the
  * temperature and at 1, of which alpha = 1 or 0 leaves one without a meaning) goes to
- * qsdp_distill_loss_backward with it as d_loss and the same alpha. d_logits may overwrite the logits
- * (same pointer and stride). The labels are not looked at for alpha = 1 (NULL allowed), the list
- * not for alpha = 0 (top = 0 allowed).
- * A row of nothing but -inf: loss +inf if anything is asked of it, gradient 0. top <= 128.
+ * qsdp_distill_loss_backward with it as d_loss and the same temperature and alpha. d_logits may
+ * overwrite the logits (same pointer and stride). The labels are not looked at for alpha = 1 (NULL
+ * allowed), the list not for alpha = 0 (top = 0 allowed).
+ * A row of nothing but -inf: loss +inf if anything is asked of it, gradient 0. A row with a NaN or
+ * +inf: NaN in loss and gradient if anything is asked of it, else 0 in both. A NaN or +inf in a
+ * present slot of the list: NaN in the loss and in the gradient at the list's places. A label
+ * >= vocab has no part in the gradient. Where row_scale or d_loss is 0 the gradient is 0, whatever
+ * the row holds. top <= 128.
  */
 int qsdp_distill_loss(const void* logits, qsdp_dtype dtype, uint64_t rows, uint64_t vocab,
                       uint64_t row_stride, const int32_t* teacher_index,
@@ -692,6 +697,8 @@ int qsdp_distill_loss_backward(const void* logits, qsdp_dtype dtype, uint64_t ro
  *   y = s * sum_buckets (scale D + (base + 128 scale) sums) + bias
  *   wcodes 16-byte, wmeta 8-byte aligned; bias nullable float[n]
  * qsdp_linear_codes does both; workspace: qsdp_tokens_bytes(m, k, bucket) bytes, 16-byte aligned.
+ * There is no gradient for the tokens: the product is for weights that answer. A training step
+ * decodes them (qsdp_dequantize).
  */
 size_t qsdp_tokens_bytes(uint64_t m, uint64_t k, int bucket);
 int qsdp_quantize_tokens(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k,

@@ -90,3 +90,36 @@ def test_lists_on_tokens_masked_with_the_lowest_value(tau, dtype):
         assert bool(((got - want).abs() <= 128 * lu.EPS * want.abs())[want < 0.99 * limit].all())
         assert bool((got == math.inf)[want > 1.01 * limit].all())
         assert bool((want < 0.99 * limit)[0]) and lu.near(d, want_d, off)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [301, 50257, 131073])
+def test_what_is_no_number_in_distillation(vocab, dtype):
+    """A NaN or +inf among the logits makes loss and gradient NaN where anything is asked of the row; among the teacher's, the loss
+    and the gradient at the list's places; a label past the vocabulary the loss alone. No row_scale, no gradient."""
+    z = lu.make_rows(9, vocab, lu.DTYPES[dtype], 1, seed=vocab)
+    index, logit = lists(9, vocab, 6, vocab)
+    z[0, vocab // 2] = math.nan
+    z[1, vocab - 1] = math.inf
+    z[2, 0], index[2] = math.nan, -1              # neither list nor label
+    z[3, 5] = math.nan                            # row_scale 0
+    logit[4, 2] = math.nan
+    logit[5, 3] = math.inf
+    logit[6, 1], index[6, 1] = math.nan, -1       # an absent slot's
+    labels = torch.tensor([1, -1, -1, 4, 5, -1, 7, vocab, 1 << 33])
+    scale = torch.tensor([1.0, 1.0, 1.0, 0.0, 1.0, 1.0, 1.0, 1.0, 1.0])
+    zg, ig, tg, lg, sg = lu.to_gpu(z), index.to(lu.DEV), logit.to(lu.DEV), labels.to(lu.DEV), scale.to(lu.DEV)
+    for tau in (1.0, 2.0, 3.0):
+        loss, stats = torch.empty(9, device=lu.DEV), torch.empty((9, 3), device=lu.DEV)
+        d, after = (torch.empty((9, vocab), dtype=z.dtype, device=lu.DEV) for _ in range(2))
+        qb.qsdp_distill_loss(zg, ig, tg, lg, tau, 0.5, sg, loss, stats, d)
+        qb.qsdp_distill_loss_backward(zg, ig, tg, lg, tau, 0.5, stats, sg, after)
+        assert loss.isnan().tolist() == [True, True, False, True, True, True, False, True, True] and float(loss[2]) == 0.0
+        listed = torch.zeros((9, vocab), dtype=torch.bool)
+        listed[4, index[4].long()] = listed[5, index[5].long()] = True
+        listed[:2] = True
+        for g in (d, after):
+            assert torch.equal(g.isnan().cpu(), listed)
+            assert bool((g[2:4] == 0).all())
+        _, want, _, off = lu.distill(z[6:], index[6:], logit[6:], labels[6:], tau, 0.5)
+        assert lu.near(d[6:], want, off) and lu.near(after[6:], want, off)
