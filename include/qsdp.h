@@ -636,7 +636,8 @@ int qsdp_token_logprobs(const void* logits, qsdp_dtype dtype, uint64_t rows, uin
  * NULL; stats, and with h the entropy, as qsdp_token_logprobs gave them):
  *   d_logits[r, j] = (g ([j = tokens[r]] - p_j) - h p_j (log p_j + entropy)) / temperature
  * in the format of the logits, which d_logits may overwrite (same pointer and stride). A row
- * without a token, or with one >= vocab, has no part from g.
+ * without a token, or with one >= vocab, has no part from g. Here and in distillation a p_j (or q_j)
+ * below 2^-126 counts as 0.
  */
 int qsdp_token_logprobs_backward(const void* logits, qsdp_dtype dtype, uint64_t rows,
                                  uint64_t vocab, uint64_t row_stride, const int64_t* tokens,

@@ -22,7 +22,7 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 // s = max |x| times the rounded 1/127, q = rint(x / s) with an IEEE division in binary32; slots past k are zero. A workgroup
 // per token, which keeps the token in registers between its maximum and its codes: eight elements to a thread at a time, of
 // which the NV-th part is the last that is held; a longer token is read twice. HBM bounds it for many tokens: 8192 of 8192 bf16
-// elements 45 us, 4.5 TB/s both ways.
+// elements 45 us, 4.5 TB/s both ways. Buckets are added up one after the other, so many short ones cost (8192 in eight: 68 us).
 template <class T>
 struct Eight {
     float v[8];
@@ -139,8 +139,12 @@ __device__ __forceinline__ void put4(typename O::raw* y, const float* v, int cou
 // STAGES steps deep: while one is multiplied the next ones are on their way, and one barrier a step separates them. LDS holds rows of
 // 128 bytes whose eight pieces of 16 are permuted by the row (piece c of row r in place c ^ (r % 8)), so that sixteen rows
 // read the same piece from all banks; the permutation is in the addresses that the lanes read from memory. A wave multiplies
-// WN channels (first operand, so that four consecutive channels of a token end up in a lane) by WM tokens. The matrix units bound
-// large products: 8192^3 495 us, 2223 TOP/s (the library's int8 product 2202), 8192 x 2048 x 8192 114-127 us.
+// WN channels (first operand, so that four consecutive channels of a token end up in a lane) by WM tokens. Large products: 8192^3
+// 495 us, 2223 TOP/s (the library's int8 product 2202), 8192 x 2048 x 8192 117-122 us. What bounds them there is the turn of the
+// steps: the matrix units are busy in 51 % of the cycles, a third of the waves' time goes to waits for loads and at the barrier
+// that ends each step, which two waves to a SIMD do not fill; reads of LDS hold up 2 %. The 256-wide tile spills 4 (fp32 outputs) to
+// 16 registers, the 128-wide one of several buckets 2, all outside the loop over the steps. With several buckets, in 128-wide
+// tiles that add their sums up at each end, 8192 x 2048 x 8192 takes 193 us in eight.
 typedef __attribute__((address_space(1))) const void* global_ptr;
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
@@ -438,7 +442,7 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * GROUPS * 64, 2) void tiles_
 // codes of a channel: by buckets, or a bucket's codes among several waves, so that enough loads are on their way. Each wave
 // moves its codes through LDS of its own, as the tiles do, and waits for nobody. Whole numbers meet in LDS before they are
 // scaled; waves that take whole buckets scale their own, and their sums meet in the order of the waves. One token times 8192 x 2048
-// 6.3 us (2.7 TB/s: the latency of the loads).
+// 6.3 us (2.7 TB/s: the latency of the loads, and as many bytes of tokens through LDS as of weights).
 template <int MT, int WAVES, int STAGES, class O>
 __global__ __launch_bounds__(WAVES * 64) void few_kernel(MatmulParams p) {
     constexpr int ROWS = 16 + 16 * MT, LOADS = 2 + 2 * MT;

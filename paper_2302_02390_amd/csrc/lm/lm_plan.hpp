@@ -68,8 +68,11 @@ constexpr Product choose_small_tile(uint64_t m, uint64_t n, uint64_t k, uint64_t
 }
 
 constexpr Product choose_product(uint64_t m, uint64_t n, uint64_t k, uint64_t buckets) {
-    // Few tokens: waves with loads of their own as long as the channels alone do not fill the chip (1 x 8192 x 2048 4.7 us, in
-    // tiles 7.6; 16 x 50257 x 2048 21 us, in tiles 18), more of them to a channel where there are fewer workgroups.
+    // Few tokens: waves with loads of their own as long as the channels alone do not fill the chip, more of them to a channel where
+    // there are fewer workgroups. Weights from memory, us by such waves / in tiles: 1 x 8192 x 2048 6.2 / 9.4, 16 x 2048 x 2048 4.5 / 8.5,
+    // 32 x 4096 x 2048 5.9 / 9.8, 32 x 2048 x 8192 11 / 22; 16 x 50257 x 2048 29 / 24, 32 x 32768 x 2048 27 / 19. Between, the two cross
+    // earlier for short channels (16 x 16384 x 2048 11.9 / 10.9, 32 x 16384 x 2048 14.5 / 11.7) and later for long ones (1 x 50257 x 8192
+    // 82 / 106), which these limits leave out.
     const uint64_t groups = (n + 15) / 16;
     if (m <= 16 && groups <= 2048) return groups <= 512 ? Product::FEW_16_8 : Product::FEW_16_4;
     if (m <= 32 && groups <= 1024) return groups <= 256 ? Product::FEW_32_8 : Product::FEW_32_4;

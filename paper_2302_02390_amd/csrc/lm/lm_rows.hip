@@ -1,7 +1,8 @@
 // Kernels on rows of logits: log probabilities with entropy and top alternatives, their gradient, and distillation from a
 // teacher's top logits. A workgroup per row; its threads hold the row in registers in the logits' format, 16 bytes to a
-// piece, so that the logits are read once whatever follows: maximum, sums of exponentials, alternatives, gradient. Rows that
-// do not fit are read once per use, chunk by chunk.
+// piece, and in LDS what is left, so that the logits are read once whatever follows: maximum, sums of exponentials, alternatives,
+// gradient. Rows of more than 51968 (binary32) or 103935 (16 bits) logits do not fit and are read once per use, chunk by chunk
+// (2048 rows of 65536 fp32 logits with 20 alternatives 162 us, of 131072 329, in bf16 185; without alternatives 178 and 93).
 #include <type_traits>
 
 #include "lm_common.hpp"
@@ -352,6 +353,7 @@ __device__ __forceinline__ Sums join(Sums a, float scale2, float other2, float& 
 
 // ---- top alternatives ------------------------------------------------------------------------------------------------
 // Order: value downwards (a NaN above all, the two zeros equal), then index upwards; larger keys first.
+// The search has no vector register to spare at 64: it spills two at most, of values that are the same for a wave's elements.
 __device__ __forceinline__ uint32_t value_key(float z) {
     const uint32_t u = __float_as_uint(z + 0.0f);
     return z != z ? 0xffffffffu : (int32_t)u < 0 ? ~u : u | 0x80000000u;
@@ -398,7 +400,9 @@ __device__ __forceinline__ void collect(R& row, TopRoom<THREADS>& room, H hit) {
 // The `top` first elements, as keys in room.list[0 .. return value), in no order and with some more. Threshold: the top-th
 // largest of up to 256 groups' maxima, which at least `top` elements reach and on ordinary data not many more (about
 // -g log(1 - top / g) of g groups: 74 for 64). Where too many reach it (ties, masks, large values in few groups) or a NaN takes
-// part, the top-th value itself is found bit by bit, and of its equals the first by index are taken.
+// part, the top-th value itself is found bit by bit, and of its equals the first by index are taken: 32 passes over the row,
+// which is slow (48 rows of 50257 bf16 logits with 20 alternatives 11 us, 73 where a mask leaves 30 neighbours; 16 rows of 1000
+// fp32 ones 5.5 us with 20 alternatives, 104 with 128).
 template <class T, int THREADS, class R>
 __device__ __forceinline__ uint32_t top_list(R& row, uint32_t top, bool plain, float most, TopRoom<THREADS>& room) {
     constexpr int GROUPS = TopRoom<THREADS>::GROUPS, SHARE = THREADS / GROUPS, LOW = key_low_bits<T>();
@@ -541,7 +545,7 @@ __device__ __forceinline__ void put_top(const ScoreParams& p, uint64_t r, uint32
 // m, S = sum 2^a and U = sum 2^a a with a = (z - m) scale2 give the log probability of any logit, and the entropy log S - U ln2 / S.
 // Alternatives: the `top`-th largest of the threads' group maxima is a threshold that at least `top` logits reach; the few that
 // do are collected and each is ranked by how many come before it.
-// HBM bounds calls of many rows: 4096 rows of 50257 bf16 logits 72 us (5.7 TB/s of reads), of fp32 ones with 64 alternatives
+// HBM bounds calls of many rows: 4096 rows of 50257 bf16 logits 73 us (5.6 TB/s of reads), of fp32 ones with 64 alternatives
 // 158 us (5.2 TB/s). A call of one row is bound by its workgroup's chain of reductions: 50257 logits 10 us.
 // PART: one of kParts parts of a row, to be joined.
 template <class T, int THREADS, int NV, Rest REST, bool TOP, bool PART>
@@ -789,7 +793,9 @@ struct Slope {
 
 // Loss, and in the same pass the gradient if it is asked for: the row is still in registers and LDS when its sums are known. Two
 // sums at once (at the temperature and at 1), where both terms are asked for, by one exponential if the temperature is 2: the
-// square of e^(t/2) is e^t. HBM bounds it: 8192 rows of 50257 bf16 logits with 32 in the list 331 us, 5.0 TB/s both ways.
+// square of e^(t/2) is e^t. HBM bounds it: 8192 rows of 50257 bf16 logits with 32 in the list 333 us, 4.9 TB/s both ways (at
+// temperature 3, by two exponentials, a hundredth more; 2048 rows with 64 101 us, at temperature 3 110). The loss alone 150 us, 5.5
+// TB/s of reads.
 template <class T, int THREADS, int NV, Rest REST, Second MORE>
 __global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void distill_kernel(DistillParams p) {
     __shared__ float waves[THREADS / 64][4], scratch[THREADS / 64];
@@ -845,7 +851,9 @@ __global__ __launch_bounds__(THREADS, REST == Rest::STREAM ? 4 : 8) void distill
     slope.template aim<T>(list, p.top, z_label, dz, 0, n);
 }
 
-// The gradient alone, from the row's statistics: rows are cut into pieces as for the gradient of log probabilities.
+// The gradient alone, from the row's statistics: rows are cut into segments as for the gradient of log probabilities, each of which
+// computes the list's probabilities. 8192 rows of 50257 bf16 logits with 32 in the list 289 us (5.7 TB/s both ways), 2048 rows with
+// 64 90 us (4.6).
 template <class T, Second MORE>
 __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p) {
     __shared__ float scratch[4];
