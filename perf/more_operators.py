@@ -21,7 +21,7 @@ AdamW: m' = beta1 m + (1 - beta1) g, v' = beta2 v + (1 - beta2) g^2,
   largest |m| and sqrt v. With w the value over M / 127^2 (or R / 255^2) and c = floor sqrt w the new code is c + 1 where
   w - c^2 > (2 c + 1) t, else c; at most 127 (255), and at least 1 where v' > 0. The threshold t of element i of the block is
   (h + 1/2) / 2^12, h the upper 12 bits of (word + i 0x9E3779B9) mod 2^32, word the first (for m) or second (for v) of the
-  Philox4x32-10 block with the seed as key and counter (block, 0, 2, 0). Tensors' blocks are numbered in order, each
+  Philox4x32-10 block with the seed as key and counter (block, 0, 3, 0). Tensors' blocks are numbered in order, each
   tensor's from the next multiple of 8 on.
 """
 import math
@@ -378,7 +378,7 @@ def _moved(p, m, v):
 
 
 def _words(block, seed):
-    """The first two words of the Philox4x32-10 blocks with key `seed` and counters (block, 0, 2, 0)."""
+    """The first two words of the Philox4x32-10 blocks with key `seed` and counters (block, 0, 3, 0)."""
     low = 0xFFFFFFFF
 
     def product(a, c):  # upper and lower half, out of two that fit 64 bits
@@ -386,7 +386,7 @@ def _words(block, seed):
         whole = top + (bottom >> 16)
         return whole >> 16, ((whole & 0xFFFF) << 16) | (bottom & 0xFFFF)
 
-    c = [block & low, block >> 32, torch.full_like(block, 2), torch.zeros_like(block)]
+    c = [block & low, block >> 32, torch.full_like(block, 3), torch.zeros_like(block)]
     k0, k1 = seed & low, seed >> 32
     for _ in range(10):
         (h0, l0), (h1, l1) = product(0xD2511F53, c[0]), product(0xCD9E8D57, c[2])
