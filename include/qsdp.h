@@ -715,6 +715,130 @@ int qsdp_linear_codes(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k,
                       uint64_t y_row_stride, void* workspace, uint64_t workspace_bytes,
                       void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators of a training step in few bits: what a step does next to the codec (norms, products in
+ * 8-bit floating point, the optimizer of many tensors). Conventions, matrices and alignment as for
+ * the operators on logits: elements' alignment, 16 bytes where said, binary32 inside, one rounding
+ * at the end, no atomics, so that equal calls give equal bits. Infinities and NaN are allowed.
+ * ---------------------------------------------------------------------------------------------
+ *
+ * Layer norm of every row x of n elements:
+ *   mean = sum x / n, rstd = 1 / sqrt(sum (x - mean)^2 / n + eps), y = (x - mean) rstd weight + bias
+ * weight, bias: [n] in w_dtype, which is QSDP_F32 or the format of y; a NULL one is 1 (0). y has
+ * the format of x, or any where x is QSDP_F32; it may overwrite x where the formats and strides are
+ * the same. stats, nullable: {mean, rstd} of each row, what the gradient needs. eps >= 0 (0 and a
+ * constant row: NaN). A row with a NaN or an infinity: NaN. n <= 2^24.
+ */
+int qsdp_layer_norm(const void* x, qsdp_dtype dtype, uint64_t rows, uint64_t n, uint64_t row_stride,
+                    const void* weight, const void* bias, qsdp_dtype w_dtype, float eps, void* y,
+                    qsdp_dtype y_dtype, uint64_t y_row_stride, float* stats, void* stream);
+
+/*
+ * Its gradients, with h = (x - mean) rstd and g = dy weight:
+ *   dx = rstd (g - mean of g - h (mean of g h)),  dw = sum over rows of dy h,  db = sum over rows of dy
+ * dy: the format of y; dx: that of x, it may overwrite dy or x where format and stride are the same.
+ * dw, db: float[n], added to what they hold with accumulate != 0. Each of the three may be NULL, but
+ * not all. No rows: dw and db are 0, or stay as they are with accumulate.
+ *   workspace    qsdp_layer_norm_backward_bytes(rows, n) bytes, 16-byte aligned, where dw or db is
+ *                asked for. Its contents need no preparation and are not kept.
+ */
+size_t qsdp_layer_norm_backward_bytes(uint64_t rows, uint64_t n);
+int qsdp_layer_norm_backward(const void* x, qsdp_dtype dtype, uint64_t rows, uint64_t n,
+                             uint64_t row_stride, const void* weight, qsdp_dtype w_dtype,
+                             const float* stats, const void* dy, qsdp_dtype dy_dtype,
+                             uint64_t dy_row_stride, void* dx, uint64_t dx_row_stride, float* dw,
+                             float* db, int accumulate, void* workspace, uint64_t workspace_bytes,
+                             void* stream);
+
+/*
+ * 8-bit floating point in blocks. A code is an e4m3 number (four bits of exponent, three of mantissa,
+ * largest 448, no infinities); 128 consecutive codes of a row share a scale, or 128 x 128 do:
+ *   a = max(max |x|, 2^-100) over the block,  code = e4m3(x (448 / a)),  scale = a / 448
+ * to nearest even, in binary32 with IEEE divisions; x stands for scale * code. A NaN stays one; a block
+ * with an infinity has an infinite scale, and what is summed over it is NaN.
+ *   codes    uint8[rows, ceil(cols / 128) * 128], zeros past cols, 16-byte aligned
+ *   scales   float[ceil(cols / 128), rows], or [ceil(cols / 128), ceil(rows / 128)] with square != 0
+ * and the transposed matrix, whose blocks lie along the columns of x (square ones are the same):
+ *   codes_t  uint8[cols, ceil(rows / 128) * 128], scales_t  float[ceil(rows / 128), cols or blocks]
+ * Either pair may be NULL. A training step needs both: codes for the product with a weight, codes_t for
+ * the sums over rows in the weight's gradient. rows, cols <= 2^26.
+ *
+ * qsdp_matmul_blocks: y[m, n] = A B^T (+ bias) (+ y with accumulate != 0), A [m, k] in blocks of a row,
+ * B [n, k] in square blocks (b_square != 0) or blocks of a row, codes and scales as above, the codes
+ * past k zero in both. Forward: A = x, B = W. Gradient of x: A = dy, B = W transposed. Gradient of W:
+ * A = dy transposed, B = x transposed. bias float[n], nullable. m < 2^31, n <= 2^26, k <= 2^20.
+ *   workspace  qsdp_matmul_blocks_bytes(m, n, k) bytes, 16-byte aligned, let a call of few tiles and a
+ *              long sum share the sum among workgroups (0 bytes: no use for one). Less or none is
+ *              allowed and slower; the order of additions goes by whether it is given.
+ *
+ * qsdp_linear_blocks: y = x W^T + bias with W in square blocks, x [m, k] rounded on the way.
+ *   workspace  qsdp_linear_blocks_bytes(m, n, k) bytes, 16-byte aligned
+ */
+int qsdp_quantize_blocks(const void* x, qsdp_dtype dtype, uint64_t rows, uint64_t cols,
+                         uint64_t row_stride, int square, uint8_t* codes, float* scales,
+                         uint8_t* codes_t, float* scales_t, void* stream);
+size_t qsdp_matmul_blocks_bytes(uint64_t m, uint64_t n, uint64_t k);
+int qsdp_matmul_blocks(const uint8_t* a, const float* a_scales, uint64_t m, const uint8_t* b,
+                       const float* b_scales, int b_square, uint64_t n, uint64_t k,
+                       const float* bias, qsdp_dtype out_dtype, void* y, uint64_t y_row_stride,
+                       int accumulate, void* workspace, uint64_t workspace_bytes, void* stream);
+size_t qsdp_linear_blocks_bytes(uint64_t m, uint64_t n, uint64_t k);
+int qsdp_linear_blocks(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k, uint64_t row_stride,
+                       const uint8_t* w, const float* w_scales, uint64_t n, const float* bias,
+                       qsdp_dtype out_dtype, void* y, uint64_t y_row_stride, void* workspace,
+                       uint64_t workspace_bytes, void* stream);
+
+/*
+ * AdamW over many tensors in one launch, without quantizers around it (the tensors that the codec
+ * leaves in full precision, or a run whose step is not quantized). Per element, in binary32, with g
+ * times *grad_scale where that is given:
+ *   m <- fma(beta1, m, (1-beta1)*g);   v <- fma(beta2, v, ((1-beta2)*g)*g);
+ *   u = (m * (1/bias1)) / fma(sqrt(v), 1/sqrt(bias2), eps);   x <- fma(-lr, fma(weight_decay, x, u), x)
+ * with the tensor's weight_decay, and lr times its lr_scale. x16, where given, gets x rounded to its
+ * format. Moments are float[n] (state_bits 32) or 8-bit codes (state_bits 8), by blocks of 256 elements
+ * of the tensor with the block's largest |m| and sqrt(v), M and R, in scale (float[2 * ceil(n / 256)],
+ * {M, R} of each block):
+ *   m = M c |c| / 127^2 (int8 c),  sqrt(v) = R c^2 / 255^2 (uint8 c);  all zero: a new state
+ * The step uses the new m and v before they are rounded. With w = |m| * (127^2 / M) (or sqrt(v) *
+ * (255^2 / R)) and c = floor(sqrt(w)) the new code is c + 1 where w - c^2 > (2c + 1) t, else c; at most
+ * 127 (255), at least 1 where v > 0; with M (R) below 2^-96 it and the codes are 0. The threshold t of
+ * element i of a block is (h + 1/2) / 2^12, h the upper 12 bits of (word + i * 0x9E3779B9) mod 2^32,
+ * word 0 (for m) or 1 (for v) of the Philox block with counter (block, stream 3); block = 8 * first + the
+ * block's number in its tensor. So each rounding is right in the mean over seeds; give every step
+ * another one. A non-finite gradient makes its x non-finite and its block's moments unspecified.
+ *   table       DEVICE copy of a table that qsdp_adamw_build has completed, 8-byte aligned
+ *   pieces      what that returned
+ *   seed_dev    nullable device uint64, added to seed when the kernel starts
+ *   schedule    nullable device float[3], {lr, bias1, bias2} in the place of these arguments, read when
+ *               the kernel starts: both are for replays of a captured call
+ *   grad_scale  nullable device float; an infinity or a NaN leaves everything as it is
+ */
+typedef struct qsdp_adamw_tensor {
+    float* x;            /* in/out device float[n] */
+    const void* g;       /* device, n elements of g_dtype */
+    void* m;             /* in/out device float[n], or int8[n], 8-byte aligned */
+    void* v;             /* in/out device float[n], or uint8[n], 8-byte aligned */
+    float* scale;        /* in/out device float[2 * ceil(n / 256)], 8-byte aligned; NULL with 32 bits */
+    void* x16;           /* out, nullable device, n elements of x16_dtype (QSDP_BF16 or QSDP_F16) */
+    uint64_t n;          /* elements, 0 allowed */
+    uint64_t first;      /* written by qsdp_adamw_build: pieces of 2048 elements before this tensor */
+    float lr_scale;
+    float weight_decay;
+    int32_t g_dtype;
+    int32_t x16_dtype;
+    int32_t state_bits;  /* 8 or 32 */
+    int32_t reserved;    /* 0 */
+} qsdp_adamw_tensor;
+
+/* Host only: looks at the entries of a HOST table (alignments, formats, no overlap among what the step
+ * writes, or of that with a gradient) and writes their `first`. Returns the number of pieces, or 0 where
+ * an entry is refused or none has elements. The library does not look at the device copy. */
+uint64_t qsdp_adamw_build(qsdp_adamw_tensor* table, uint32_t count);
+int qsdp_adamw_tensors(const qsdp_adamw_tensor* table, uint32_t count, uint64_t pieces, float lr,
+                       float beta1, float beta2, float eps, float bias1, float bias2, uint64_t seed,
+                       const uint64_t* seed_dev, const float* schedule, const float* grad_scale,
+                       void* stream);
+
 #ifdef __cplusplus
 }
 #endif

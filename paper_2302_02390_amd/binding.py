@@ -107,6 +107,20 @@ _SIGNATURES = {
     "qsdp_matmul_codes": (_i32, [_vp, _vp, _vp, _u64, _vp, _vp, _u64, _u64, _i32, _vp, _i32, _vp, _u64, _vp]),
     "qsdp_linear_codes": (_i32,
         [_vp, _i32, _u64, _u64, _u64, _vp, _vp, _u64, _i32, _vp, _i32, _vp, _u64, _vp, _u64, _vp]),
+    "qsdp_layer_norm": (_i32, [_vp, _i32, _u64, _u64, _u64, _vp, _vp, _i32, _f32, _vp, _i32, _u64, _vp, _vp]),
+    "qsdp_layer_norm_backward_bytes": (C.c_size_t, [_u64, _u64]),
+    "qsdp_layer_norm_backward": (_i32,
+        [_vp, _i32, _u64, _u64, _u64, _vp, _i32, _vp, _vp, _i32, _u64, _vp, _u64, _vp, _vp, _i32, _vp, _u64, _vp]),
+    "qsdp_quantize_blocks": (_i32, [_vp, _i32, _u64, _u64, _u64, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "qsdp_matmul_blocks_bytes": (C.c_size_t, [_u64, _u64, _u64]),
+    "qsdp_matmul_blocks": (_i32,
+        [_vp, _vp, _u64, _vp, _vp, _i32, _u64, _u64, _vp, _i32, _vp, _u64, _i32, _vp, _u64, _vp]),
+    "qsdp_linear_blocks_bytes": (C.c_size_t, [_u64, _u64, _u64]),
+    "qsdp_linear_blocks": (_i32,
+        [_vp, _i32, _u64, _u64, _u64, _vp, _vp, _u64, _vp, _i32, _vp, _u64, _vp, _u64, _vp]),
+    "qsdp_adamw_build": (_u64, [_vp, _u32]),
+    "qsdp_adamw_tensors": (_i32,
+        [_vp, _u32, _u64, _f32, _f32, _f32, _f32, _f32, _f32, _u64, _vp, _vp, _vp, _vp]),
 }
 EXPORTS = tuple(_SIGNATURES)
 # Where the entry points take pointers, the stream left out.
@@ -1015,13 +1029,255 @@ def qsdp_linear_codes(x, wcodes, wmeta, n, bucket, bias, y, workspace=None):
             _bytes_of(workspace))
 
 
+# ---- operators of a training step in few bits ---------------------------------------------------------------------
+def _parameters(n, like, *tensors):
+    """The format that a norm's weight and bias share: float32 or that of `like`."""
+    kinds = {t.dtype for t in tensors if t is not None}
+    if len(kinds) > 1:
+        raise TypeError("weight and bias differ in format")
+    dtype = kinds.pop() if kinds else torch.float32
+    if dtype not in (torch.float32, like.dtype):
+        raise TypeError(f"weight and bias are float32 or {like.dtype}")
+    _per_row(n, dtype, *tensors)
+    return _DTYPES[dtype]
+
+
+def _same_shape(x, *tensors):
+    for t in tensors:
+        if t is not None and t.shape != x.shape:
+            raise ValueError(f"{tuple(t.shape)} for rows of {tuple(x.shape)}")
+
+
+def _norm_formats(x, y):
+    if x.dtype != torch.float32 and y.dtype != x.dtype:
+        raise TypeError(f"rows in {x.dtype} have outputs in {x.dtype}")
+
+
+def qsdp_layer_norm(x, weight, bias, eps, y, stats=None):
+    """x [rows, n] in float32, bfloat16 or float16; weight, bias [n] (float32 or y's format) or None; y [rows, n] in x's format,
+    or any where x is float32; stats float32[rows, 2]."""
+    dt, stride = _matrix(x)
+    out, y_stride = _matrix(y)
+    _same_shape(x, y); _norm_formats(x, y)
+    rows, n = x.shape
+    wdt = _parameters(n, y, weight, bias)
+    _per_row(2 * rows, torch.float32, stats)
+    _launch(x, "qsdp_layer_norm", x, dt, rows, n, stride, weight, bias, wdt, eps, y, out, y_stride, stats)
+
+
+def layer_norm_backward_bytes(rows, n):
+    """Bytes of workspace that qsdp_layer_norm_backward needs for the gradients of weight and bias."""
+    return int(lib().qsdp_layer_norm_backward_bytes(int(rows), int(n)))
+
+
+def qsdp_layer_norm_backward(x, weight, stats, dy, dx, dw=None, db=None, accumulate=False, workspace=None):
+    """stats as qsdp_layer_norm gave them; dy in y's format; dx (or None) in x's, which may be dy or x where they are alike; dw, db
+    float32[n] or None. Without a workspace (uint8, layer_norm_backward_bytes) one is taken from torch's allocator."""
+    dt, stride = _matrix(x)
+    dy_dt, dy_stride = _matrix(dy)
+    _same_shape(x, dy, dx); _norm_formats(x, dy)
+    rows, n = x.shape
+    dx_stride = 0
+    if dx is not None:
+        if dx.dtype != x.dtype:
+            raise TypeError(f"the gradient of rows in {x.dtype} is {dx.dtype}")
+        dx_stride = _matrix(dx)[1]
+    wdt = _parameters(n, dy, weight)
+    _per_row(2 * rows, torch.float32, stats)
+    _per_row(n, torch.float32, dw, db)
+    if workspace is None and (dw is not None or db is not None):
+        workspace = torch.empty(layer_norm_backward_bytes(rows, n), dtype=torch.uint8, device=x.device)
+    _launch(x, "qsdp_layer_norm_backward", x, dt, rows, n, stride, weight, wdt, stats, dy, dy_dt, dy_stride, dx, dx_stride, dw,
+            db, int(accumulate), workspace, _bytes_of(workspace))
+
+
+def _codes8(t, rows, cols, what):
+    """e4m3 codes of a matrix, as float8_e4m3fn or uint8: whole blocks of 128 to a row."""
+    if t.dtype not in (torch.float8_e4m3fn, torch.uint8):
+        raise TypeError(f"{what}: expected float8_e4m3fn or uint8")
+    _is(t, t.dtype)
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != -(-cols // 128) * 128:
+        raise ValueError(f"{what} is {tuple(t.shape)}, not {(rows, -(-cols // 128) * 128)}")
+
+
+def _scales8(t, blocks, rows, what):
+    _is(t, torch.float32)
+    if tuple(t.shape) != (blocks, rows):
+        raise ValueError(f"{what} is {tuple(t.shape)}, not {(blocks, rows)}")
+
+
+def alloc_blocks(rows, cols, square, device):
+    """Empty (codes, scales, codes_t, scales_t) of a matrix and its transpose for qsdp_quantize_blocks."""
+    r, c = -(-rows // 128), -(-cols // 128)
+    codes = torch.empty((rows, 128 * c), dtype=torch.float8_e4m3fn, device=device)
+    codes_t = torch.empty((cols, 128 * r), dtype=torch.float8_e4m3fn, device=device)
+    return (codes, torch.empty((c, r if square else rows), dtype=torch.float32, device=device),
+            codes_t, torch.empty((r, c if square else cols), dtype=torch.float32, device=device))
+
+
+def qsdp_quantize_blocks(x, square, codes=None, scales=None, codes_t=None, scales_t=None):
+    """x [rows, cols] to e4m3 codes (float8_e4m3fn or uint8) with a scale for 128 elements of a row, or for 128 x 128; the
+    transposed matrix's as well, in blocks along the columns of x. Shapes as alloc_blocks gives them; either pair may be None."""
+    dt, stride = _matrix(x)
+    rows, cols = x.shape
+    r, c = -(-rows // 128), -(-cols // 128)
+    if (codes is None) != (scales is None) or (codes_t is None) != (scales_t is None):
+        raise ValueError("codes and scales come together")
+    if codes is not None:
+        _codes8(codes, rows, cols, "codes")
+        _scales8(scales, c, r if square else rows, "scales")
+    if codes_t is not None:
+        _codes8(codes_t, cols, rows, "codes_t")
+        _scales8(scales_t, r, c if square else cols, "scales_t")
+    _launch(x, "qsdp_quantize_blocks", x, dt, rows, cols, stride, int(square), codes, scales, codes_t, scales_t)
+
+
+def _square(b, b_scales, n, k):
+    """Whether b [n, k] is in square blocks, by the shape of its scales."""
+    _codes8(b, n, k, "codes")
+    _is(b_scales, torch.float32)
+    blocks = -(-k // 128)
+    if tuple(b_scales.shape) == (blocks, -(-n // 128)):
+        return 1
+    _scales8(b_scales, blocks, n, "scales")
+    return 0
+
+
+def matmul_blocks_bytes(m, n, k):
+    """Bytes of workspace with which qsdp_matmul_blocks shares long sums of few tiles among workgroups."""
+    return int(lib().qsdp_matmul_blocks_bytes(int(m), int(n), int(k)))
+
+
+def _bias(bias, n):
+    if bias is not None:
+        _is(bias, torch.float32)
+        if bias.numel() != n:
+            raise ValueError(f"{bias.numel()} bias values for {n} columns")
+
+
+def qsdp_matmul_blocks(a, a_scales, b, b_scales, k, bias, y, accumulate=False, workspace=None):
+    """y [m, n] = A B^T (+ bias) (+ y) with A [m, k] in blocks of a row and B [n, k] in square blocks or blocks of a row, codes and
+    scales as qsdp_quantize_blocks gives them; y in any of the three formats; workspace uint8 or None."""
+    dt, stride = _matrix(y)
+    m, n = y.shape
+    _codes8(a, m, k, "codes")
+    _scales8(a_scales, -(-k // 128), m, "scales")
+    square = _square(b, b_scales, n, k)
+    _bias(bias, n)
+    _launch(y, "qsdp_matmul_blocks", a, a_scales, m, b, b_scales, square, n, k, bias, dt, y, stride, int(accumulate), workspace,
+            _bytes_of(workspace))
+
+
+def linear_blocks_bytes(m, n, k):
+    """Bytes of workspace that qsdp_linear_blocks needs."""
+    return int(lib().qsdp_linear_blocks_bytes(int(m), int(n), int(k)))
+
+
+def qsdp_linear_blocks(x, w, w_scales, bias, y, workspace=None):
+    """y [m, n] = x [m, k] W^T + bias, x rounded on the way, W [n, k] in square blocks. Without a workspace (uint8,
+    linear_blocks_bytes) one is taken from torch's allocator for the call."""
+    dt, stride = _matrix(x)
+    out, y_stride = _matrix(y)
+    m, k = x.shape
+    n = y.shape[1]
+    if y.shape[0] != m:
+        raise ValueError(f"y is {tuple(y.shape)} for {m} rows")
+    _codes8(w, n, k, "codes")
+    _scales8(w_scales, -(-k // 128), -(-n // 128), "scales")
+    _bias(bias, n)
+    if workspace is None:
+        workspace = torch.empty(linear_blocks_bytes(m, n, k), dtype=torch.uint8, device=x.device)
+    _launch(x, "qsdp_linear_blocks", x, dt, m, k, stride, w, w_scales, n, bias, out, y, y_stride, workspace,
+            _bytes_of(workspace))
+
+
+class AdamWTensor(C.Structure):
+    """qsdp_adamw_tensor."""
+    _fields_ = [("x", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("scale", C.c_void_p),
+                ("x16", C.c_void_p), ("n", _u64), ("first", _u64), ("lr_scale", _f32), ("weight_decay", _f32),
+                ("g_dtype", C.c_int32), ("x16_dtype", C.c_int32), ("state_bits", C.c_int32), ("reserved", C.c_int32)]
+
+
+def alloc_moments(x, bits):
+    """(m, v, scale) of a new state for the tensor x: float32 zeros and None, or 8-bit codes and their blocks' scales."""
+    n = x.numel()
+    if bits == 32:
+        return (*(torch.zeros(n, dtype=torch.float32, device=x.device) for _ in range(2)), None)
+    if bits != 8:
+        raise QsdpError(QSDP_EINVAL, "alloc_moments")
+    return (torch.zeros(n, dtype=torch.int8, device=x.device), torch.zeros(n, dtype=torch.uint8, device=x.device),
+            torch.zeros(2 * -(-n // 256), dtype=torch.float32, device=x.device))
+
+
+class AdamWTensors:
+    """The table of qsdp_adamw_tensors for lists of tensors, one entry of each per parameter: params float32, grads in any of
+    the three formats, moments and scales as alloc_moments gives them (which says how many bits they have), copies bfloat16 or
+    float16 or None. weight_decay and lr_scale: a number, or one per parameter. The table holds addresses, and this object the
+    tensors: where a gradient becomes another tensor, a new table is needed. A step writes the parameters, moments, scales and
+    copies of its table, none of which may share memory with another."""
+
+    def __init__(self, params, grads, m, v, scales=None, copies=None, weight_decay=0.0, lr_scale=1.0):
+        count = len(params)
+        each = [list(a) if isinstance(a, (list, tuple)) else [a] * count for a in (scales, copies, weight_decay, lr_scale)]
+        lists = [list(params), list(grads), list(m), list(v)] + each
+        if count == 0 or any(len(a) != count for a in lists):
+            raise ValueError("lists of one entry per parameter are needed")
+        table = (AdamWTensor * count)()
+        devices = set()
+        for t, x, g, m_, v_, scale, copy, decay, rate in zip(table, *lists):
+            _is(x, torch.float32)
+            gdt = _DTYPES.get(g.dtype)
+            if gdt is None:
+                raise TypeError("gradients are float32, bfloat16 or float16")
+            _is(g, g.dtype)
+            n, eight = x.numel(), scale is not None
+            _is(m_, torch.int8 if eight else torch.float32)
+            _is(v_, torch.uint8 if eight else torch.float32)
+            if any(o.numel() != n for o in (g, m_, v_)):
+                raise ValueError("a parameter, its gradient and its moments differ in size")
+            if eight:
+                _is(scale, torch.float32)
+                if scale.numel() != 2 * -(-n // 256):
+                    raise ValueError(f"{scale.numel()} scales for {n} elements, {2 * -(-n // 256)} are needed")
+            if copy is not None:
+                if copy.dtype not in _G16:
+                    raise TypeError("copies are float16 or bfloat16")
+                _is(copy, copy.dtype)
+                if copy.numel() != n:
+                    raise ValueError("a parameter and its copy differ in size")
+                t.x16, t.x16_dtype = copy.data_ptr(), _G16[copy.dtype]
+            t.x, t.g, t.m, t.v, t.n = x.data_ptr(), g.data_ptr(), m_.data_ptr(), v_.data_ptr(), n
+            t.scale = scale.data_ptr() if eight else None
+            t.g_dtype, t.state_bits, t.weight_decay, t.lr_scale = gdt, 8 if eight else 32, decay, rate
+            devices.update(o.device for o in (x, g, m_, v_, scale, copy) if o is not None)
+        if len(devices) != 1:
+            raise ValueError(f"tensors on {sorted(map(str, devices))}")
+        self.pieces = int(lib().qsdp_adamw_build(table, count))
+        if self.pieces == 0:
+            raise QsdpError(QSDP_EINVAL, "qsdp_adamw_build")
+        self.count, self.tensors = count, lists[:6]
+        self.device = torch.frombuffer(bytearray(table), dtype=torch.uint8).to(devices.pop())
+
+
+def qsdp_adamw_tensors(table, lr, beta1, beta2, eps, bias1, bias2, seed=0, seed_increment=None, schedule=None,
+                       grad_scale=None):
+    """One step of every tensor of an AdamWTensors. seed_increment int64[1], schedule float32[3] {lr, bias1, bias2}, grad_scale
+    float32[1], all on the GPU, or None."""
+    for t, dtype, count in ((seed_increment, torch.int64, 1), (schedule, torch.float32, 3), (grad_scale, torch.float32, 1)):
+        if t is not None:
+            _is(t, dtype)
+            _need(t, count, "a device value")
+    _launch(table.device, "qsdp_adamw_tensors", table.device, table.count, table.pieces, lr, beta1, beta2, eps, bias1, bias2,
+            seed, seed_increment, schedule, grad_scale)
+
+
 def _devices_ok(name, args, kwargs):
     """Every tensor argument of an entry point (and a segment table) must live on the same device: the
     kernel runs on the device of the first one and would fault on memory of another."""
     device = None
     for a in list(args) + list(kwargs.values()):
         for t in (a if isinstance(a, (tuple, list)) else (a,)):
-            if isinstance(t, Segments):
+            if isinstance(t, (Segments, AdamWTensors)):
                 t = t.device
             if isinstance(t, torch.Tensor):
                 if device is None:

@@ -49,6 +49,9 @@ def _units():
     units = [(f"lm_rows_{t.lower()}.o", os.path.join("lm", "lm_rows.hip"), LM_FLAGS + [f"-DQSDP_LM_FORMAT={t}"])
              for t in LM_FORMATS]
     units += [(f"{name}.o", os.path.join("lm", f"{name}.hip"), LM_FLAGS) for name in ("lm_linear", "lm_api")]
+    # the operators of a training step (csrc/train), where a NaN has to come through as well
+    units += [(f"{name}.o", os.path.join("train", f"{name}.hip"), LM_FLAGS)
+              for name in ("train_norm", "train_product", "train_adamw", "train_blocks", "train_api")]
     units.append(("qsdp_api.o", "qsdp_api.hip", []))
     for b, (g, r, w) in WAVE_SHAPES.items():
         units.append((f"qsdp_wave_{b}.o", "qsdp_wave_inst.hip",

@@ -25,7 +25,7 @@ namespace {
 // its name `_raw_stream`.
 PyObject *is_in_python, *rows_in_python, *packed_in_python, *rows_ok_in_python, *outputs_in_python, *launch_in_python,
     *devices_in_python, *names;
-PyObject *raw_stream_name, *segments_name, *device_name;
+PyObject *raw_stream_name, *segments_name, *tensors_name, *device_name;
 
 bool plain_tensor(PyObject* o) { return THPVariable_CheckExact(o); }
 
@@ -124,7 +124,9 @@ const Entry entries[] = {
     E(qsdp_fused_adamw_step_segmented), E(qsdp_fused_step_codes_segmented), E(qsdp_recv_step_segmented),
     E(qsdp_recv_adamw_step_segmented), E(qsdp_fit_levels_segmented), E(qsdp_quantize_levels_segmented),
     E(qsdp_dequantize_levels_segmented), E(qsdp_token_logprobs), E(qsdp_token_logprobs_backward), E(qsdp_distill_loss),
-    E(qsdp_distill_loss_backward), E(qsdp_quantize_tokens), E(qsdp_matmul_codes), E(qsdp_linear_codes)};
+    E(qsdp_distill_loss_backward), E(qsdp_quantize_tokens), E(qsdp_matmul_codes), E(qsdp_linear_codes),
+    E(qsdp_layer_norm), E(qsdp_layer_norm_backward), E(qsdp_quantize_blocks), E(qsdp_matmul_blocks),
+    E(qsdp_linear_blocks), E(qsdp_adamw_tensors)};
 #undef E
 
 // Call sites name their entry points by literals, which Python interns, so the object itself is compared.
@@ -253,11 +255,12 @@ bool plain_value(PyObject* o) {
     return o == Py_None || PyLong_CheckExact(o) || PyFloat_CheckExact(o) || PyBool_Check(o);
 }
 
-// Whether o is a value, or a tensor or segment table on the device of those before it (none yet: -2).
+// Whether o is a value, or a tensor or table of segments or tensors on the device of those before it (none yet: -2).
 bool same_device(PyObject* o, int& device) {
     if (plain_value(o)) return true;
     if (!plain_tensor(o)) {  // a table's tensor is its attribute `device`
-        if ((PyObject*)Py_TYPE(o) != PyDict_GetItem(names, segments_name)) return false;
+        PyObject* type = (PyObject*)Py_TYPE(o);
+        if (type != PyDict_GetItem(names, segments_name) && type != PyDict_GetItem(names, tensors_name)) return false;
         PyObject* table = PyObject_GetAttr(o, device_name);
         if (table == nullptr) PyErr_Clear();
         const bool ok = table != nullptr && plain_tensor(table) && same_device(table, device);
@@ -323,8 +326,10 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalli
 PyMODINIT_FUNC PyInit__marshal(void) {
     raw_stream_name = PyUnicode_InternFromString("_raw_stream");
     segments_name = PyUnicode_InternFromString("Segments");
+    tensors_name = PyUnicode_InternFromString("AdamWTensors");
     device_name = PyUnicode_InternFromString("device");
-    if (raw_stream_name == nullptr || segments_name == nullptr || device_name == nullptr) return nullptr;
+    if (raw_stream_name == nullptr || segments_name == nullptr || tensors_name == nullptr || device_name == nullptr)
+        return nullptr;
     for (size_t i = 0; i < kEntries; ++i) {
         entry_names[i] = PyUnicode_InternFromString(entries[i].name);
         if (entry_names[i] == nullptr) return nullptr;

@@ -1,0 +1,435 @@
+// Layer norm of rows and its gradients.
+//
+//   mu = sum x / n, r = 1 / sqrt(sum (x - mu)^2 / n + eps), h = (x - mu) r, y = h w + b
+//   g = dy w, dx = r (g - mean g - h mean(g h)), dw = sum over rows of dy h, db = sum over rows of dy
+// The variance is the mean of the centred squares, not a difference of two means, so rows far from zero keep their digits.
+#include "train_common.hpp"
+#include "train_norm.hpp"
+#include "train_plan.hpp"
+
+namespace qsdp_train {
+namespace {
+
+// Over a team of TEAM threads: every thread gets the sums. Teams of more than a wave meet in `scratch` (a word for each wave and
+// value), in the order of their waves; all teams of the workgroup come here together then.
+template <int TEAM, int N>
+__device__ __forceinline__ void team_sums(float (&v)[N], float* scratch) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = reduce64(v[i], Add());
+    if constexpr (TEAM > 64) {
+        constexpr int WAVES = TEAM / 64;
+        const int wave = threadIdx.x / 64, lead = wave / WAVES * WAVES;
+        __syncthreads();  // what was here before has been read
+        if (threadIdx.x % 64 == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) scratch[wave * N + i] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = scratch[lead * N + i];
+            for (int w = 1; w < WAVES; ++w) v[i] += scratch[(lead + w) * N + i];
+        }
+    }
+}
+
+// ---- forward -------------------------------------------------------------------------------------------------------------
+// A team keeps its row in registers between mean, variance and output: one read, one write. Weight and bias come out of the
+// caches for every row.
+template <class X, class Y, int THREADS, int TEAM, int NV>
+__global__ __launch_bounds__(THREADS) void norm_kernel(NormParams p) {
+    __shared__ float scratch[THREADS / 64];
+    const int t = threadIdx.x % TEAM;
+    const uint64_t row = p.first + (uint64_t)blockIdx.x * (THREADS / TEAM) + threadIdx.x / TEAM;
+    const bool here = row < p.rows;
+    const auto* x = static_cast<const typename X::raw*>(p.x) + (here ? row : 0) * p.x_stride;
+    Raw8<X> raw[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
+        if (here && k < p.n) raw[i].load(x, k, p.n);
+        else raw[i].none();
+    }
+    float v[NV][8], sum[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[i][e] = raw[i].at(e);
+            sum[0] += v[i][e];
+        }
+    team_sums<TEAM>(sum, scratch);
+    const float count = (float)p.n, mean = sum[0] / count;
+    sum[0] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[i][e] -= mean;
+            sum[0] = fmaf(v[i][e], k + e < p.n ? v[i][e] : 0.0f, sum[0]);
+        }
+    }
+    team_sums<TEAM>(sum, scratch);
+    const float rstd = 1.0f / sqrtf(sum[0] / count + p.eps);
+    if (!here) return;
+    if (p.stats && t == 0) {
+        p.stats[2 * row] = mean;
+        p.stats[2 * row + 1] = rstd;
+    }
+    auto* y = static_cast<typename Y::raw*>(p.y) + row * p.y_stride;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
+        if (k >= p.n) continue;
+        float w[8], b[8];
+        parameters8(p.weight, p.w_dtype, k, p.n, 1.0f, w);
+        parameters8(p.bias, p.w_dtype, k, p.n, 0.0f, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e] * rstd, w[e], b[e]);
+        store8<Y>(y, k, p.n, v[i]);
+    }
+}
+
+// Rows that no team holds: read three times.
+template <class X, class Y>
+__global__ __launch_bounds__(1024) void norm_stream_kernel(NormParams p) {
+    __shared__ float scratch[16];
+    const uint64_t row = p.first + blockIdx.x;
+    const auto* x = static_cast<const typename X::raw*>(p.x) + row * p.x_stride;
+    auto* y = static_cast<typename Y::raw*>(p.y) + row * p.y_stride;
+    const float count = (float)p.n;
+    float sum[1] = {0.0f};
+    Raw8<X> raw;
+    for (uint64_t k = (uint64_t)threadIdx.x * 8; k < p.n; k += 8192) {
+        raw.load(x, k, p.n);
+        float part = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) part += raw.at(e);
+        sum[0] += part;
+    }
+    team_sums<1024>(sum, scratch);
+    const float mean = sum[0] / count;
+    sum[0] = 0.0f;
+    for (uint64_t k = (uint64_t)threadIdx.x * 8; k < p.n; k += 8192) {
+        raw.load(x, k, p.n);
+        float part = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float d = k + e < p.n ? raw.at(e) - mean : 0.0f;
+            part = fmaf(d, d, part);
+        }
+        sum[0] += part;
+    }
+    team_sums<1024>(sum, scratch);
+    const float rstd = 1.0f / sqrtf(sum[0] / count + p.eps);
+    if (p.stats && threadIdx.x == 0) {
+        p.stats[2 * row] = mean;
+        p.stats[2 * row + 1] = rstd;
+    }
+    for (uint64_t k = (uint64_t)threadIdx.x * 8; k < p.n; k += 8192) {
+        raw.load(x, k, p.n);
+        float w[8], b[8], v[8];
+        parameters8(p.weight, p.w_dtype, k, p.n, 1.0f, w);
+        parameters8(p.bias, p.w_dtype, k, p.n, 0.0f, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = fmaf((raw.at(e) - mean) * rstd, w[e], b[e]);
+        store8<Y>(y, k, p.n, v);
+    }
+}
+
+// ---- backward ------------------------------------------------------------------------------------------------------------
+// Workgroup g takes the rows g, g + G, ... of its teams; a team holds its row of x and dy, and the sums over its rows of dy h
+// and dy for its columns, in registers. The teams' sums meet in LDS in their order, the workgroups' in a kernel after this one:
+// no atomics, so equal calls give equal bits.
+template <class X, class Y, int TEAM, int NV>
+__global__ __launch_bounds__(kNormThreads, NV <= 2 ? 4 : 2) void norm_backward_kernel(NormBackwardParams p) {
+    constexpr int TEAMS = (int)kNormThreads / TEAM;
+    __shared__ float scratch[2 * kNormThreads / 64];
+    __shared__ __attribute__((aligned(16))) float meet[TEAMS > 1 ? 2 * 8 * NV * TEAM : 1];
+    const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+    const auto* x = static_cast<const typename X::raw*>(p.x);
+    const auto* dy = static_cast<const typename Y::raw*>(p.dy);
+    float w[NV][8], dw[NV][8], db[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        parameters8(p.weight, p.w_dtype, (uint64_t)(i * TEAM + t) * 8, p.n, 1.0f, w[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.0f;
+    }
+    Raw8<X> xr[NV];
+    Raw8<Y> yr[NV];
+    float mean = 0.0f, rstd = 0.0f;
+    auto fetch = [&](uint64_t row) __attribute__((always_inline)) {
+        const bool here = row < p.rows;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
+            if (here && k < p.n) {
+                xr[i].load(x + row * p.x_stride, k, p.n);
+                yr[i].load(dy + row * p.dy_stride, k, p.n);
+            } else {
+                xr[i].none();
+                yr[i].none();
+            }
+        }
+        mean = here ? p.stats[2 * row] : 0.0f;
+        rstd = here ? p.stats[2 * row + 1] : 0.0f;
+    };
+    const uint64_t step = (uint64_t)gridDim.x * TEAMS;
+    const float inverse = 1.0f / (float)p.n;
+    fetch((uint64_t)blockIdx.x * TEAMS + team);
+    for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < p.rows; base += step) {
+        const uint64_t row = base + team;
+        float h[NV][8], d[NV][8], sums[2] = {0.0f, 0.0f};
+        const float r = rstd;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                h[i][e] = (xr[i].at(e) - mean) * r;
+                const float y = yr[i].at(e);
+                // past the row's end: dy is zero, and h only meets it
+                dw[i][e] = fmaf(y, k + e < p.n ? h[i][e] : 0.0f, dw[i][e]);
+                db[i][e] += y;
+                d[i][e] = y * w[i][e];
+                sums[0] += d[i][e];
+                sums[1] = fmaf(d[i][e], k + e < p.n ? h[i][e] : 0.0f, sums[1]);
+            }
+        }
+        fetch(row + step);
+        if (!p.dx) continue;
+        team_sums<TEAM>(sums, scratch);
+        if (row >= p.rows) continue;
+        const float c0 = sums[0] * inverse, c1 = sums[1] * inverse;
+        auto* dx = static_cast<typename X::raw*>(p.dx) + row * p.dx_stride;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
+            if (k >= p.n) continue;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[i][e] = r * (d[i][e] - fmaf(h[i][e], c1, c0));
+            store8<X>(dx, k, p.n, d[i]);
+        }
+    }
+    if (!p.partial) return;
+    if constexpr (TEAMS > 1) {
+        for (int other = 1; other < TEAMS; ++other) {
+            __syncthreads();
+            if (team == other)
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        meet[(i * 16 + e) * TEAM + t] = dw[i][e];
+                        meet[(i * 16 + 8 + e) * TEAM + t] = db[i][e];
+                    }
+            __syncthreads();
+            if (team == 0)
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        dw[i][e] += meet[(i * 16 + e) * TEAM + t];
+                        db[i][e] += meet[(i * 16 + 8 + e) * TEAM + t];
+                    }
+        }
+        if (team) return;
+    }
+    float* to = p.partial + (uint64_t)blockIdx.x * 2 * p.n;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
+        if (k >= p.n) continue;
+        store8<F32>(to, k, p.n, dw[i]);
+        store8<F32>(to + p.n, k, p.n, db[i]);
+    }
+}
+
+// Rows that no team holds: dx of a row by a workgroup, which reads it twice ...
+template <class X, class Y>
+__global__ __launch_bounds__(1024) void norm_rows_backward_kernel(NormBackwardParams p, uint64_t first) {
+    __shared__ float scratch[32];
+    const uint64_t row = first + blockIdx.x;
+    const auto* x = static_cast<const typename X::raw*>(p.x) + row * p.x_stride;
+    const auto* dy = static_cast<const typename Y::raw*>(p.dy) + row * p.dy_stride;
+    auto* dx = static_cast<typename X::raw*>(p.dx) + row * p.dx_stride;
+    const float mean = p.stats[2 * row], r = p.stats[2 * row + 1], inverse = 1.0f / (float)p.n;
+    float sums[2] = {0.0f, 0.0f};
+    Raw8<X> xr;
+    Raw8<Y> yr;
+    for (uint64_t k = (uint64_t)threadIdx.x * 8; k < p.n; k += 8192) {
+        xr.load(x, k, p.n);
+        yr.load(dy, k, p.n);
+        float w[8], part[2] = {0.0f, 0.0f};
+        parameters8(p.weight, p.w_dtype, k, p.n, 1.0f, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float g = yr.at(e) * w[e], h = k + e < p.n ? (xr.at(e) - mean) * r : 0.0f;
+            part[0] += g;
+            part[1] = fmaf(g, h, part[1]);
+        }
+        sums[0] += part[0];
+        sums[1] += part[1];
+    }
+    team_sums<1024>(sums, scratch);
+    const float c0 = sums[0] * inverse, c1 = sums[1] * inverse;
+    for (uint64_t k = (uint64_t)threadIdx.x * 8; k < p.n; k += 8192) {
+        xr.load(x, k, p.n);
+        yr.load(dy, k, p.n);
+        float w[8], d[8];
+        parameters8(p.weight, p.w_dtype, k, p.n, 1.0f, w);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = r * (yr.at(e) * w[e] - fmaf((xr.at(e) - mean) * r, c1, c0));
+        store8<X>(dx, k, p.n, d);
+    }
+}
+
+// ... and the sums of 2048 columns over a run of rows by another.
+template <class X, class Y>
+__global__ __launch_bounds__(256) void norm_columns_backward_kernel(NormBackwardParams p, uint64_t groups) {
+    const auto* x = static_cast<const typename X::raw*>(p.x);
+    const auto* dy = static_cast<const typename Y::raw*>(p.dy);
+    const uint64_t k = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (k >= p.n) return;
+    float dw[8], db[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) dw[e] = db[e] = 0.0f;
+    for (uint64_t row = blockIdx.y; row < p.rows; row += groups) {
+        Raw8<X> xr;
+        Raw8<Y> yr;
+        xr.load(x + row * p.x_stride, k, p.n);
+        yr.load(dy + row * p.dy_stride, k, p.n);
+        const float mean = p.stats[2 * row], r = p.stats[2 * row + 1];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float y = yr.at(e);
+            dw[e] = fmaf(y, k + e < p.n ? (xr.at(e) - mean) * r : 0.0f, dw[e]);
+            db[e] += y;
+        }
+    }
+    float* to = p.partial + (uint64_t)blockIdx.y * 2 * p.n;
+    store8<F32>(to, k, p.n, dw);
+    store8<F32>(to + p.n, k, p.n, db);
+}
+
+// Sums of the workgroups' partial sums: 16 columns to a workgroup, whose 16 groups of threads take every sixteenth partial.
+__global__ __launch_bounds__(256) void norm_total_kernel(const float* partial, uint64_t workgroups, uint64_t n, float* dw,
+                                                        float* db, bool accumulate) {
+    __shared__ float sums[16][17];
+    const uint64_t at = (uint64_t)blockIdx.x * 16 + threadIdx.x % 16;  // of the 2 n columns
+    const int part = threadIdx.x / 16;
+    float sum = 0.0f;
+    if (at < 2 * n)
+        for (uint64_t g = part; g < workgroups; g += 16) sum += partial[g * 2 * n + at];
+    sums[part][threadIdx.x % 16] = sum;
+    __syncthreads();
+    if (part || at >= 2 * n) return;
+    for (int i = 1; i < 16; ++i) sum += sums[i][threadIdx.x];
+    float* to = at < n ? dw : db;
+    if (!to) return;
+    to += at < n ? at : at - n;
+    *to = accumulate ? *to + sum : sum;
+}
+
+}  // namespace
+
+template <class X, class Y, int THREADS, int TEAM, int NV>
+static hipError_t launch_team(NormParams p, hipStream_t s) {
+    constexpr uint64_t EACH = THREADS / TEAM;
+    for (p.first = 0; p.first < p.rows; p.first += kMaxGrid * EACH) {
+        const uint64_t left = (p.rows - p.first + EACH - 1) / EACH;
+        hipLaunchKernelGGL((norm_kernel<X, Y, THREADS, TEAM, NV>), dim3((unsigned)(left < kMaxGrid ? left : kMaxGrid)),
+                           dim3(THREADS), 0, s, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+template <class X, class Y>
+static hipError_t launch_norm_of(NormParams p, hipStream_t s) {
+    switch (choose_norm(p.rows, p.n)) {
+        case NormTeam::W1: return launch_team<X, Y, 256, 64, 1>(p, s);
+        case NormTeam::W2: return launch_team<X, Y, 256, 64, 2>(p, s);
+        case NormTeam::W4: return launch_team<X, Y, 256, 64, 4>(p, s);
+        case NormTeam::WIDE: return launch_team<X, Y, 256, 256, 1>(p, s);
+        case NormTeam::T256: return launch_team<X, Y, 256, 256, 4>(p, s);
+        case NormTeam::T1024: return launch_team<X, Y, 1024, 1024, 4>(p, s);
+        case NormTeam::STREAM: break;
+    }
+    for (p.first = 0; p.first < p.rows; p.first += kMaxGrid) {
+        const uint64_t left = p.rows - p.first;
+        hipLaunchKernelGGL((norm_stream_kernel<X, Y>), dim3((unsigned)(left < kMaxGrid ? left : kMaxGrid)), dim3(1024), 0, s, p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+// f with null pointers to the formats of x and of y (that of x, or any for binary32).
+template <class F>
+static hipError_t by_formats(qsdp_dtype x, qsdp_dtype y, F f) {
+    if (x == QSDP_BF16) return f((BF16*)nullptr, (BF16*)nullptr);
+    if (x == QSDP_F16) return f((F16*)nullptr, (F16*)nullptr);
+    if (y == QSDP_BF16) return f((F32*)nullptr, (BF16*)nullptr);
+    if (y == QSDP_F16) return f((F32*)nullptr, (F16*)nullptr);
+    return f((F32*)nullptr, (F32*)nullptr);
+}
+
+hipError_t launch_norm(qsdp_dtype x, qsdp_dtype y, NormParams p, hipStream_t s) {
+    return by_formats(x, y, [&](auto* a, auto* b) {
+        return launch_norm_of<std::remove_pointer_t<decltype(a)>, std::remove_pointer_t<decltype(b)>>(p, s);
+    });
+}
+
+template <class X, class Y, int TEAM, int NV>
+static hipError_t launch_backward_team(const NormBackwardParams& p, hipStream_t s) {
+    hipLaunchKernelGGL((norm_backward_kernel<X, Y, TEAM, NV>), dim3((unsigned)norm_workgroups(p.rows, p.n)), dim3(kNormThreads), 0,
+                       s, p);
+    return hipGetLastError();
+}
+
+template <class X, class Y>
+static hipError_t launch_norm_backward_of(const NormBackwardParams& p, hipStream_t s) {
+    switch (choose_norm_backward(p.n)) {
+        case NormBackwardTeam::W1: return launch_backward_team<X, Y, 64, 1>(p, s);
+        case NormBackwardTeam::W2: return launch_backward_team<X, Y, 64, 2>(p, s);
+        case NormBackwardTeam::W4: return launch_backward_team<X, Y, 64, 4>(p, s);
+        case NormBackwardTeam::T256: return launch_backward_team<X, Y, 256, 4>(p, s);
+        case NormBackwardTeam::T512: return launch_backward_team<X, Y, 512, 4>(p, s);
+        case NormBackwardTeam::STREAM: break;
+    }
+    // the sums first: dx may overwrite what they read
+    if (p.partial) {
+        const uint64_t groups = norm_workgroups(p.rows, p.n);
+        hipLaunchKernelGGL((norm_columns_backward_kernel<X, Y>), dim3((unsigned)((p.n + 2047) / 2048), (unsigned)groups), dim3(256),
+                           0, s, p, groups);
+    }
+    if (p.dx)
+        for (uint64_t first = 0; first < p.rows; first += kMaxGrid) {
+            const uint64_t left = p.rows - first;
+            hipLaunchKernelGGL((norm_rows_backward_kernel<X, Y>), dim3((unsigned)(left < kMaxGrid ? left : kMaxGrid)), dim3(1024),
+                               0, s, p, first);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_backward(qsdp_dtype x, qsdp_dtype y, const NormBackwardParams& p, float* dw, float* db, bool accumulate,
+                                hipStream_t s) {
+    if (p.rows == 0) {  // sums of nothing
+        hipLaunchKernelGGL(norm_total_kernel, dim3((unsigned)((2 * p.n + 15) / 16)), dim3(256), 0, s, nullptr, 0, p.n, dw, db, false);
+        return hipGetLastError();
+    }
+    const hipError_t e = by_formats(x, y, [&](auto* a, auto* b) {
+        return launch_norm_backward_of<std::remove_pointer_t<decltype(a)>, std::remove_pointer_t<decltype(b)>>(p, s);
+    });
+    if (e != hipSuccess || !p.partial) return e;
+    hipLaunchKernelGGL(norm_total_kernel, dim3((unsigned)((2 * p.n + 15) / 16)), dim3(256), 0, s, p.partial,
+                       norm_workgroups(p.rows, p.n), p.n, dw, db, accumulate);
+    return hipGetLastError();
+}
+
+}  // namespace qsdp_train
