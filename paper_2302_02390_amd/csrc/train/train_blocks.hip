@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(BlockParams p) {
     Raw8<T> raw[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        if (r0 + i < p.rows && c0 < p.cols) raw[i].load(static_cast<const typename T::raw*>(p.x) + (r0 + i) * p.stride, c0, p.cols);
+        if (r0 + i < p.rows && c0 < p.cols) raw[i].load(static_cast<const typename T::raw*>(p.x) + (r0 + i) * p.stride + c0, (int)(p.cols - c0));
         else raw[i].none();
     }
     float by_row[8], by_col[8];

@@ -33,60 +33,88 @@ __device__ __forceinline__ void team_sums(float (&v)[N], float* scratch) {
 }
 
 // ---- forward -------------------------------------------------------------------------------------------------------------
-// A team keeps its row in registers between mean, variance and output: one read, one write. Weight and bias come out of the
-// caches for every row.
+// A team keeps its row in registers between mean, variance and output: one read, one write. It goes on to the row a grid further,
+// whose elements are on their way meanwhile; weight and bias stay in a wave's registers.
 template <class X, class Y, int THREADS, int TEAM, int NV>
 __global__ __launch_bounds__(THREADS) void norm_kernel(NormParams p) {
     __shared__ float scratch[THREADS / 64];
-    const int t = threadIdx.x % TEAM;
-    const uint64_t row = p.first + (uint64_t)blockIdx.x * (THREADS / TEAM) + threadIdx.x / TEAM;
-    const bool here = row < p.rows;
-    const auto* x = static_cast<const typename X::raw*>(p.x) + (here ? row : 0) * p.x_stride;
-    Raw8<X> raw[NV];
+    constexpr int TEAMS = THREADS / TEAM;
+    const int n = (int)p.n, t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+    Raw8<X> next[NV];
+    auto fetch = [&](uint64_t row) __attribute__((always_inline)) {
+        const auto* x = static_cast<const typename X::raw*>(p.x) + row * p.x_stride;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
-        if (here && k < p.n) raw[i].load(x, k, p.n);
-        else raw[i].none();
-    }
-    float v[NV][8], sum[1] = {0.0f};
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[i][e] = raw[i].at(e);
-            sum[0] += v[i][e];
+        for (int i = 0; i < NV; ++i) {
+            const int k = (i * TEAM + t) * 8;
+            if (row < p.rows && k < n) next[i].load(x + k, n - k);
+            else next[i].none();
         }
-    team_sums<TEAM>(sum, scratch);
-    const float count = (float)p.n, mean = sum[0] / count;
-    sum[0] = 0.0f;
+    };
+    const uint64_t step = (uint64_t)gridDim.x * TEAMS;
+    fetch((uint64_t)blockIdx.x * TEAMS + team);
+        constexpr bool KEEP = NV <= 2;  // longer rows' come out of the caches
+    float w[KEEP ? NV : 1][8], b[KEEP ? NV : 1][8];
+    if constexpr (KEEP) {
+        Parameters8 of[2][NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
+        for (int i = 0; i < NV; ++i) {
+            const int k = (i * TEAM + t) * 8;
+            of[0][i].load(p.weight, p.w_dtype, k, n - k);
+            of[1][i].load(p.bias, p.w_dtype, k, n - k);
+        }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[i][e] -= mean;
-            sum[0] = fmaf(v[i][e], k + e < p.n ? v[i][e] : 0.0f, sum[0]);
+        for (int i = 0; i < NV; ++i) {
+            of[0][i].get(p.weight, p.w_dtype, 1.0f, w[i]);
+            of[1][i].get(p.bias, p.w_dtype, 0.0f, b[i]);
         }
     }
-    team_sums<TEAM>(sum, scratch);
-    const float rstd = 1.0f / sqrtf(sum[0] / count + p.eps);
-    if (!here) return;
-    if (p.stats && t == 0) {
-        p.stats[2 * row] = mean;
-        p.stats[2 * row + 1] = rstd;
-    }
-    auto* y = static_cast<typename Y::raw*>(p.y) + row * p.y_stride;
+    const float count = (float)p.n;
+    for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < p.rows; base += step) {
+        const uint64_t row = base + team;
+        float v[NV][8], sum[1] = {0.0f};
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
-        if (k >= p.n) continue;
-        float w[8], b[8];
-        parameters8(p.weight, p.w_dtype, k, p.n, 1.0f, w);
-        parameters8(p.bias, p.w_dtype, k, p.n, 0.0f, b);
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e] * rstd, w[e], b[e]);
-        store8<Y>(y, k, p.n, v[i]);
+            for (int e = 0; e < 8; ++e) {
+                v[i][e] = next[i].at(e);
+                sum[0] += v[i][e];
+            }
+        if (base + step < p.rows) fetch(row + step);
+        team_sums<TEAM>(sum, scratch);
+        const float mean = sum[0] / count;
+        sum[0] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int k = (i * TEAM + t) * 8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[i][e] = k + e < n ? v[i][e] - mean : 0.0f;
+                sum[0] = fmaf(v[i][e], v[i][e], sum[0]);
+            }
+        }
+        team_sums<TEAM>(sum, scratch);
+        const float rstd = 1.0f / sqrtf(sum[0] / count + p.eps);
+        if (row >= p.rows) continue;
+        if (p.stats && t == 0) {
+            p.stats[2 * row] = mean;
+            p.stats[2 * row + 1] = rstd;
+        }
+        auto* y = static_cast<typename Y::raw*>(p.y) + row * p.y_stride;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int k = (i * TEAM + t) * 8;
+            if (k >= n) continue;
+            if constexpr (!KEEP) {
+                Parameters8 of[2];
+                of[0].load(p.weight, p.w_dtype, k, n - k);
+                of[1].load(p.bias, p.w_dtype, k, n - k);
+                of[0].get(p.weight, p.w_dtype, 1.0f, w[0]);
+                of[1].get(p.bias, p.w_dtype, 0.0f, b[0]);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = fmaf(v[i][e] * rstd, w[KEEP ? i : 0][e], b[KEEP ? i : 0][e]);
+            store8<Y>(y + k, n - k, v[i]);
+        }
     }
 }
 
@@ -94,14 +122,15 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(NormParams p) {
 template <class X, class Y>
 __global__ __launch_bounds__(1024) void norm_stream_kernel(NormParams p) {
     __shared__ float scratch[16];
+    const int n = (int)p.n;
     const uint64_t row = p.first + blockIdx.x;
     const auto* x = static_cast<const typename X::raw*>(p.x) + row * p.x_stride;
     auto* y = static_cast<typename Y::raw*>(p.y) + row * p.y_stride;
     const float count = (float)p.n;
     float sum[1] = {0.0f};
     Raw8<X> raw;
-    for (uint64_t k = (uint64_t)threadIdx.x * 8; k < p.n; k += 8192) {
-        raw.load(x, k, p.n);
+    for (int k = (int)threadIdx.x * 8; k < n; k += 8192) {
+        raw.load(x + k, n - k);
         float part = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) part += raw.at(e);
@@ -110,12 +139,12 @@ __global__ __launch_bounds__(1024) void norm_stream_kernel(NormParams p) {
     team_sums<1024>(sum, scratch);
     const float mean = sum[0] / count;
     sum[0] = 0.0f;
-    for (uint64_t k = (uint64_t)threadIdx.x * 8; k < p.n; k += 8192) {
-        raw.load(x, k, p.n);
+    for (int k = (int)threadIdx.x * 8; k < n; k += 8192) {
+        raw.load(x + k, n - k);
         float part = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float d = k + e < p.n ? raw.at(e) - mean : 0.0f;
+            const float d = k + e < n ? raw.at(e) - mean : 0.0f;
             part = fmaf(d, d, part);
         }
         sum[0] += part;
@@ -126,14 +155,17 @@ __global__ __launch_bounds__(1024) void norm_stream_kernel(NormParams p) {
         p.stats[2 * row] = mean;
         p.stats[2 * row + 1] = rstd;
     }
-    for (uint64_t k = (uint64_t)threadIdx.x * 8; k < p.n; k += 8192) {
-        raw.load(x, k, p.n);
+    for (int k = (int)threadIdx.x * 8; k < n; k += 8192) {
+        raw.load(x + k, n - k);
         float w[8], b[8], v[8];
-        parameters8(p.weight, p.w_dtype, k, p.n, 1.0f, w);
-        parameters8(p.bias, p.w_dtype, k, p.n, 0.0f, b);
+        Parameters8 of[2];
+        of[0].load(p.weight, p.w_dtype, k, n - k);
+        of[1].load(p.bias, p.w_dtype, k, n - k);
+        of[0].get(p.weight, p.w_dtype, 1.0f, w);
+        of[1].get(p.bias, p.w_dtype, 0.0f, b);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = fmaf((raw.at(e) - mean) * rstd, w[e], b[e]);
-        store8<Y>(y, k, p.n, v);
+        store8<Y>(y + k, n - k, v);
     }
 }
 
@@ -142,62 +174,76 @@ __global__ __launch_bounds__(1024) void norm_stream_kernel(NormParams p) {
 // and dy for its columns, in registers. The teams' sums meet in LDS in their order, the workgroups' in a kernel after this one:
 // no atomics, so equal calls give equal bits.
 template <class X, class Y, int TEAM, int NV>
-__global__ __launch_bounds__(kNormThreads, NV <= 2 ? 4 : 2) void norm_backward_kernel(NormBackwardParams p) {
-    constexpr int TEAMS = (int)kNormThreads / TEAM;
+__global__ __launch_bounds__(kNormThreads, 4) void norm_backward_kernel(NormBackwardParams p) {
+    constexpr int TEAMS = kNormThreads / TEAM;
     __shared__ float scratch[2 * kNormThreads / 64];
     __shared__ __attribute__((aligned(16))) float meet[TEAMS > 1 ? 2 * 8 * NV * TEAM : 1];
-    const int t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
+    const int n = (int)p.n, t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
     const auto* x = static_cast<const typename X::raw*>(p.x);
     const auto* dy = static_cast<const typename Y::raw*>(p.dy);
-    float w[NV][8], dw[NV][8], db[NV][8];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        parameters8(p.weight, p.w_dtype, (uint64_t)(i * TEAM + t) * 8, p.n, 1.0f, w[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.0f;
-    }
-    Raw8<X> xr[NV];
-    Raw8<Y> yr[NV];
-    float mean = 0.0f, rstd = 0.0f;
+    Raw8<X> x_next[NV];
+    Raw8<Y> y_next[NV];
+    float mean_next = 0.0f, rstd_next = 0.0f;
     auto fetch = [&](uint64_t row) __attribute__((always_inline)) {
         const bool here = row < p.rows;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
-            if (here && k < p.n) {
-                xr[i].load(x + row * p.x_stride, k, p.n);
-                yr[i].load(dy + row * p.dy_stride, k, p.n);
+            const int k = (i * TEAM + t) * 8;
+            if (here && k < n) {
+                x_next[i].load(x + row * p.x_stride + k, n - k);
+                y_next[i].load(dy + row * p.dy_stride + k, n - k);
             } else {
-                xr[i].none();
-                yr[i].none();
+                x_next[i].none();
+                y_next[i].none();
             }
         }
-        mean = here ? p.stats[2 * row] : 0.0f;
-        rstd = here ? p.stats[2 * row + 1] : 0.0f;
+        mean_next = here ? p.stats[2 * row] : 0.0f;
+        rstd_next = here ? p.stats[2 * row + 1] : 0.0f;
     };
     const uint64_t step = (uint64_t)gridDim.x * TEAMS;
     const float inverse = 1.0f / (float)p.n;
     fetch((uint64_t)blockIdx.x * TEAMS + team);
+    // the weight, as all teams take it, in LDS: in registers it would be a quarter of what a lane has
+    __shared__ __attribute__((aligned(16))) f32x4 weight[NV][2][TEAM];
+    float dw[NV][8], db[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        if (team == 0) {
+            float w[8];
+            Parameters8 of;
+            of.load(p.weight, p.w_dtype, (i * TEAM + t) * 8, n - (i * TEAM + t) * 8);
+            of.get(p.weight, p.w_dtype, 1.0f, w);
+            weight[i][0][t] = f32x4{w[0], w[1], w[2], w[3]};
+            weight[i][1][t] = f32x4{w[4], w[5], w[6], w[7]};
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw[i][e] = db[i][e] = 0.0f;
+    }
+    __syncthreads();
     for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < p.rows; base += step) {
         const uint64_t row = base + team;
-        float h[NV][8], d[NV][8], sums[2] = {0.0f, 0.0f};
-        const float r = rstd;
+        Raw8<X> xr[NV];
+        Raw8<Y> yr[NV];
+        const float mean = mean_next, r = rstd_next;
+        asm volatile("" ::: "memory");  // the weight is read anew
+        float sums[2] = {0.0f, 0.0f};
+        // h of an element; past the row's end it meets a dy of zero
+        auto centred = [&](int i, int e) __attribute__((always_inline)) { return (xr[i].at(e) - mean) * r; };
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
+            xr[i] = x_next[i];
+            yr[i] = y_next[i];
+            const f32x4 w[2] = {weight[i][0][t], weight[i][1][t]};
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                h[i][e] = (xr[i].at(e) - mean) * r;
-                const float y = yr[i].at(e);
-                // past the row's end: dy is zero, and h only meets it
-                dw[i][e] = fmaf(y, k + e < p.n ? h[i][e] : 0.0f, dw[i][e]);
+                const float h = centred(i, e), y = yr[i].at(e), g = y * w[e / 4][e % 4];
+                dw[i][e] = fmaf(y, h, dw[i][e]);
                 db[i][e] += y;
-                d[i][e] = y * w[i][e];
-                sums[0] += d[i][e];
-                sums[1] = fmaf(d[i][e], k + e < p.n ? h[i][e] : 0.0f, sums[1]);
+                sums[0] += g;
+                sums[1] = fmaf(g, h, sums[1]);
             }
         }
-        fetch(row + step);
+        if (base + step < p.rows) fetch(row + step);
         if (!p.dx) continue;
         team_sums<TEAM>(sums, scratch);
         if (row >= p.rows) continue;
@@ -205,11 +251,15 @@ __global__ __launch_bounds__(kNormThreads, NV <= 2 ? 4 : 2) void norm_backward_k
         auto* dx = static_cast<typename X::raw*>(p.dx) + row * p.dx_stride;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
-            if (k >= p.n) continue;
+            const int k = (i * TEAM + t) * 8;
+            if (k >= n) continue;
+            xr[i].again();  // what is computed of it a second time takes fewer registers than what would be kept
+            yr[i].again();
+            const f32x4 w[2] = {weight[i][0][t], weight[i][1][t]};
+            float d[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) d[i][e] = r * (d[i][e] - fmaf(h[i][e], c1, c0));
-            store8<X>(dx, k, p.n, d[i]);
+            for (int e = 0; e < 8; ++e) d[e] = r * (yr[i].at(e) * w[e / 4][e % 4] - fmaf(centred(i, e), c1, c0));
+            store8<X>(dx + k, n - k, d);
         }
     }
     if (!p.partial) return;
@@ -239,10 +289,10 @@ __global__ __launch_bounds__(kNormThreads, NV <= 2 ? 4 : 2) void norm_backward_k
     float* to = p.partial + (uint64_t)blockIdx.x * 2 * p.n;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const uint64_t k = (uint64_t)(i * TEAM + t) * 8;
-        if (k >= p.n) continue;
-        store8<F32>(to, k, p.n, dw[i]);
-        store8<F32>(to + p.n, k, p.n, db[i]);
+        const int k = (i * TEAM + t) * 8;
+        if (k >= n) continue;
+        store8<F32>(to + k, n - k, dw[i]);
+        store8<F32>(to + p.n + k, n - k, db[i]);
     }
 }
 
@@ -250,6 +300,7 @@ __global__ __launch_bounds__(kNormThreads, NV <= 2 ? 4 : 2) void norm_backward_k
 template <class X, class Y>
 __global__ __launch_bounds__(1024) void norm_rows_backward_kernel(NormBackwardParams p, uint64_t first) {
     __shared__ float scratch[32];
+    const int n = (int)p.n;
     const uint64_t row = first + blockIdx.x;
     const auto* x = static_cast<const typename X::raw*>(p.x) + row * p.x_stride;
     const auto* dy = static_cast<const typename Y::raw*>(p.dy) + row * p.dy_stride;
@@ -258,14 +309,16 @@ __global__ __launch_bounds__(1024) void norm_rows_backward_kernel(NormBackwardPa
     float sums[2] = {0.0f, 0.0f};
     Raw8<X> xr;
     Raw8<Y> yr;
-    for (uint64_t k = (uint64_t)threadIdx.x * 8; k < p.n; k += 8192) {
-        xr.load(x, k, p.n);
-        yr.load(dy, k, p.n);
+    for (int k = (int)threadIdx.x * 8; k < n; k += 8192) {
+        xr.load(x + k, n - k);
+        yr.load(dy + k, n - k);
         float w[8], part[2] = {0.0f, 0.0f};
-        parameters8(p.weight, p.w_dtype, k, p.n, 1.0f, w);
+        Parameters8 of;
+        of.load(p.weight, p.w_dtype, k, n - k);
+        of.get(p.weight, p.w_dtype, 1.0f, w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float g = yr.at(e) * w[e], h = k + e < p.n ? (xr.at(e) - mean) * r : 0.0f;
+            const float g = yr.at(e) * w[e], h = k + e < n ? (xr.at(e) - mean) * r : 0.0f;
             part[0] += g;
             part[1] = fmaf(g, h, part[1]);
         }
@@ -274,14 +327,16 @@ __global__ __launch_bounds__(1024) void norm_rows_backward_kernel(NormBackwardPa
     }
     team_sums<1024>(sums, scratch);
     const float c0 = sums[0] * inverse, c1 = sums[1] * inverse;
-    for (uint64_t k = (uint64_t)threadIdx.x * 8; k < p.n; k += 8192) {
-        xr.load(x, k, p.n);
-        yr.load(dy, k, p.n);
+    for (int k = (int)threadIdx.x * 8; k < n; k += 8192) {
+        xr.load(x + k, n - k);
+        yr.load(dy + k, n - k);
         float w[8], d[8];
-        parameters8(p.weight, p.w_dtype, k, p.n, 1.0f, w);
+        Parameters8 of;
+        of.load(p.weight, p.w_dtype, k, n - k);
+        of.get(p.weight, p.w_dtype, 1.0f, w);
 #pragma unroll
         for (int e = 0; e < 8; ++e) d[e] = r * (yr.at(e) * w[e] - fmaf((xr.at(e) - mean) * r, c1, c0));
-        store8<X>(dx, k, p.n, d);
+        store8<X>(dx + k, n - k, d);
     }
 }
 
@@ -290,38 +345,46 @@ template <class X, class Y>
 __global__ __launch_bounds__(256) void norm_columns_backward_kernel(NormBackwardParams p, uint64_t groups) {
     const auto* x = static_cast<const typename X::raw*>(p.x);
     const auto* dy = static_cast<const typename Y::raw*>(p.dy);
-    const uint64_t k = ((uint64_t)blockIdx.x * 256 + threadIdx.x) * 8;
-    if (k >= p.n) return;
+    const int n = (int)p.n, k = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 8;
+    if (k >= n) return;
     float dw[8], db[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[e] = db[e] = 0.0f;
     for (uint64_t row = blockIdx.y; row < p.rows; row += groups) {
         Raw8<X> xr;
         Raw8<Y> yr;
-        xr.load(x + row * p.x_stride, k, p.n);
-        yr.load(dy + row * p.dy_stride, k, p.n);
+        xr.load(x + row * p.x_stride + k, n - k);
+        yr.load(dy + row * p.dy_stride + k, n - k);
         const float mean = p.stats[2 * row], r = p.stats[2 * row + 1];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float y = yr.at(e);
-            dw[e] = fmaf(y, k + e < p.n ? (xr.at(e) - mean) * r : 0.0f, dw[e]);
+            dw[e] = fmaf(y, k + e < n ? (xr.at(e) - mean) * r : 0.0f, dw[e]);
             db[e] += y;
         }
     }
     float* to = p.partial + (uint64_t)blockIdx.y * 2 * p.n;
-    store8<F32>(to, k, p.n, dw);
-    store8<F32>(to + p.n, k, p.n, db);
+    store8<F32>(to + k, n - k, dw);
+    store8<F32>(to + p.n + k, n - k, db);
 }
 
-// Sums of the workgroups' partial sums: 16 columns to a workgroup, whose 16 groups of threads take every sixteenth partial.
+// Sums of the workgroups' partial sums: 16 columns to a workgroup, whose 16 groups of threads take every sixteenth partial, eight of
+// them on their way at a time.
 __global__ __launch_bounds__(256) void norm_total_kernel(const float* partial, uint64_t workgroups, uint64_t n, float* dw,
                                                         float* db, bool accumulate) {
     __shared__ float sums[16][17];
     const uint64_t at = (uint64_t)blockIdx.x * 16 + threadIdx.x % 16;  // of the 2 n columns
     const int part = threadIdx.x / 16;
     float sum = 0.0f;
-    if (at < 2 * n)
-        for (uint64_t g = part; g < workgroups; g += 16) sum += partial[g * 2 * n + at];
+    if (at < 2 * n) {
+        for (uint64_t g = part; g < workgroups; g += 16 * 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = g + i * 16 < workgroups ? partial[(g + i * 16) * 2 * n + at] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i];
+        }
+    }
     sums[part][threadIdx.x % 16] = sum;
     __syncthreads();
     if (part || at >= 2 * n) return;
@@ -335,27 +398,24 @@ __global__ __launch_bounds__(256) void norm_total_kernel(const float* partial, u
 }  // namespace
 
 template <class X, class Y, int THREADS, int TEAM, int NV>
-static hipError_t launch_team(NormParams p, hipStream_t s) {
-    constexpr uint64_t EACH = THREADS / TEAM;
-    for (p.first = 0; p.first < p.rows; p.first += kMaxGrid * EACH) {
-        const uint64_t left = (p.rows - p.first + EACH - 1) / EACH;
-        hipLaunchKernelGGL((norm_kernel<X, Y, THREADS, TEAM, NV>), dim3((unsigned)(left < kMaxGrid ? left : kMaxGrid)),
-                           dim3(THREADS), 0, s, p);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+static hipError_t launch_team(const NormParams& p, hipStream_t s) {
+    constexpr uint64_t EACH = THREADS / TEAM, MOST = 256 * (1024 / THREADS);  // 16 waves to a compute unit
+    const uint64_t need = (p.rows + EACH - 1) / EACH;
+    hipLaunchKernelGGL((norm_kernel<X, Y, THREADS, TEAM, NV>), dim3((unsigned)(need < MOST ? need : MOST)), dim3(THREADS), 0, s, p);
+    return hipGetLastError();
 }
 
 template <class X, class Y>
 static hipError_t launch_norm_of(NormParams p, hipStream_t s) {
     switch (choose_norm(p.rows, p.n)) {
-        case NormTeam::W1: return launch_team<X, Y, 256, 64, 1>(p, s);
-        case NormTeam::W2: return launch_team<X, Y, 256, 64, 2>(p, s);
-        case NormTeam::W4: return launch_team<X, Y, 256, 64, 4>(p, s);
-        case NormTeam::WIDE: return launch_team<X, Y, 256, 256, 1>(p, s);
-        case NormTeam::T256: return launch_team<X, Y, 256, 256, 4>(p, s);
-        case NormTeam::T1024: return launch_team<X, Y, 1024, 1024, 4>(p, s);
+        case NormTeam::T64: return launch_team<X, Y, 256, 64, 1>(p, s);
+        case NormTeam::T64_2: return launch_team<X, Y, 512, 64, 2>(p, s);
+        case NormTeam::T128_2: return launch_team<X, Y, 512, 128, 2>(p, s);
+        case NormTeam::T256_2: return launch_team<X, Y, 512, 256, 2>(p, s);
+        case NormTeam::T512_2: return launch_team<X, Y, 512, 512, 2>(p, s);
+        case NormTeam::T1024_2: return launch_team<X, Y, 1024, 1024, 2>(p, s);
+        case NormTeam::T1024_4: return launch_team<X, Y, 1024, 1024, 4>(p, s);
+        case NormTeam::SHORT: return launch_team<X, Y, 256, 256, 1>(p, s);
         case NormTeam::STREAM: break;
     }
     for (p.first = 0; p.first < p.rows; p.first += kMaxGrid) {
@@ -393,11 +453,12 @@ static hipError_t launch_backward_team(const NormBackwardParams& p, hipStream_t 
 template <class X, class Y>
 static hipError_t launch_norm_backward_of(const NormBackwardParams& p, hipStream_t s) {
     switch (choose_norm_backward(p.n)) {
-        case NormBackwardTeam::W1: return launch_backward_team<X, Y, 64, 1>(p, s);
-        case NormBackwardTeam::W2: return launch_backward_team<X, Y, 64, 2>(p, s);
-        case NormBackwardTeam::W4: return launch_backward_team<X, Y, 64, 4>(p, s);
-        case NormBackwardTeam::T256: return launch_backward_team<X, Y, 256, 4>(p, s);
-        case NormBackwardTeam::T512: return launch_backward_team<X, Y, 512, 4>(p, s);
+        case NormBackwardTeam::T64: return launch_backward_team<X, Y, 64, 1>(p, s);
+        case NormBackwardTeam::T128: return launch_backward_team<X, Y, 128, 1>(p, s);
+        case NormBackwardTeam::T256: return launch_backward_team<X, Y, 256, 1>(p, s);
+        case NormBackwardTeam::T512: return launch_backward_team<X, Y, 512, 1>(p, s);
+        case NormBackwardTeam::T1024: return launch_backward_team<X, Y, 1024, 1>(p, s);
+        case NormBackwardTeam::T1024_2: return launch_backward_team<X, Y, 1024, 2>(p, s);
         case NormBackwardTeam::STREAM: break;
     }
     // the sums first: dx may overwrite what they read

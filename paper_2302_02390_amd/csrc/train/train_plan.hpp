@@ -5,47 +5,52 @@
 namespace qsdp_train {
 
 // ---- layer norm (train_norm.hip) -----------------------------------------------------------------------------------------
-// Threads to a row, and groups of eight elements to a thread: a wave to a row as long as it holds one, as it then waits for
-// nobody. WIDE: few short rows among four waves each, as nothing else fills the chip. STREAM: row read again for each use.
-enum class NormTeam { W1, W2, W4, WIDE, T256, T1024, STREAM };
+// Threads to a row, the fewest that hold it with 8 elements each (backward, which also holds its columns' sums) or 16 (forward).
+// A wave to a row waits for nobody. SHORT: few rows of up to 2048 by four waves each, as nothing else fills the chip.
+// STREAM: rows that no team holds, read again for each use.
+enum class NormTeam { T64, T64_2, T128_2, T256_2, T512_2, T1024_2, T1024_4, SHORT, STREAM };
 
 constexpr NormTeam choose_norm(uint64_t rows, uint64_t n) {
-    if (n <= 512) return NormTeam::W1;
-    if (n <= 2048 && rows <= 1024) return NormTeam::WIDE;
-    if (n <= 1024) return NormTeam::W2;
-    if (n <= 2048) return NormTeam::W4;
-    if (n <= 8192) return NormTeam::T256;
-    if (n <= 32768) return NormTeam::T1024;
+    if (n <= 512) return NormTeam::T64;
+    if (n <= 2048 && rows <= 1024) return NormTeam::SHORT;
+    if (n <= 1024) return NormTeam::T64_2;
+    if (n <= 2048) return NormTeam::T128_2;
+    if (n <= 4096) return NormTeam::T256_2;
+    if (n <= 8192) return NormTeam::T512_2;
+    if (n <= 16384) return NormTeam::T1024_2;
+    if (n <= 32768) return NormTeam::T1024_4;
     return NormTeam::STREAM;
 }
 
-enum class NormBackwardTeam { W1, W2, W4, T256, T512, STREAM };
+enum class NormBackwardTeam { T64, T128, T256, T512, T1024, T1024_2, STREAM };
 
 constexpr NormBackwardTeam choose_norm_backward(uint64_t n) {
-    if (n <= 512) return NormBackwardTeam::W1;
-    if (n <= 1024) return NormBackwardTeam::W2;
-    if (n <= 2048) return NormBackwardTeam::W4;
-    if (n <= 8192) return NormBackwardTeam::T256;
-    if (n <= 16384) return NormBackwardTeam::T512;
+    if (n <= 512) return NormBackwardTeam::T64;
+    if (n <= 1024) return NormBackwardTeam::T128;
+    if (n <= 2048) return NormBackwardTeam::T256;
+    if (n <= 4096) return NormBackwardTeam::T512;
+    if (n <= 8192) return NormBackwardTeam::T1024;
+    if (n <= 16384) return NormBackwardTeam::T1024_2;
     return NormBackwardTeam::STREAM;
 }
 
-constexpr uint64_t kNormThreads = 512;  // of a backward workgroup
-
-// Rows that a backward workgroup has at once.
+// Threads of a backward workgroup, and the rows that it has at once.
+constexpr int kNormThreads = 1024;
 constexpr uint64_t norm_rows_at_once(uint64_t n) {
     switch (choose_norm_backward(n)) {
-        case NormBackwardTeam::W1: case NormBackwardTeam::W2: case NormBackwardTeam::W4: return kNormThreads / 64;
+        case NormBackwardTeam::T64: return kNormThreads / 64;
+        case NormBackwardTeam::T128: return kNormThreads / 128;
         case NormBackwardTeam::T256: return kNormThreads / 256;
+        case NormBackwardTeam::T512: return kNormThreads / 512;
         default: return 1;
     }
 }
 
-// Workgroups of the backward pass, each of which leaves one partial sum for the weight and one for the bias: one to a compute
-// unit, and two where registers let two run. (Rows that no team holds: runs of rows, for every 2048 columns.)
+// Workgroups of the backward pass, each of which leaves one partial sum for the weight and one for the bias: what the chip runs
+// at once. (Rows that no team holds: runs of rows, for every 2048 columns.)
 constexpr uint64_t norm_workgroups(uint64_t rows, uint64_t n) {
     const uint64_t at_once = norm_rows_at_once(n), need = (rows + at_once - 1) / at_once;
-    const uint64_t most = n <= 1024 ? 512 : n <= 16384 ? 256 : 32;
+    const uint64_t most = n <= 16384 ? 256 : 32;
     return need < most ? need : most;
 }
 
