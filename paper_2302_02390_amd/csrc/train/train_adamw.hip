@@ -28,80 +28,105 @@ struct Step {
         m = fmaf(beta1, m, rest1 * g);
         v = fmaf(beta2, v, (rest2 * g) * g);
     }
+    // the quotient to two units in the last place, of an update that is itself small beside x
     __device__ __forceinline__ float weight(float x, float m, float root) const {
-        const float u = (m * inverse1) / fmaf(root, inverse2, eps);
+        const float u = (m * inverse1) * __builtin_amdgcn_rcpf(fmaf(root, inverse2, eps));
         return fmaf(-lr, fmaf(decay, x, u), x);
     }
 };
 
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// Four consecutive elements, zeros past the tensor's end; and back.
+template <class T>
+__device__ __forceinline__ void load4(const void* p, uint64_t at, uint64_t n, float* v) {
+    typedef typename T::raw raw;
+    typedef raw anywhere __attribute__((ext_vector_type(4), aligned(sizeof(raw))));
+    const raw* from = static_cast<const raw*>(p) + at;
+    if (at + 4 <= n) {
+        const anywhere four = __builtin_nontemporal_load(reinterpret_cast<const anywhere*>(from));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = T::get(four[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = at + e < n ? T::get(from[e]) : 0.0f;
+    }
+}
+template <class T>
+__device__ __forceinline__ void store4(void* p, uint64_t at, uint64_t n, const float* v) {
+    typedef typename T::raw raw;
+    typedef raw anywhere __attribute__((ext_vector_type(4), aligned(sizeof(raw))));
+    raw* to = static_cast<raw*>(p) + at;
+    if (at + 4 <= n) {
+        if constexpr (sizeof(raw) == 4) {
+            __builtin_nontemporal_store(anywhere{v[0], v[1], v[2], v[3]}, reinterpret_cast<anywhere*>(to));
+        } else {
+            typedef uint32_t two __attribute__((ext_vector_type(2), aligned(2)));
+            __builtin_nontemporal_store(two{T::two(v[0], v[1]), T::two(v[2], v[3])}, reinterpret_cast<two*>(to));
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (at + e < n) to[e] = T::put(v[e]);
+    }
+}
 
-// Over the 32 lanes that share a block: all get the largest.
-__device__ __forceinline__ float largest32(float v) {
-    v = reduce16(v, Max());
-    const uint32_t u = __builtin_bit_cast(uint32_t, v);
-    const auto rows = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)rows[0]), __builtin_bit_cast(float, (uint32_t)rows[1]));
+// The root to nearest of numbers from 2^-96 on, in a third of the instructions that all numbers take: Newton's step for both the
+// root and half its reciprocal, and the rest of the square (Markstein).
+__device__ __forceinline__ float root_of(float v) {
+    const float y = __builtin_amdgcn_rsqf(v), s = v * y, h = 0.5f * y, e = fmaf(-h, s, 0.5f);
+    const float s1 = fmaf(s, e, s);
+    return fmaf(fmaf(-s1, s1, v), fmaf(h, e, h), s1);
 }
 
 // The code of a value that is not negative, `scaled` in units of the code's square; word: the upper 12 bits are the threshold.
-__device__ __forceinline__ float code_of(float scaled, uint32_t word, float most) {
+__device__ __forceinline__ float code_of(float scaled, uint32_t word) {
     const float c = floorf(__builtin_amdgcn_sqrtf(scaled));
     const float t = fmaf((float)(word >> 20), 0x1p-12f, 0x1p-13f);
-    const float up = scaled - c * c > fmaf(2.0f, c, 1.0f) * t ? c + 1.0f : c;
-    return fminf(up, most);
+    return fmaf(fmaf(2.0f, c, 1.0f), -t, scaled - c * c) > 0.0f ? c + 1.0f : c;  // all exact but the last rounding, which keeps the sign
 }
 
-__device__ __forceinline__ void gradients(const qsdp_adamw_tensor& t, uint64_t at, uint64_t n, float* g) {
-    if (t.g_dtype == QSDP_F32) {
-        Raw8<F32> raw;
-        raw.load(static_cast<const float*>(t.g), at, n);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = raw.at(e);
-    } else if (t.g_dtype == QSDP_BF16) {
-        Raw8<BF16> raw;
-        raw.load(static_cast<const uint16_t*>(t.g), at, n);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = raw.at(e);
-    } else {
-        Raw8<F16> raw;
-        raw.load(static_cast<const _Float16*>(t.g), at, n);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = raw.at(e);
-    }
+// The largest over the wave of four values: in the lanes of row q (of 16), that of value q. Halves and rows change places between two
+// registers at a time, so that both are reduced by the same instructions.
+__device__ __forceinline__ float largest_of_four(float a, float b, float c, float d) {
+    auto halves = [](float u, float v) __attribute__((always_inline)) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(u), __float_as_uint(v), false, false);
+        return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+    };
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(halves(a, c)), __float_as_uint(halves(b, d)), false, false);
+    return reduce16(fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])), Max());
 }
 
-__device__ __forceinline__ void floats(const void* p, uint64_t at, uint64_t n, float* v) {
-    Raw8<F32> raw;
-    raw.load(static_cast<const float*>(p), at, n);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = raw.at(e);
+__device__ __forceinline__ void gradients(const qsdp_adamw_tensor& t, uint64_t at, float* g) {
+    if (t.g_dtype == QSDP_F32) load4<F32>(t.g, at, t.n, g);
+    else if (t.g_dtype == QSDP_BF16) load4<BF16>(t.g, at, t.n, g);
+    else load4<F16>(t.g, at, t.n, g);
 }
 
 __device__ __forceinline__ void put_weights(const qsdp_adamw_tensor& t, uint64_t at, const float* x) {
-    store8<F32>(t.x, at, t.n, x);
+    store4<F32>(t.x, at, t.n, x);
     if (t.x16) {
-        if (t.x16_dtype == QSDP_BF16) store8<BF16>(static_cast<uint16_t*>(t.x16), at, t.n, x);
-        else store8<F16>(static_cast<_Float16*>(t.x16), at, t.n, x);
+        if (t.x16_dtype == QSDP_BF16) store4<BF16>(t.x16, at, t.n, x);
+        else store4<F16>(t.x16, at, t.n, x);
     }
 }
 
-// Eight codes, those past the tensor's end zero and left as they are.
-__device__ __forceinline__ u32x2 load_codes(const uint8_t* p, uint64_t at, uint64_t n) {
-    if (at + 8 <= n) return __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p + at));
-    u32x2 v = {0, 0};
+// Four codes, zeros past the tensor's end; and back, what lies behind left as it is.
+__device__ __forceinline__ uint32_t load_codes(const void* p, uint64_t at, uint64_t n) {
+    const uint8_t* from = static_cast<const uint8_t*>(p) + at;
+    if (at + 4 <= n) return __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(from));
+    uint32_t v = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (at + e < n) v[e / 4] |= (uint32_t)p[at + e] << (e % 4 * 8);
+    for (int e = 0; e < 4; ++e)
+        if (at + e < n) v |= (uint32_t)from[e] << (e * 8);
     return v;
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, uint64_t at, uint64_t n, u32x2 v) {
-    if (at + 8 <= n) {
-        __builtin_nontemporal_store(v, reinterpret_cast<u32x2*>(p + at));
+__device__ __forceinline__ void store_codes(void* p, uint64_t at, uint64_t n, uint32_t v) {
+    uint8_t* to = static_cast<uint8_t*>(p) + at;
+    if (at + 4 <= n) {
+        __builtin_nontemporal_store(v, reinterpret_cast<uint32_t*>(to));
     } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (at + e < n) p[at + e] = (uint8_t)(v[e / 4] >> (e % 4 * 8));
+        for (int e = 0; e < 4; ++e)
+            if (at + e < n) to[e] = (uint8_t)(v >> (e * 8));
     }
 }
 
@@ -119,12 +144,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamWParams p) {
     }
     const qsdp_adamw_tensor t = p.table[__builtin_amdgcn_readfirstlane(low)];
     Step s;
-    float bias1 = p.bias1, bias2 = p.bias2, scale = 1.0f;
+    float scale = 1.0f;
     s.lr = p.lr;
+    s.inverse1 = p.inverse1;
+    s.inverse2 = p.inverse2;
     if (p.schedule) {
         s.lr = p.schedule[0];
-        bias1 = p.schedule[1];
-        bias2 = p.schedule[2];
+        s.inverse1 = 1.0f / p.schedule[1];
+        s.inverse2 = 1.0f / sqrtf(p.schedule[2]);
     }
     if (p.grad_scale) {
         scale = *p.grad_scale;
@@ -136,91 +163,106 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamWParams p) {
     s.rest1 = 1.0f - p.beta1;
     s.rest2 = 1.0f - p.beta2;
     s.eps = p.eps;
-    s.inverse1 = 1.0f / bias1;
-    s.inverse2 = 1.0f / sqrtf(bias2);
     s.decay = t.weight_decay;
-    const uint64_t local = piece - t.first, at = local * kPiece + threadIdx.x * 8;
-    const bool some = at < t.n;
-    float x[8], g[8];
-    if (t.state_bits == 32) {
-        if (!some) return;
-        float m[8], v[8];
-        floats(t.x, at, t.n, x);
-        gradients(t, at, t.n, g);
-        floats(t.m, at, t.n, m);
-        floats(t.v, at, t.n, v);
+    // A wave has two blocks of 256 elements, a lane four neighbours of each, so that every access of the wave is one run.
+    const uint64_t block = (piece - t.first) * (kPiece / kBlock) + wave_index() * 2;
+    if (block * kBlock >= t.n) return;
+    const uint64_t at[2] = {block * kBlock + lane * 4, (block + 1) * kBlock + lane * 4};
+    float x[2][4], g[2][4], m[2][4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (p.grad_scale) g[e] *= scale;
-            s.moments(g[e], m[e], v[e]);
-            x[e] = s.weight(x[e], m[e], sqrtf(v[e]));
+    for (int j = 0; j < 2; ++j) {
+        load4<F32>(t.x, at[j], t.n, x[j]);
+        gradients(t, at[j], g[j]);
+        if (p.grad_scale)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) g[j][e] *= scale;
+    }
+    if (t.state_bits == 32) {
+        float v[2][4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            load4<F32>(t.m, at[j], t.n, m[j]);
+            load4<F32>(t.v, at[j], t.n, v[j]);
         }
-        put_weights(t, at, x);
-        store8<F32>(static_cast<float*>(t.m), at, t.n, m);
-        store8<F32>(static_cast<float*>(t.v), at, t.n, v);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s.moments(g[j][e], m[j][e], v[j][e]);
+                x[j][e] = s.weight(x[j][e], m[j][e], sqrtf(v[j][e]));
+            }
+            put_weights(t, at[j], x[j]);
+            store4<F32>(t.m, at[j], t.n, m[j]);
+            store4<F32>(t.v, at[j], t.n, v[j]);
+        }
         return;
     }
-    // a wave has two blocks, whose draws are scalar
-    const uint64_t pair = local * (kPiece / kBlock) + wave_index() * 2;
-    const uint64_t seed = p.seed + (p.seed_increment ? *p.seed_increment : 0);
-    uint32_t word[2][4];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-        const uint64_t block = t.first * (kPiece / kBlock) + pair + b;
-        qsdp::philox4x32_10((uint32_t)block, (uint32_t)(block >> 32), 3u, 0u, (uint32_t)seed, (uint32_t)(seed >> 32), word[b]);
-    }
-    if (pair * kBlock >= t.n) return;  // whole waves, as lanes that share a block meet below
-    const uint64_t block = pair + (lane >= 32);
-    u32x2 mc = {0, 0}, vc = {0, 0};
-    float2 top = make_float2(0.0f, 0.0f);
+    uint32_t mc[2], vc[2];
+    float2 top[2];
     float2* scales = reinterpret_cast<float2*>(t.scale) + block;
-    if (some) {
-        floats(t.x, at, t.n, x);
-        gradients(t, at, t.n, g);
-        mc = load_codes(static_cast<const uint8_t*>(t.m), at, t.n);
-        vc = load_codes(static_cast<const uint8_t*>(t.v), at, t.n);
-        top = *scales;
-    } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = g[e] = 0.0f;
+    for (int j = 0; j < 2; ++j) {
+        mc[j] = load_codes(t.m, at[j], t.n);
+        vc[j] = load_codes(t.v, at[j], t.n);
+        top[j] = (block + j) * kBlock < t.n ? scales[j] : make_float2(0.0f, 0.0f);
     }
-    const float m_unit = top.x * (1.0f / kMostM), v_unit = top.y * (1.0f / kMostV);
-    float m[8], root[8], m_top = 0.0f, v_top = 0.0f;
+    // the draws are scalar, a block for each
+    const uint64_t seed = p.seed + (p.seed_increment ? *p.seed_increment : 0);
+    float root[2][4], m_top[2], v_top[2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float c = (float)(int8_t)(mc[e / 4] >> (e % 4 * 8)), d = (float)(uint8_t)(vc[e / 4] >> (e % 4 * 8));
-        const float r = v_unit * (d * d);
-        float v = r * r;
-        m[e] = m_unit * (c * fabsf(c));
-        if (p.grad_scale) g[e] *= scale;
-        s.moments(g[e], m[e], v);
-        root[e] = sqrtf(v);
-        x[e] = s.weight(x[e], m[e], root[e]);
-        m_top = fmaxf(m_top, fabsf(m[e]));
-        v_top = fmaxf(v_top, root[e]);
-    }
-    m_top = largest32(m_top);
-    v_top = largest32(v_top);
-    if (!some) return;
-    put_weights(t, at, x);
-    m_top = m_top >= kLeast ? m_top : 0.0f;
-    v_top = v_top >= kLeast ? v_top : 0.0f;
-    const float m_per = m_top > 0.0f ? kMostM / m_top : 0.0f, v_per = v_top > 0.0f ? kMostV / v_top : 0.0f;
-    const uint32_t in = (lane % 32) * 8;
-    const uint32_t m_word = (lane < 32 ? word[0][0] : word[1][0]) + in * 0x9E3779B9u;
-    const uint32_t v_word = (lane < 32 ? word[0][1] : word[1][1]) + in * 0x9E3779B9u;
-    mc = vc = u32x2{0, 0};
+    for (int j = 0; j < 2; ++j) {
+        const float m_unit = top[j].x * (1.0f / kMostM), v_unit = top[j].y * (1.0f / kMostV);
+        const uint32_t biased = mc[j] ^ 0x80808080u;  // as unsigned bytes about 128
+        bool tiny = false;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float c = code_of(fabsf(m[e]) * m_per, m_word + e * 0x9E3779B9u, 127.0f);
-        float d = code_of(root[e] * v_per, v_word + e * 0x9E3779B9u, 255.0f);
-        if (root[e] > 0.0f && v_top > 0.0f) d = fmaxf(d, 1.0f);
-        mc[e / 4] |= ((uint32_t)(int)copysignf(c, m[e]) & 0xffu) << (e % 4 * 8);
-        vc[e / 4] |= (uint32_t)d << (e % 4 * 8);
+        for (int e = 0; e < 4; ++e) {
+            const float c = (float)(uint8_t)(biased >> (e * 8)) - 128.0f, d = (float)(uint8_t)(vc[j] >> (e * 8));
+            const float r = v_unit * (d * d);
+            root[j][e] = r * r;
+            m[j][e] = m_unit * (c * fabsf(c));
+            s.moments(g[j][e], m[j][e], root[j][e]);
+            tiny |= root[j][e] < 0x1p-96f;
+        }
+        if (__any(tiny)) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) root[j][e] = sqrtf(root[j][e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) root[j][e] = root_of(root[j][e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[j][e] = s.weight(x[j][e], m[j][e], root[j][e]);
+        m_top[j] = fmaxf(fmaxf(fabsf(m[j][0]), fabsf(m[j][1])), fmaxf(fabsf(m[j][2]), fabsf(m[j][3])));
+        v_top[j] = fmaxf(fmaxf(root[j][0], root[j][1]), fmaxf(root[j][2], root[j][3]));
+        put_weights(t, at[j], x[j]);
     }
-    store_codes(static_cast<uint8_t*>(t.m), at, t.n, mc);
-    store_codes(static_cast<uint8_t*>(t.v), at, t.n, vc);
-    if (lane % 32 == 0) *scales = make_float2(m_top, v_top);
+    // rows of 16 lanes: M of the first block, its R, M of the second, its R; and what their quotients with the codes' squares are
+    float tops = largest_of_four(m_top[0], v_top[0], m_top[1], v_top[1]);
+    tops = tops >= kLeast ? tops : 0.0f;  // (R is 0 or from 2^-75 on)
+    const float per = tops > 0.0f ? (lane & 16 ? kMostV : kMostM) / tops : 0.0f;
+    auto of_row = [&](float v, int row) __attribute__((always_inline)) {
+        return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), row * 16));
+    };
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const float m_per = of_row(per, 2 * j), v_per = of_row(per, 2 * j + 1);
+        const uint64_t number = t.first * (kPiece / kBlock) + block + j;
+        uint32_t word[4];
+        qsdp::philox4x32_10((uint32_t)number, (uint32_t)(number >> 32), 3u, 0u, (uint32_t)seed, (uint32_t)(seed >> 32), word);
+        mc[j] = vc[j] = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t golden = (lane * 4 + e) * 0x9E3779B9u;
+            const float c = fminf(code_of(fabsf(m[j][e]) * m_per, word[0] + golden), 127.0f);
+            // at least 1 for a root that is not 0, which is from 2^-75 on; past 255 the conversion stops
+            const float d = fmaxf(code_of(root[j][e] * v_per, word[1] + golden), fminf(root[j][e] * 0x1p76f, 1.0f));
+            mc[j] = __builtin_amdgcn_cvt_pk_u8_f32(copysignf(c, m[j][e]) + 128.0f, e, mc[j]);
+            vc[j] = __builtin_amdgcn_cvt_pk_u8_f32(d, e, vc[j]);
+        }
+        store_codes(t.m, at[j], t.n, mc[j] ^ 0x80808080u);
+        store_codes(t.v, at[j], t.n, vc[j]);
+        if (lane == 0 && (block + j) * kBlock < t.n) scales[j] = make_float2(of_row(tops, 2 * j), of_row(tops, 2 * j + 1));
+    }
 }
 
 }  // namespace

@@ -15,7 +15,7 @@ struct AdamWParams {
     const qsdp_adamw_tensor* table;
     uint32_t count;
     uint64_t first;  // piece of a launch's first workgroup
-    float lr, beta1, beta2, eps, bias1, bias2;
+    float lr, beta1, beta2, eps, inverse1, inverse2;  // 1 / bias1, 1 / sqrt(bias2)
     uint64_t seed;
     const uint64_t* seed_increment;  // or none
     const float *schedule, *grad_scale;  // or none

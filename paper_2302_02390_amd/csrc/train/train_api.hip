@@ -208,11 +208,12 @@ int qsdp_adamw_tensors(const qsdp_adamw_tensor* table, uint32_t count, uint64_t 
                        float eps, float bias1, float bias2, uint64_t seed, const uint64_t* seed_dev, const float* schedule,
                        const float* grad_scale, void* stream) {
     if (!table || count == 0 || pieces == 0 || !std::isfinite(lr) || !(beta1 >= 0.0f && beta1 < 1.0f) ||
-        !(beta2 >= 0.0f && beta2 < 1.0f) || !(eps > 0.0f && std::isfinite(eps)) || !(bias1 > 0.0f && std::isfinite(bias1)) ||
+        !(beta2 >= 0.0f && beta2 < 1.0f) || !(eps >= 0x1p-126f && std::isfinite(eps)) || !(bias1 > 0.0f && std::isfinite(bias1)) ||
         !(bias2 > 0.0f && std::isfinite(bias2)))
         return QSDP_EINVAL;
     if (!aligned(table, 8) || !aligned(seed_dev, 8) || !aligned(schedule, 4) || !aligned(grad_scale, 4)) return QSDP_EALIGN;
-    const AdamWParams p = {table, count, 0, lr, beta1, beta2, eps, bias1, bias2, seed, seed_dev, schedule, grad_scale};
+    const AdamWParams p = {table, count, 0, lr, beta1, beta2, eps, 1.0f / bias1, 1.0f / std::sqrt(bias2), seed, seed_dev, schedule,
+                           grad_scale};
     return status_of(launch_adamw(p, pieces, static_cast<hipStream_t>(stream)));
 }
 

@@ -114,7 +114,7 @@ def test_adamw_tensors():
     good = [OK, 3, 5, 1e-3, 0.9, 0.95, 1e-8, 0.1, 0.05, 0, OK, OK, OK, None]
     _variants("qsdp_adamw_tensors", good, [
         (0, None, E), (0, FOUR, A), (1, 0, E), (2, 0, E), (3, math.nan, E), (3, math.inf, E), (4, 1.0, E), (4, -0.1, E),
-        (4, math.nan, E), (5, 1.0, E), (6, 0.0, E), (6, -1.0, E), (6, math.inf, E), (7, 0.0, E), (7, math.nan, E), (8, -1.0, E),
+        (4, math.nan, E), (5, 1.0, E), (6, 0.0, E), (6, 1e-39, E), (6, -1.0, E), (6, math.inf, E), (7, 0.0, E), (7, math.nan, E), (8, -1.0, E),
         (8, math.inf, E), (10, FOUR, A), (11, ODD, A), (12, ODD, A)])
 
 
