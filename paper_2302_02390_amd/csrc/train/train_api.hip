@@ -161,6 +161,10 @@ int qsdp_linear_blocks(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k, 
     if (!aligned(x, width(dtype)) || !aligned(w, 16) || !aligned(w_scales, 4) || !aligned(bias, 4) ||
         !aligned(y, width(out_dtype)) || !aligned(workspace, 16))
         return QSDP_EALIGN;
+    if (m <= kFewRows) {
+        const ProductParams p = {nullptr, nullptr, m, m, w, w_scales, n, k, pitch_of(k), bias, out_dtype, y, y_row_stride, false};
+        return status_of(launch_linear_few({x, dtype, row_stride}, p, static_cast<hipStream_t>(stream)));
+    }
     uint8_t* codes = static_cast<uint8_t*>(workspace);
     float* scales = reinterpret_cast<float*>(codes + m * pitch_of(k));
     const int status = qsdp_quantize_blocks(x, dtype, m, k, row_stride, 0, codes, scales, nullptr, nullptr, stream);

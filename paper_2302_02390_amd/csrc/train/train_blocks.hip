@@ -10,32 +10,6 @@
 namespace qsdp_train {
 namespace {
 
-constexpr float kMost = 448.0f, kLeast = 0x1p-100f;
-
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-
-// Eight codes.
-__device__ __forceinline__ u32x2 codes8(const float* v) {
-    u32x2 c;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        int word = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
-        word = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], word, true);
-        c[i] = (uint32_t)word;
-    }
-    return c;
-}
-
-// Over the lanes that are 16 and 32 apart.
-__device__ __forceinline__ float largest_of_rows(float v) {
-    uint32_t u = __builtin_bit_cast(uint32_t, v);
-    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-    v = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
-    u = __builtin_bit_cast(uint32_t, v);
-    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
-}
-
 // A workgroup rounds 128 x 128 elements both ways round from one read: a thread has eight consecutive columns of eight
 // consecutive rows, so that a row's block is 16 neighbouring lanes, and eight codes of a column, like those of a row, are one store.
 template <class T, bool SQUARE>
@@ -65,19 +39,19 @@ __global__ __launch_bounds__(256) void quantize_kernel(BlockParams p) {
         float most = by_row[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) most = fmaxf(most, by_row[i]);
-        most = fmaxf(reduce_block<256>(most, Max(), &largest[0][0]), kLeast);
+        most = fmaxf(reduce_block<256>(most, Max(), &largest[0][0]), kLeastBlock);
 #pragma unroll
         for (int i = 0; i < 8; ++i) by_row[i] = by_col[i] = most;
         if (threadIdx.x == 0) {
-            if (p.codes) p.scales[col_block * blocks_of(p.rows) + row_block] = most / kMost;
-            if (p.codes_t) p.scales_t[row_block * blocks_of(p.cols) + col_block] = most / kMost;
+            if (p.codes) p.scales[col_block * blocks_of(p.rows) + row_block] = most / kMostCode;
+            if (p.codes_t) p.scales_t[row_block * blocks_of(p.cols) + col_block] = most / kMostCode;
         }
     } else {
         if (p.codes) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                by_row[i] = fmaxf(reduce16(by_row[i], Max()), kLeast);
-                if (lane % 16 == i && r0 + i < p.rows) p.scales[col_block * p.rows + r0 + i] = by_row[i] / kMost;
+                by_row[i] = fmaxf(reduce16(by_row[i], Max()), kLeastBlock);
+                if (lane % 16 == i && r0 + i < p.rows) p.scales[col_block * p.rows + r0 + i] = by_row[i] / kMostCode;
             }
         }
         if (p.codes_t) {
@@ -90,8 +64,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(BlockParams p) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 by_col[e] = fmaxf(fmaxf(fmaxf(largest[0][col + e], largest[1][col + e]),
-                                        fmaxf(largest[2][col + e], largest[3][col + e])), kLeast);
-                if (threadIdx.x < 16 && c0 + e < p.cols) p.scales_t[row_block * p.cols + c0 + e] = by_col[e] / kMost;
+                                        fmaxf(largest[2][col + e], largest[3][col + e])), kLeastBlock);
+                if (threadIdx.x < 16 && c0 + e < p.cols) p.scales_t[row_block * p.cols + c0 + e] = by_col[e] / kMostCode;
             }
         }
     }
@@ -101,7 +75,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(BlockParams p) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             if (r0 + i >= p.rows) continue;
-            const float up = kMost / by_row[i];
+            const float up = kMostCode / by_row[i];
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = raw[i].at(e) * up;
@@ -114,7 +88,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(BlockParams p) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             if (c0 + e >= p.cols) continue;
-            const float up = kMost / by_col[e];
+            const float up = kMostCode / by_col[e];
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = raw[i].at(e) * up;

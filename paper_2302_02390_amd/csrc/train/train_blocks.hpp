@@ -13,6 +13,8 @@ constexpr uint32_t kWide = 128;  // elements of a block along the summed axis, a
 
 constexpr uint64_t blocks_of(uint64_t n) { return (n + kWide - 1) / kWide; }
 
+constexpr float kMostCode = 448.0f, kLeastBlock = 0x1p-100f;
+
 struct BlockParams {
     const void* x;
     uint64_t rows, cols, stride;  // elements
@@ -37,7 +39,16 @@ struct ProductParams {
     bool accumulate;
 };
 
+// Few rows of a product, as they come: rounded on the way, by every workgroup.
+struct FewRows {
+    const void* x;
+    qsdp_dtype dtype;
+    uint64_t stride;  // elements
+};
+
 hipError_t launch_quantize(qsdp_dtype dtype, bool square, const BlockParams& p, hipStream_t s);
 hipError_t launch_product(bool b_square, const ProductParams& p, hipStream_t s);
+// The product of at most kFewRows rows with square blocks; p.a, p.a_scale and p.a_rows are not looked at.
+hipError_t launch_linear_few(const FewRows& x, const ProductParams& p, hipStream_t s);
 
 }  // namespace qsdp_train

@@ -56,6 +56,30 @@ __device__ __forceinline__ void store8(typename T::raw* p, int left, const float
     }
 }
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Eight codes of 8-bit floating point, to nearest even.
+__device__ __forceinline__ u32x2 codes8(const float* v) {
+    u32x2 c;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int word = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
+        word = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], word, true);
+        c[i] = (uint32_t)word;
+    }
+    return c;
+}
+
+// Over the lanes that are 16 and 32 apart.
+__device__ __forceinline__ float largest_of_rows(float v) {
+    uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    v = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+    u = __builtin_bit_cast(uint32_t, v);
+    const auto b = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]), __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+
 // Eight parameters in a format that the call names, zeros past the row's end. Asked for first and turned into numbers later, so that
 // several groups are on their way together.
 struct Parameters8 {

@@ -54,4 +54,19 @@ constexpr uint64_t norm_workgroups(uint64_t rows, uint64_t n) {
     return need < most ? need : most;
 }
 
+// ---- products (train_product.hip) ------------------------------------------------------------------------------------------
+constexpr uint64_t kFewRows = 16;
+
+// Groups of 16 columns to a workgroup: more of them share the rounding of the rows, fewer fill the chip.
+constexpr int few_groups(uint64_t n) { return n >= 32768 ? 4 : n >= 8192 ? 2 : 1; }
+
+enum class ProductTile { T64, T128, T256 };
+
+// exact: results in binary32, whose operands take twice the registers in the 256-wide tile.
+constexpr ProductTile choose_tile(uint64_t m, uint64_t n, uint64_t k, bool exact) {
+    const uint64_t of_128 = (m + 127) / 128 * ((n + 127) / 128), of_256 = (m + 255) / 256 * ((n + 255) / 256);
+    if (!exact && of_256 >= 224 && k >= 4096) return ProductTile::T256;
+    return of_128 >= 224 ? ProductTile::T128 : ProductTile::T64;
+}
+
 }  // namespace qsdp_train

@@ -7,6 +7,8 @@
 // random operands' sums come out 1.3e-5 of their norm off (16 x 16 x 128 and 32 x 32 x 64 alike; codes within a factor of 2^9 are
 // exact). That is lost in 16-bit results, whose rounding is 2^-9 or 2^-12. Results in binary32 go by bf16 instructions
 // (EXACT): every code is a bf16 number, the products are exact, and the matrix units take twice the time.
+#include <type_traits>
+
 #include "train_blocks.hpp"
 #include "train_common.hpp"
 #include "train_plan.hpp"
@@ -80,58 +82,39 @@ __device__ __forceinline__ v8i fragment(const uint8_t* row, int first, int secon
 }
 
 // ---- results ---------------------------------------------------------------------------------------------------------------
-// Four consecutive results of a row, or the first `count` of them.
+// The first `count` of four consecutive results of a row.
 template <class O>
-__device__ __forceinline__ void put_to(typename O::raw* y, float* v, int count, bool accumulate) {
-    if (count == 4) {
-        if constexpr (sizeof(typename O::raw) == 4) {
-            typedef float anywhere __attribute__((ext_vector_type(4), aligned(4)));
-            anywhere* to = reinterpret_cast<anywhere*>(y);
-            anywhere r = {v[0], v[1], v[2], v[3]};
-            if (accumulate) {
-                const anywhere old = *to;
+__device__ __forceinline__ void put_some(typename O::raw* y, const float* v, int count, bool accumulate) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) r[c] += old[c];
-            }
-            *to = r;
-        } else {
+    for (int c = 0; c < 4; ++c)
+        if (c < count) y[c] = O::put(accumulate ? v[c] + O::get(y[c]) : v[c]);
+}
+
+// 4 Q consecutive results of a row, of which the matrix has `left`.
+template <class O, int Q>
+__device__ __forceinline__ void put_row(typename O::raw* y, const float (&v)[4 * Q], int left, bool accumulate) {
+    if (left >= 4 * Q && !accumulate) {
+        if constexpr (Q == 1 && O::PER == 8) {
             typedef uint32_t anywhere __attribute__((ext_vector_type(2), aligned(2)));
-            anywhere* to = reinterpret_cast<anywhere*>(y);
-            if (accumulate) {
-                const anywhere old = *to;
-                const u32x4 both = {old[0], old[1], 0, 0};
+            *reinterpret_cast<anywhere*>(y) = anywhere{O::two(v[0], v[1]), O::two(v[2], v[3])};
+        } else {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] += O::at(both, c);
-            }
-            *to = anywhere{O::two(v[0], v[1]), O::two(v[2], v[3])};
+            for (int i = 0; i < 4 * Q / O::PER; ++i) *reinterpret_cast<u32x4_anywhere*>(y + i * O::PER) = O::pack(v + i * O::PER);
         }
     } else {
 #pragma unroll
-        for (int c = 0; c < 3; ++c)
-            if (c < count) y[c] = O::put(accumulate ? v[c] + O::get(y[c]) : v[c]);
+        for (int i = 0; i < Q; ++i) put_some<O>(y + 4 * i, v + 4 * i, left - 4 * i, accumulate);
     }
 }
 
-__device__ __forceinline__ void put4(const ProductParams& p, uint64_t m, uint64_t n, float* v) {
-    const int count = p.n - n < 4 ? (int)(p.n - n) : 4;
-    if (p.bias)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) v[c] += p.bias[c < count ? n + c : n];
-    const uint64_t at = m * p.y_stride + n;
-    if (p.out == QSDP_F32) put_to<F32>(static_cast<float*>(p.y) + at, v, count, p.accumulate);
-    else if (p.out == QSDP_BF16) put_to<BF16>(static_cast<uint16_t*>(p.y) + at, v, count, p.accumulate);
-    else put_to<F16>(static_cast<_Float16*>(p.y) + at, v, count, p.accumulate);
-}
-
 // ---- tiles -----------------------------------------------------------------------------------------------------------------
-template <int TN, int TM, int WN, int WM, bool SQUARE>
+template <int TN, int TM, int WN, int WM>
 struct Tile {
     static constexpr int WAVES = TN / WN * (TM / WM), THREADS = WAVES * 64;
-    static constexpr int CODES = (TN + TM) * (int)kWide;           // bytes of a step's codes in LDS,
-    static constexpr int SCALES = TM + (SQUARE ? 0 : TN);          // and its scales
-    static constexpr int BYTES = CODES + SCALES * 4;
+    static constexpr int CODES = (TN + TM) * (int)kWide;  // bytes of a step's codes in LDS, behind them
+    static constexpr int BYTES = CODES + (TN + TM) * 4;   // the scales of the rows and of the columns
     static constexpr int B_LOADS = TN / 8 / WAVES, A_LOADS = TM / 8 / WAVES;  // of 8 rows, for each wave
-    static constexpr int LOADS = B_LOADS + A_LOADS + 1 + (SQUARE ? 0 : 1);
+    static constexpr int LOADS = B_LOADS + A_LOADS + 2;   // columns, their scales, rows, their scales
     static_assert(TN % (8 * WAVES) == 0 && TM % (8 * WAVES) == 0 && TN % 64 == 0 && TM % 64 == 0, "whole loads");
 };
 
@@ -150,105 +133,311 @@ __device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_
 
 // A workgroup computes TN columns x TM rows of y in steps of a block of 128. Both operands' codes go straight from memory into
 // LDS, two steps deep, and one barrier a step separates them. LDS holds rows of 128 bytes whose eight pieces of 16 are permuted by the
-// row (piece c of row r in place c ^ (r % 8)), so that sixteen rows read the same piece from all banks; the permutation is in the
-// addresses that the lanes read from memory. A wave multiplies WN columns (first operand, so that four consecutive columns of a row
-// of y end up in a lane) by WM rows: it keeps a step's columns in registers and walks over the rows.
+// row (piece c in place c ^ key), so that the rows of a fragment read the same piece from all banks; the permutation is in the
+// addresses that the lanes read from memory. A wave multiplies WN columns (first operand, four rows of whose result are in a lane) by
+// WM rows. Which columns a fragment has is free: every fourth four, so that a lane ends with WN / 4 neighbours of a row. It keeps a step's columns in registers and walks over the rows, sixteen at a time. While these are
+// multiplied the next sixteen come out of LDS and the sums before go into the result; with the last ones the next step begins.
 template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT>
 __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(ProductParams p, uint32_t n_tiles, uint32_t m_tiles) {
-    typedef Tile<TN, TM, WN, WM, SQUARE> S;
+    typedef Tile<TN, TM, WN, WM> S;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES][S::BYTES];
-    constexpr int A = WN / 16, B = WM / 16;
+    constexpr int A = WN / 16, B = WM / 16, WIDTH = 4 * A;  // fragments; consecutive columns of a lane
+    static_assert(B % 2 == 0 && A % 2 == 0, "fragments and products in turn");
     uint32_t n_tile, m_tile;
     place(blockIdx.x, n_tiles, m_tiles, n_tile, m_tile);
     const int lane = threadIdx.x % 64, wave = wave_index();
     const uint64_t n0 = (uint64_t)n_tile * TN, m0 = (uint64_t)m_tile * TM;
     // what the lane loads: a piece of 16 bytes of a row of eight; rows past the matrix are its last one
-    const uint32_t piece = (uint32_t)((lane % 8) ^ (lane / 8)) * 16;
     uint32_t b_at[S::B_LOADS], a_at[S::A_LOADS];
 #pragma unroll
     for (int i = 0; i < S::B_LOADS; ++i) {
-        uint64_t row = (uint64_t)(wave * S::B_LOADS + i) * 8 + lane / 8;
-        if (n0 + row >= p.n) row = p.n - 1 - n0;
-        b_at[i] = (uint32_t)(row * p.pitch) + piece;
+        const int in = (wave * S::B_LOADS + i) * 8 + lane / 8;
+        const uint64_t row = n0 + in < p.n ? in : p.n - 1 - n0;
+        b_at[i] = (uint32_t)(row * p.pitch) + ((lane % 8) ^ (in % 4 + in / WIDTH % 2 * 4)) * 16;
     }
 #pragma unroll
     for (int i = 0; i < S::A_LOADS; ++i) {
-        uint64_t row = (uint64_t)(wave * S::A_LOADS + i) * 8 + lane / 8;
-        if (m0 + row >= p.m) row = p.m - 1 - m0;
-        a_at[i] = (uint32_t)(row * p.pitch) + piece;
+        const int in = (wave * S::A_LOADS + i) * 8 + lane / 8;
+        const uint64_t row = m0 + in < p.m ? in : p.m - 1 - m0;
+        a_at[i] = (uint32_t)(row * p.pitch) + ((lane % 8) ^ (in % 8)) * 16;
     }
     const uint8_t* b = p.b + n0 * p.pitch;
     const uint8_t* a = p.a + m0 * p.pitch;
-    // scales: 64 to a load; waves that have none of their own load another's again
+    // Scales: 64 to a load; waves that have none of their own load another's again. A column has a scale of its own, or that of its
+    // square block.
     const int a_part = wave % (TM / 64) * 64, b_part = wave % (TN / 64) * 64;
-    const float* a_scale = p.a_scale + (m0 + a_part + lane < p.m ? m0 + a_part + lane : p.m - 1);
-    const float* b_scale = SQUARE ? p.b_scale : p.b_scale + (n0 + b_part + lane < p.n ? n0 + b_part + lane : p.n - 1);
-    auto fetch = [&](uint8_t* to, uint32_t s) __attribute__((always_inline)) {
+    const uint64_t of_row = m0 + a_part + lane < p.m ? m0 + a_part + lane : p.m - 1;
+    const uint64_t of_column = n0 + b_part + lane < p.n ? n0 + b_part + lane : p.n - 1;
+    const float* a_scale = p.a_scale + of_row;
+    const float* b_scale = p.b_scale + (SQUARE ? of_column / kWide : of_column);
+    const uint64_t b_scales = SQUARE ? blocks_of(p.n) : p.n;
+    // loads [from, to) of the wave's of a step
+    auto fetch = [&](uint8_t* at, uint32_t s, int from, int to) __attribute__((always_inline)) {
         const uint32_t k0 = s * kWide;
 #pragma unroll
-        for (int i = 0; i < S::B_LOADS; ++i)
-            __builtin_amdgcn_global_load_lds((global_ptr)(b + k0 + b_at[i]), (lds_ptr)(to + (wave * S::B_LOADS + i) * 1024), 16, 0, 0);
-#pragma unroll
-        for (int i = 0; i < S::A_LOADS; ++i)
-            __builtin_amdgcn_global_load_lds((global_ptr)(a + k0 + a_at[i]),
-                                             (lds_ptr)(to + TN * kWide + (wave * S::A_LOADS + i) * 1024), 16, 0, 0);
-        __builtin_amdgcn_global_load_lds((global_ptr)(a_scale + s * p.a_rows), (lds_ptr)(to + S::CODES + a_part * 4), 4, 0, 0);
-        if constexpr (!SQUARE)
-            __builtin_amdgcn_global_load_lds((global_ptr)(b_scale + s * p.n), (lds_ptr)(to + S::CODES + (TM + b_part) * 4), 4, 0, 0);
+        for (int l = from; l < to; ++l) {
+            const int l_a = l - S::B_LOADS - 1;
+            if (l < S::B_LOADS)
+                __builtin_amdgcn_global_load_lds((global_ptr)(b + k0 + b_at[l]), (lds_ptr)(at + (wave * S::B_LOADS + l) * 1024), 16, 0, 0);
+            else if (l == S::B_LOADS)
+                __builtin_amdgcn_global_load_lds((global_ptr)(b_scale + s * b_scales), (lds_ptr)(at + S::CODES + (TM + b_part) * 4), 4, 0, 0);
+            else if (l_a < S::A_LOADS)
+                __builtin_amdgcn_global_load_lds((global_ptr)(a + k0 + a_at[l_a]),
+                                                 (lds_ptr)(at + TN * kWide + (wave * S::A_LOADS + l_a) * 1024), 16, 0, 0);
+            else
+                __builtin_amdgcn_global_load_lds((global_ptr)(a_scale + s * p.a_rows), (lds_ptr)(at + S::CODES + a_part * 4), 4, 0, 0);
+        }
     };
     const int wn = wave % (TN / WN) * WN, wm = wave / (TN / WN) * WM;
     const int r = lane % 16, part = lane / 16;
     const int first = (part ^ (r % 8)) * 16, second = ((4 + part) ^ (r % 8)) * 16;
-    const uint64_t n_blocks = blocks_of(p.n);
-    const float* square = p.b_scale + ((n0 + wn) / kWide < n_blocks ? (n0 + wn) / kWide : n_blocks - 1);
+    const int b_row = (wn + r / 4 * WIDTH + r % 4) * kWide, a_row = (TN + wm + r) * kWide, a_of = S::CODES + (wm + r) * 4;
+    const int b_of = S::CODES + (TM + wn + (SQUARE ? 0 : part * WIDTH)) * 4;
     const uint32_t steps = (uint32_t)(p.pitch / kWide);
+    // the wave's loads of columns and their scales; and those up to the middle of the rows'
+    constexpr bool EARLY = B >= 4;
+    constexpr int OF_B = S::B_LOADS + 1, MIDDLE = OF_B + (S::A_LOADS + 1) / 2;
+    static_assert(!EARLY || STAGES == 2, "steps in LDS");
     v4f sum[A][B];
 #pragma unroll
     for (int i = 0; i < A; ++i)
 #pragma unroll
         for (int j = 0; j < B; ++j) sum[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    v8i bv[A], av[2];  // this step's columns, these rows and the next
+    float of[2];       // and the rows' scales
+    v4f of_b[SQUARE ? 1 : A], of_b_next[SQUARE ? 1 : A];
+    v4f now[4];        // sums over a block that are not in the result yet
+    auto read_b = [&](const uint8_t* from, int i) __attribute__((always_inline)) {
+        bv[i] = fragment(from + b_row + i * 4 * kWide, first, second);
+    };
+    auto read_a = [&](const uint8_t* from, int j, int set) __attribute__((always_inline)) {
+        av[set] = fragment(from + a_row + j * 16 * kWide, first, second);
+        of[set] = *reinterpret_cast<const float*>(from + a_of + j * 64);
+    };
+    auto read_scales = [&](const uint8_t* from) __attribute__((always_inline)) {
+        if constexpr (SQUARE) {
+            of_b_next[0][0] = *reinterpret_cast<const float*>(from + b_of);
+        } else {
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s)
-        if ((uint32_t)s < steps) fetch(lds[s], s);
-    for (uint32_t s = 0; s < steps; ++s) {
-        wait_loads<0>();
-        meet_here();
-        if (s + STAGES - 1 < steps) fetch(lds[(s + STAGES - 1) % STAGES], s + STAGES - 1);
-        const uint8_t* from = lds[s % STAGES];
-        const float* scales = reinterpret_cast<const float*>(from + S::CODES);
-        const float of_b = SQUARE ? square[s * n_blocks] : 1.0f;
-        v8i bv[A];
+            for (int i = 0; i < A; ++i) of_b_next[i] = *reinterpret_cast<const v4f*>(from + b_of + i * 16);
+        }
+    };
+    if constexpr (EARLY) {
+        fetch(lds[0], 0, 0, S::LOADS);
+        if (1 < steps) {
+            fetch(lds[1], 1, 0, MIDDLE);
+            wait_loads<MIDDLE>();
+        } else {
+            wait_loads<0>();
+        }
+    } else {
 #pragma unroll
-        for (int i = 0; i < A; ++i) bv[i] = fragment(from + (wn + i * 16 + r) * kWide, first, second);
+        for (int s = 0; s < STAGES; ++s)
+            if ((uint32_t)s < steps) fetch(lds[s], s, 0, S::LOADS);
+        if (STAGES <= steps) wait_loads<(STAGES - 1) * S::LOADS>();
+        else wait_loads<0>();
+    }
+    meet_here();
+    read_a(lds[0], 0, 0);
+    read_scales(lds[0]);
+    __builtin_amdgcn_sched_barrier(0);  // the scales before the columns: these have come when those have
+#pragma unroll
+    for (int i = 0; i < A; ++i) read_b(lds[0], i);
+#pragma unroll
+    for (int i = 0; i < (SQUARE ? 1 : A); ++i) of_b[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) now[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    float factor = 0.0f, factor_before = 0.0f;  // of these rows and of those before
+    // A product goes into the result when two more have been asked for: the code stands in the order in which it is to run.
+    auto add = [&](int i, int j, int at, float of_a) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            sum[i][j][c] = fmaf(now[at % 4][c], SQUARE ? of_a : of_a * of_b[SQUARE ? 0 : i][c], sum[i][j][c]);
+    };
+    // One step; FETCH: a further one is asked for, NEXT: there is a next one. Without a branch, behind which the compiler would move the
+    // sums.
+    auto step = [&](uint32_t s, auto FETCH, auto NEXT) __attribute__((always_inline)) {
+        uint8_t* here = lds[s % STAGES];
+        uint8_t* there = lds[(s + 1) % STAGES];
 #pragma unroll
         for (int j = 0; j < B; ++j) {
-            const Operand<EXACT> av(fragment(from + (TN + wm + j * 16 + r) * kWide, first, second));
-            const float of = scales[wm + j * 16 + r] * of_b;
+            const int set = j % 2;
+            const bool last = j + 1 == B;
+            if (EARLY && j == 1 && FETCH) meet_here();  // all have this step's columns in registers
+            if (last && NEXT) {
+                // The next step is there for all waves, and all have read this one.
+                wait_reads();
+                if (FETCH) wait_loads<EARLY ? OF_B : (STAGES - 2) * S::LOADS>();
+                else wait_loads<0>();
+                meet_here();
+            }
+            const Operand<EXACT> rows(av[set]);
+            if (last && NEXT) {
+                read_a(there, 0, 0);
+                read_scales(there);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            factor_before = factor;
+            factor = SQUARE ? of[set] * (j ? of_b[0][0] : of_b_next[0][0]) : of[set];
 #pragma unroll
             for (int i = 0; i < A; ++i) {
-                const v4f part_sum = product(Operand<EXACT>(bv[i]), av);
-                v4f by = {of, of, of, of};
-                if constexpr (!SQUARE) by = *reinterpret_cast<const v4f*>(scales + TM + wn + i * 16 + part * 4) * of;
+                const int q = j * A + i;
+                now[q % 4] = product(Operand<EXACT>(bv[i]), rows);
+                __builtin_amdgcn_sched_barrier(0);
+                if (last) {
+                    if (NEXT) read_b(there, i);
+                } else if (i == 0) {
+                    read_a(here, j + 1, 1 - set);
+                }
+                if constexpr (EARLY) {
+                    // The columns of the step after the next, whose place is free from here on, one load at a time; its rows with the
+                    // last products, and the rest of them with the first ones of the next step.
+                    constexpr int SLOTS = (B - 2) * A;  // products between
+                    const int at = q - A;
+                    if (FETCH && at >= 0 && at < SLOTS) fetch(here, s + 2, at * OF_B / SLOTS, (at + 1) * OF_B / SLOTS);
+                    if (FETCH && last) fetch(here, s + 2, OF_B + i * (MIDDLE - OF_B) / A, OF_B + (i + 1) * (MIDDLE - OF_B) / A);
+                    if (NEXT && j == 0) fetch(there, s + 1, MIDDLE + i * (S::LOADS - MIDDLE) / A, MIDDLE + (i + 1) * (S::LOADS - MIDDLE) / A);
+                    __builtin_amdgcn_sched_barrier(0);
+                } else if (FETCH && last && i == 0) {
+                    fetch(here, s + STAGES, 0, S::LOADS);
+                }
+                if (i >= 2) add(i - 2, j, q + 2, factor);
+                else add(A - 2 + i, j ? j - 1 : B - 1, q + 2, factor_before);
+                if (j == 0 && i == 1)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) sum[i][j][c] = fmaf(part_sum[c], by[c], sum[i][j][c]);
+                    for (int e = 0; e < (SQUARE ? 1 : A); ++e) of_b[e] = of_b_next[e];
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        wait_reads();
-        meet_here();
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    uint32_t s = 0;
+    for (; s + (EARLY ? 2 : STAGES) < steps; ++s) step(s, yes, yes);
+    for (; s + 1 < steps; ++s) step(s, no, yes);
+    step(s, no, no);
+    add(A - 2, B - 1, A * B - 2, factor);
+    add(A - 1, B - 1, A * B - 1, factor);
+    // sum[i][j][c]: column wn + part * WIDTH + i * 4 + c of row wm + j * 16 + r
+    const uint64_t n = n0 + wn + part * WIDTH;
+    if (n >= p.n) return;
+    const int left = p.n - n < WIDTH ? (int)(p.n - n) : WIDTH;
+    float bias[WIDTH];
+#pragma unroll
+    for (int e = 0; e < WIDTH; ++e) bias[e] = p.bias ? p.bias[n + (e < left ? e : 0)] : 0.0f;
+    auto put = [&](auto* format) __attribute__((always_inline)) {
+        typedef std::remove_pointer_t<decltype(format)> O;
+        auto* y = static_cast<typename O::raw*>(p.y) + n;
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            const uint64_t m = m0 + wm + j * 16 + r;
+            if (m >= p.m) continue;
+            float v[WIDTH];
+#pragma unroll
+            for (int e = 0; e < WIDTH; ++e) v[e] = sum[e / 4][j][e % 4] + bias[e];
+            put_row<O, A>(y + m * p.y_stride, v, left, p.accumulate);
+        }
+    };
+    if constexpr (EXACT) put((F32*)nullptr);
+    else if (p.out == QSDP_BF16) put((BF16*)nullptr);
+    else put((F16*)nullptr);
+}
+
+// ---- few rows --------------------------------------------------------------------------------------------------------------
+// Up to 16 rows: the weights' bytes bound the time. A workgroup takes 16 * GROUPS columns; its waves share the blocks of k, each with
+// loads of its own from memory into registers, a block ahead, and waits for nobody until the sums meet in LDS, in the order of the waves.
+// The rows are rounded where they are multiplied: a lane has the pieces of its row that it multiplies, and the four lanes of a row find
+// the block's largest together.
+constexpr int kFewWaves = 8;
+
+template <class X, int GROUPS, bool EXACT>
+__global__ __launch_bounds__(kFewWaves * 64) void few_kernel(FewRows x, ProductParams p) {
+    __shared__ v4f meet[kFewWaves][GROUPS][64];
+    const int lane = threadIdx.x % 64, wave = wave_index(), r = lane % 16, part = lane / 16;
+    const uint64_t n0 = (uint64_t)blockIdx.x * (16 * GROUPS);
+    const uint8_t* b[GROUPS];
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        const uint64_t row = n0 + i * 16 + r;
+        b[i] = p.b + (row < p.n ? row : p.n - 1) * p.pitch + part * 16;
     }
-    // sum[i][j][c]: column wn + i * 16 + part * 4 + c of row wm + j * 16 + r
+    const auto* row = static_cast<const typename X::raw*>(x.x) + ((uint64_t)r < p.m ? r : p.m - 1) * x.stride + part * 16;
+    const uint64_t n_blocks = blocks_of(p.n), in = n0 / kWide;  // 128 is a multiple of a workgroup's columns
+    const float* b_scale = p.b_scale + in;
+    const uint32_t steps = (uint32_t)(p.pitch / kWide);
+    v4i codes[GROUPS][2];
+    Raw8<X> raw[4];
+    float scale = 0.0f;
+    auto fetch = [&](uint32_t s) __attribute__((always_inline)) {
+        if (s >= steps) return;
+        const uint32_t k0 = s * kWide;
 #pragma unroll
-    for (int j = 0; j < B; ++j) {
-        const uint64_t m = m0 + wm + j * 16 + r;
-        if (m >= p.m) continue;
+        for (int i = 0; i < GROUPS; ++i) {
+            codes[i][0] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(b[i] + k0));
+            codes[i][1] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(b[i] + k0 + 64));
+        }
+        const int left = (int)(p.k - k0) - part * 16;
 #pragma unroll
-        for (int i = 0; i < A; ++i) {
-            const uint64_t n = n0 + wn + i * 16 + part * 4;
-            if (n >= p.n) continue;
-            float v[4] = {sum[i][j][0], sum[i][j][1], sum[i][j][2], sum[i][j][3]};
-            put4(p, m, n, v);
+        for (int h = 0; h < 4; ++h) {
+            const int at = h / 2 * 64 + h % 2 * 8;
+            if (left > at) raw[h].load(row + k0 + at, left - at);
+            else raw[h].none();
+        }
+        scale = b_scale[s * n_blocks];
+    };
+    v4f sum[GROUPS];
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) sum[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    fetch(wave);
+    for (uint32_t s = wave; s < steps; s += kFewWaves) {
+        v8i bv[GROUPS];
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) bv[i] = __builtin_shufflevector(codes[i][0], codes[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
+        float v[32], most = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = raw[e / 8].at(e % 8);
+        const float of_b = scale;
+        fetch(s + kFewWaves);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(v[e]));
+        most = fmaxf(largest_of_rows(most), kLeastBlock);
+        const float up = kMostCode / most, of = most / kMostCode * of_b;
+        v8i av;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = v[h * 8 + e] * up;
+            const u32x2 two = codes8(w);
+            av[2 * h] = (int)two[0];
+            av[2 * h + 1] = (int)two[1];
+        }
+        const Operand<EXACT> rows(av);
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) {
+            const v4f now = product(Operand<EXACT>(bv[i]), rows);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sum[i][c] = fmaf(now[c], of, sum[i][c]);
         }
     }
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) meet[wave][i][lane] = sum[i];
+    __syncthreads();
+    if (wave >= GROUPS) return;
+    v4f total = meet[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) total += meet[w][wave][lane];
+    // columns part * 4 ... of row r
+    const uint64_t n = n0 + wave * 16 + part * 4;
+    if (n >= p.n || (uint64_t)r >= p.m) return;
+    const int left = p.n - n < 4 ? (int)(p.n - n) : 4;
+    float v[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = total[c] + (p.bias ? p.bias[n + (c < left ? c : 0)] : 0.0f);
+    const uint64_t at = r * p.y_stride + n;
+    if constexpr (EXACT) put_row<F32, 1>(static_cast<float*>(p.y) + at, v, left, false);
+    else if (p.out == QSDP_BF16) put_row<BF16, 1>(static_cast<uint16_t*>(p.y) + at, v, left, false);
+    else put_row<F16, 1>(static_cast<_Float16*>(p.y) + at, v, left, false);
 }
 
 }  // namespace
@@ -267,7 +456,7 @@ static hipError_t launch_tiles(const ProductParams& p, hipStream_t s) {
         q.m = p.m - first < now * TM ? p.m - first : now * TM;
         q.y = static_cast<uint8_t*>(p.y) + first * p.y_stride * (p.out == QSDP_F32 ? 4 : 2);
         hipLaunchKernelGGL((tiles_kernel<TN, TM, WN, WM, STAGES, SQUARE, EXACT>), dim3(n_tiles * (unsigned)now),
-                           dim3(Tile<TN, TM, WN, WM, SQUARE>::THREADS), 0, s, q, n_tiles, (uint32_t)now);
+                           dim3(Tile<TN, TM, WN, WM>::THREADS), 0, s, q, n_tiles, (uint32_t)now);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -276,12 +465,37 @@ static hipError_t launch_tiles(const ProductParams& p, hipStream_t s) {
 
 template <bool SQUARE, bool EXACT>
 static hipError_t launch_product_of(const ProductParams& p, hipStream_t s) {
-    return launch_tiles<64, 64, 32, 32, 2, SQUARE, EXACT>(p, s);
+    switch (choose_tile(p.m, p.n, p.k, EXACT)) {
+        case ProductTile::T64: return launch_tiles<64, 64, 32, 32, 3, SQUARE, EXACT>(p, s);
+        case ProductTile::T128: return launch_tiles<128, 128, 64, 64, 2, SQUARE, EXACT>(p, s);
+        case ProductTile::T256:
+            if constexpr (!EXACT) return launch_tiles<256, 256, 64, 128, 2, SQUARE, EXACT>(p, s);
+    }
+    return hipErrorInvalidValue;
 }
 
 hipError_t launch_product(bool b_square, const ProductParams& p, hipStream_t s) {
     if (p.out == QSDP_F32) return b_square ? launch_product_of<true, true>(p, s) : launch_product_of<false, true>(p, s);
     return b_square ? launch_product_of<true, false>(p, s) : launch_product_of<false, false>(p, s);
+}
+
+template <class X, int GROUPS>
+static hipError_t launch_few(const FewRows& x, const ProductParams& p, hipStream_t s) {
+    const dim3 grid((unsigned)((p.n + 16 * GROUPS - 1) / (16 * GROUPS))), block(kFewWaves * 64);
+    if (p.out == QSDP_F32) hipLaunchKernelGGL((few_kernel<X, GROUPS, true>), grid, block, 0, s, x, p);
+    else hipLaunchKernelGGL((few_kernel<X, GROUPS, false>), grid, block, 0, s, x, p);
+    return hipGetLastError();
+}
+
+template <class X>
+static hipError_t launch_few_of(const FewRows& x, const ProductParams& p, hipStream_t s) {
+    const int groups = few_groups(p.n);
+    return groups == 4 ? launch_few<X, 4>(x, p, s) : groups == 2 ? launch_few<X, 2>(x, p, s) : launch_few<X, 1>(x, p, s);
+}
+
+hipError_t launch_linear_few(const FewRows& x, const ProductParams& p, hipStream_t s) {
+    if (x.dtype == QSDP_F32) return launch_few_of<F32>(x, p, s);
+    return x.dtype == QSDP_BF16 ? launch_few_of<BF16>(x, p, s) : launch_few_of<F16>(x, p, s);
 }
 
 }  // namespace qsdp_train

@@ -92,25 +92,28 @@ def _operands(m, n, k, square, seed=0):
     ac, bc = qb.alloc_blocks(m, k, False, DEV)[:2], qb.alloc_blocks(n, k, square, DEV)[:2]
     qb.qsdp_quantize_blocks(a.to(DEV), False, *ac)
     qb.qsdp_quantize_blocks(b.to(DEV), square, *bc)
-    ha = held(ac[0].float().cpu()[:, :k], ac[1].cpu().t(), 1, 128)
-    hb = held(bc[0].float().cpu()[:, :k], bc[1].cpu().t(), 128 if square else 1, 128)
+    ha = held(ac[0].float()[:, :k], ac[1].t(), 1, 128)  # on the GPU, where products in 64 bits are quick
+    hb = held(bc[0].float()[:, :k], bc[1].t(), 128 if square else 1, 128)
     return a, ac, bc, ha, hb
 
 
 # m, n, k of products that reach every kernel
-PRODUCTS = [(1, 1, 1), (1, 64, 128), (3, 65, 129), (16, 100, 300), (17, 63, 127), (1, 2048, 2048), (33, 4097, 640), (64, 64, 1024),
-            (65, 127, 513), (130, 129, 256), (200, 1000, 2048), (513, 300, 4096), (1000, 1024, 384)]
+SMALL = [(1, 1, 1), (1, 64, 128), (3, 65, 129), (16, 100, 300), (17, 63, 127), (1, 2048, 2048), (16, 8200, 260), (5, 32805, 130),
+         (2, 40, 5000), (33, 4097, 640), (64, 64, 1024), (65, 127, 513), (130, 129, 256), (200, 1000, 2048), (513, 300, 4096),
+         (1000, 1024, 384)]
+LARGE = [(1930, 1950, 100), (1921, 1921, 200), (1920, 2000, 300), (1930, 1950, 1030), (3850, 3830, 4100), (3841, 3841, 4353)]
+PRODUCTS = SMALL + LARGE
 
 
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
 @pytest.mark.parametrize("square", [True, False])
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_products(m, n, k, square, dtype):
-    if m * n * k > 1 << 28 and dtype == "f16":
+    if (m, n, k) in LARGE and dtype == "f16":
         pytest.skip("the large ones in two formats")
     _, ac, bc, ha, hb = _operands(m, n, k, square, m + n + k)
     bias = matrix(1, n, torch.float32, seed=8)[0]
-    want, off = product(ha, hb, dtype == "f32")
+    want, off = (t.cpu() for t in product(ha, hb, dtype == "f32"))
     y = torch.full((m, n + 3), 2.0, dtype=DTYPES[dtype], device=DEV)
     qb.qsdp_matmul_blocks(*ac, *bc, k, bias.to(DEV), y[:, :n])
     assert bool((y[:, n:] == 2.0).all())
@@ -129,7 +132,9 @@ def test_linear(m, n, k, dtype, out):
     x = matrix(m, k, DTYPES[dtype], 3, 1, m + n, 2.0)
     _, _, bc, _, hb = _operands(1, n, k, True, 3)
     bias = matrix(1, n, torch.float32, seed=8)[0]
-    want, off = product(held(*blocks(x, 1, 128), 1, 128), hb, out == "f32")
+    if (m, n, k) in LARGE and dtype == "f16":
+        pytest.skip("the large ones in three formats")
+    want, off = (t.cpu() for t in product(held(*blocks(x, 1, 128), 1, 128).to(DEV), hb, out == "f32"))
     flat = torch.full((m * (n + 5) + 1,), 2.0, dtype=DTYPES[out], device=DEV)
     y = flat[1:].view(m, n + 5)
     qb.qsdp_linear_blocks(to_gpu(x), *bc, bias.to(DEV), y[:, :n])
