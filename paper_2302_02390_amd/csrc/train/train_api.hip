@@ -126,27 +126,32 @@ int qsdp_quantize_blocks(const void* x, qsdp_dtype dtype, uint64_t rows, uint64_
 }
 
 size_t qsdp_matmul_blocks_bytes(uint64_t m, uint64_t n, uint64_t k) {
-    (void)m, (void)n, (void)k;
-    return 0;
+    if (!product_ok(m, n, k)) return 0;
+    const uint64_t parts = choose_parts(m, n, k);
+    return parts > 1 ? parts * m * n * sizeof(float) : 0;
 }
 
 int qsdp_matmul_blocks(const uint8_t* a, const float* a_scales, uint64_t m, const uint8_t* b, const float* b_scales, int b_square,
                        uint64_t n, uint64_t k, const float* bias, qsdp_dtype out_dtype, void* y, uint64_t y_row_stride,
                        int accumulate, void* workspace, uint64_t workspace_bytes, void* stream) {
-    (void)workspace_bytes;
     if (!known(out_dtype) || !product_ok(m, n, k) || !stride_ok(m, n, y_row_stride)) return QSDP_EINVAL;
     if (m == 0) return QSDP_OK;
     if (!a || !a_scales || !b || !b_scales || !y) return QSDP_EINVAL;
     if (!aligned(a, 16) || !aligned(a_scales, 4) || !aligned(b, 16) || !aligned(b_scales, 4) || !aligned(bias, 4) ||
         !aligned(y, width(out_dtype)) || !aligned(workspace, 16))
         return QSDP_EALIGN;
+    const size_t bytes = qsdp_matmul_blocks_bytes(m, n, k);
+    const bool shared = bytes && workspace && workspace_bytes >= bytes;
     const ProductParams p = {a, a_scales, m, m, b, b_scales, n, k, pitch_of(k), bias, out_dtype, y, y_row_stride,
-                             accumulate != 0};
+                             accumulate != 0, shared ? static_cast<float*>(workspace) : nullptr, 0, 0};
     return status_of(launch_product(b_square != 0, p, static_cast<hipStream_t>(stream)));
 }
 
 size_t qsdp_linear_blocks_bytes(uint64_t m, uint64_t n, uint64_t k) {
-    return product_ok(m, n, k) ? rounded_bytes(m, k) + qsdp_matmul_blocks_bytes(m, n, k) : 0;
+    if (!product_ok(m, n, k)) return 0;
+    if (m > kFewRows) return rounded_bytes(m, k) + qsdp_matmul_blocks_bytes(m, n, k);
+    const uint64_t parts = choose_few_parts(n, k);
+    return parts > 1 ? parts * m * n * sizeof(float) : 16;
 }
 
 int qsdp_linear_blocks(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k, uint64_t row_stride, const uint8_t* w,
@@ -162,7 +167,8 @@ int qsdp_linear_blocks(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k, 
         !aligned(y, width(out_dtype)) || !aligned(workspace, 16))
         return QSDP_EALIGN;
     if (m <= kFewRows) {
-        const ProductParams p = {nullptr, nullptr, m, m, w, w_scales, n, k, pitch_of(k), bias, out_dtype, y, y_row_stride, false};
+        const ProductParams p = {nullptr, nullptr, m, m, w, w_scales, n, k, pitch_of(k), bias, out_dtype, y, y_row_stride, false,
+                                 static_cast<float*>(workspace), 0, 0};
         return status_of(launch_linear_few({x, dtype, row_stride}, p, static_cast<hipStream_t>(stream)));
     }
     uint8_t* codes = static_cast<uint8_t*>(workspace);

@@ -37,6 +37,9 @@ struct ProductParams {
     void* y;
     uint64_t y_stride;  // elements
     bool accumulate;
+    float* parts;  // workspace for the sums of parts of k, or none
+    uint32_t part_steps;
+    uint64_t part_elements;  // of a part's sums; both are the launch's
 };
 
 // Few rows of a product, as they come: rounded on the way, by every workgroup.

@@ -57,8 +57,32 @@ constexpr uint64_t norm_workgroups(uint64_t rows, uint64_t n) {
 // ---- products (train_product.hip) ------------------------------------------------------------------------------------------
 constexpr uint64_t kFewRows = 16;
 
-// Groups of 16 columns to a workgroup: more of them share the rounding of the rows, fewer fill the chip.
-constexpr int few_groups(uint64_t n) { return n >= 32768 ? 4 : n >= 8192 ? 2 : 1; }
+// Their kernels: workgroups that go through the columns, for rows whose codes fit into registers, or eight waves to 16 columns, or to 32,
+// which share the rounding, where that leaves enough workgroups. Time by n x k of 16 rows, WIDE against TWO: 24 us for 38 at
+// 50257 x 2048, 57 for 74 at 50257 x 4096, 10.1 for 9.7 at 16384 x 2048; TWO against ONE: 14.5 for 17.7 at 8192 x 4096, 7.7 for 7.1 at
+// 4096 x 2048.
+enum class FewKernel { ONE, TWO, WIDE };
+
+constexpr FewKernel choose_few(uint64_t n, uint64_t k) {
+    if (n >= 32768 && k <= 4096) return FewKernel::WIDE;
+    return n >= 8192 ? FewKernel::TWO : FewKernel::ONE;
+}
+
+// Parts of a sum over `steps` blocks, each with at least `least` of them and none empty, that different workgroups add up and one more
+// launch joins. Where `groups` workgroups fill the chip (256 or more) the parts cost more than they give.
+constexpr uint64_t parts_of(uint64_t groups, uint64_t steps, uint64_t least) {
+    const uint64_t by_steps = steps / least, by_groups = groups ? 448 / groups : 1;
+    const uint64_t parts = by_steps < by_groups ? by_steps : by_groups;
+    if (parts < 2) return 1;
+    const uint64_t each = (steps + parts - 1) / parts;
+    return (steps + each - 1) / each;
+}
+
+// Parts against none, by n x k: one row 11.3 us for 16.4 at 1024 x 16384, 10.1 for 11.3 at 2048 x 8192, 7.6 for 6.7 at 2048 x 4096; 16 rows
+// 12.5 for 15.1 at 2048 x 8192, 19.0 for 16.0 at 4096 x 8192.
+constexpr uint64_t choose_few_parts(uint64_t n, uint64_t k) {
+    return choose_few(n, k) == FewKernel::ONE ? parts_of((n + 15) / 16, (k + 127) / 128, 24) : 1;
+}
 
 enum class ProductTile { T64, T128, T256 };
 
@@ -67,6 +91,13 @@ constexpr ProductTile choose_tile(uint64_t m, uint64_t n, uint64_t k, bool exact
     const uint64_t of_128 = (m + 127) / 128 * ((n + 127) / 128), of_256 = (m + 255) / 256 * ((n + 255) / 256);
     if (!exact && of_256 >= 224 && k >= 4096) return ProductTile::T256;
     return of_128 >= 224 ? ProductTile::T128 : ProductTile::T64;
+}
+
+// Parts against none, results in 16 bits: 13.4 us for 21.8 at 125 x 2048 x 8192, 26 for 40 at 768 x 768 x 16384, 11.3 for 12.5 at
+// 125 x 2048 x 4096; of half the steps 9.4 for 7.9 at 125 x 2048 x 2048; of 256 tiles 17.8 for 13.2 at 1000 x 1024 x 4096.
+constexpr uint64_t choose_parts(uint64_t m, uint64_t n, uint64_t k) {
+    if (choose_tile(m, n, k, true) != ProductTile::T64) return 1;
+    return parts_of((m + 63) / 64 * ((n + 63) / 64), (k + 127) / 128, 16);
 }
 
 }  // namespace qsdp_train

@@ -137,7 +137,7 @@ __device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_
 // addresses that the lanes read from memory. A wave multiplies WN columns (first operand, four rows of whose result are in a lane) by
 // WM rows. Which columns a fragment has is free: every fourth four, so that a lane ends with WN / 4 neighbours of a row. It keeps a step's columns in registers and walks over the rows, sixteen at a time. While these are
 // multiplied the next sixteen come out of LDS and the sums before go into the result; with the last ones the next step begins.
-template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT>
+template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT, bool PARTS = false>
 __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(ProductParams p, uint32_t n_tiles, uint32_t m_tiles) {
     typedef Tile<TN, TM, WN, WM> S;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES][S::BYTES];
@@ -161,16 +161,22 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
         const uint64_t row = m0 + in < p.m ? in : p.m - 1 - m0;
         a_at[i] = (uint32_t)(row * p.pitch) + ((lane % 8) ^ (in % 8)) * 16;
     }
-    const uint8_t* b = p.b + n0 * p.pitch;
-    const uint8_t* a = p.a + m0 * p.pitch;
+    // the steps of this workgroup's part of the sum
+    uint32_t begin = 0, steps = (uint32_t)(p.pitch / kWide);
+    if constexpr (PARTS) {
+        begin = blockIdx.y * p.part_steps;
+        steps = steps - begin < p.part_steps ? steps - begin : p.part_steps;
+    }
+    const uint8_t* b = p.b + n0 * p.pitch + begin * kWide;
+    const uint8_t* a = p.a + m0 * p.pitch + begin * kWide;
     // Scales: 64 to a load; waves that have none of their own load another's again. A column has a scale of its own, or that of its
     // square block.
     const int a_part = wave % (TM / 64) * 64, b_part = wave % (TN / 64) * 64;
     const uint64_t of_row = m0 + a_part + lane < p.m ? m0 + a_part + lane : p.m - 1;
     const uint64_t of_column = n0 + b_part + lane < p.n ? n0 + b_part + lane : p.n - 1;
-    const float* a_scale = p.a_scale + of_row;
-    const float* b_scale = p.b_scale + (SQUARE ? of_column / kWide : of_column);
     const uint64_t b_scales = SQUARE ? blocks_of(p.n) : p.n;
+    const float* a_scale = p.a_scale + of_row + begin * p.a_rows;
+    const float* b_scale = p.b_scale + (SQUARE ? of_column / kWide : of_column) + begin * b_scales;
     // loads [from, to) of the wave's of a step
     auto fetch = [&](uint8_t* at, uint32_t s, int from, int to) __attribute__((always_inline)) {
         const uint32_t k0 = s * kWide;
@@ -193,7 +199,6 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
     const int first = (part ^ (r % 8)) * 16, second = ((4 + part) ^ (r % 8)) * 16;
     const int b_row = (wn + r / 4 * WIDTH + r % 4) * kWide, a_row = (TN + wm + r) * kWide, a_of = S::CODES + (wm + r) * 4;
     const int b_of = S::CODES + (TM + wn + (SQUARE ? 0 : part * WIDTH)) * 4;
-    const uint32_t steps = (uint32_t)(p.pitch / kWide);
     // the wave's loads of columns and their scales; and those up to the middle of the rows'
     constexpr bool EARLY = B >= 4;
     constexpr int OF_B = S::B_LOADS + 1, MIDDLE = OF_B + (S::A_LOADS + 1) / 2;
@@ -327,7 +332,7 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
     for (int e = 0; e < WIDTH; ++e) bias[e] = p.bias ? p.bias[n + (e < left ? e : 0)] : 0.0f;
     auto put = [&](auto* format) __attribute__((always_inline)) {
         typedef std::remove_pointer_t<decltype(format)> O;
-        auto* y = static_cast<typename O::raw*>(p.y) + n;
+        auto* y = static_cast<typename O::raw*>(p.y) + n + (PARTS ? blockIdx.y * p.part_elements : 0);
 #pragma unroll
         for (int j = 0; j < B; ++j) {
             const uint64_t m = m0 + wm + j * 16 + r;
@@ -338,21 +343,177 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
             put_row<O, A>(y + m * p.y_stride, v, left, p.accumulate);
         }
     };
-    if constexpr (EXACT) put((F32*)nullptr);
+    if constexpr (EXACT || PARTS) put((F32*)nullptr);
     else if (p.out == QSDP_BF16) put((BF16*)nullptr);
     else put((F16*)nullptr);
 }
 
 // ---- few rows --------------------------------------------------------------------------------------------------------------
-// Up to 16 rows: the weights' bytes bound the time. A workgroup takes 16 * GROUPS columns; its waves share the blocks of k, each with
-// loads of its own from memory into registers, a block ahead, and waits for nobody until the sums meet in LDS, in the order of the waves.
-// The rows are rounded where they are multiplied: a lane has the pieces of its row that it multiplies, and the four lanes of a row find
-// the block's largest together.
+// Up to 16 rows: the weights' bytes bound the time. The rows are rounded where they are multiplied: a lane has the pieces of its row
+// that it multiplies, and the four lanes of a row find the block's largest together.
 constexpr int kFewWaves = 8;
 
-template <class X, int GROUPS, bool EXACT>
+// The 32 elements of row `row` (from the lane's first piece on) that the lane multiplies in the block at k0: two pieces of 16.
+template <class X>
+__device__ __forceinline__ void load_pieces(Raw8<X> (&raw)[4], const typename X::raw* row, uint32_t k0, int left) {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        const int at = h / 2 * 64 + h % 2 * 8;
+        if (left > at) raw[h].load(row + k0 + at, left - at);
+        else raw[h].none();
+    }
+}
+
+// Their codes and the block's scale.
+template <class X>
+__device__ __forceinline__ v8i round_pieces(const Raw8<X> (&raw)[4], float& scale) {
+    float most = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(raw[e / 8].at(e % 8)));
+    most = fmaxf(largest_of_rows(most), kLeastBlock);
+    const float up = kMostCode / most;
+    scale = most / kMostCode;
+    v8i codes;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = raw[h].at(e) * up;
+        const u32x2 two = codes8(w);
+        codes[2 * h] = (int)two[0];
+        codes[2 * h + 1] = (int)two[1];
+    }
+    return codes;
+}
+
+// Columns part * 4 ... of row r, of 16. Without a bias nothing is waited for that is on its way.
+template <bool EXACT>
+__device__ __forceinline__ void put_few(const ProductParams& p, v4f total, uint64_t n0, int lane) {
+    const int r = lane % 16;
+    const uint64_t n = n0 + lane / 16 * 4;
+    if (n >= p.n || (uint64_t)r >= p.m) return;
+    const int left = p.n - n < 4 ? (int)(p.n - n) : 4;
+    const uint64_t at = r * p.y_stride + n;
+    auto put = [&](const float (&v)[4]) __attribute__((always_inline)) {
+        if constexpr (EXACT) put_row<F32, 1>(static_cast<float*>(p.y) + at, v, left, false);
+        else if (p.out == QSDP_BF16) put_row<BF16, 1>(static_cast<uint16_t*>(p.y) + at, v, left, false);
+        else put_row<F16, 1>(static_cast<_Float16*>(p.y) + at, v, left, false);
+    };
+    float v[4] = {total[0], total[1], total[2], total[3]};
+    if (p.bias) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] += p.bias[n + (c < left ? c : 0)];
+        put(v);
+    } else {
+        put(v);
+    }
+}
+
+// Many columns: a workgroup goes through them sixteen at a time. Its eight waves load their weights, runs of 2048 bytes of each, into LDS
+// while they multiply those before, and share the blocks of k; each rounds the rows' blocks that it multiplies once and keeps them in
+// registers. One barrier a run: behind it the run is there, and so are the sums of the columns before, which one wave writes out.
+constexpr int kRun = 2048;
+constexpr int kOnce = 2;  // the loads' policy: weights are read once and stay out of the caches' way (24.6 us for 27)
+
+template <class X, int RUNS, bool EXACT>
+__global__ __launch_bounds__(kFewWaves * 64, RUNS == 1 ? 4 : 2) void few_wide_kernel(FewRows x, ProductParams p, uint32_t groups) {
+    constexpr int EACH = kRun / (int)kWide / kFewWaves;  // blocks of a run that a wave multiplies
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2][16 * kRun];
+    __shared__ v4f meet[2][kFewWaves][64];
+    const int lane = threadIdx.x % 64, wave = wave_index(), r = lane % 16, part = lane / 16;
+    const uint32_t steps = (uint32_t)(p.pitch / kWide);
+    const uint64_t n_blocks = blocks_of(p.n);
+    // block t of run u for this wave: u * 16 + t * 8 + wave
+    const auto* row = static_cast<const typename X::raw*>(x.x) + ((uint64_t)r < p.m ? r : p.m - 1) * x.stride + part * 16;
+    uint32_t zero = 0;  // which the compiler does not know: the weights' scales are not scalar loads, which LDS would have to wait for
+    asm volatile("" : "+v"(zero));
+    float of_next[EACH];
+    auto fetch = [&](uint8_t* to, uint32_t group, int u) __attribute__((always_inline)) {
+        const uint64_t n0 = (uint64_t)group * 16;
+        const uint32_t k0 = u * kRun;
+#pragma unroll
+        for (int l = 0; l < 4; ++l) {  // half a run of a column
+            const int in = wave * 2 + l / 2;
+            const uint64_t of_row = n0 + in < p.n ? n0 + in : p.n - 1;
+            uint32_t k = k0 + l % 2 * 1024 + lane / 8 * kWide + ((lane % 8) ^ (in % 8)) * 16;
+            k = k < p.pitch ? k : k0;  // behind the row's end: what nobody multiplies
+            __builtin_amdgcn_global_load_lds((global_ptr)(p.b + of_row * p.pitch + k), (lds_ptr)(to + in * kRun + l % 2 * 1024), 16, 0, kOnce);
+        }
+#pragma unroll
+        for (int t = 0; t < EACH; ++t) {
+            const uint32_t s = u * (kRun / kWide) + t * kFewWaves + wave;
+            of_next[t] = p.b_scale[(s < steps ? s : steps - 1) * n_blocks + n0 / kWide + zero];
+        }
+    };
+    v8i codes[RUNS * EACH];
+    float scale[RUNS * EACH];
+#pragma unroll
+    for (int u = 0; u < RUNS; ++u) {
+        Raw8<X> raw[EACH][4];
+#pragma unroll
+        for (int t = 0; t < EACH; ++t) {
+            const uint32_t k0 = ((u * EACH + t) * kFewWaves + wave) * kWide;
+            load_pieces(raw[t], row, k0, (int)((int64_t)p.k - (int64_t)k0 - part * 16));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (u == 0) fetch(lds[0], blockIdx.x, 0);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < EACH; ++t) codes[u * EACH + t] = round_pieces(raw[t], scale[u * EACH + t]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    const int first = (part ^ (r % 8)) * 16, second = ((4 + part) ^ (r % 8)) * 16;
+    uint32_t turn = 0, place = 0;  // of the columns; of the run in LDS
+    auto put = [&](uint32_t group) __attribute__((always_inline)) {
+        const auto& sums = meet[(turn - 1) % 2];
+        v4f total = sums[0][lane];
+#pragma unroll
+        for (int w = 1; w < kFewWaves; ++w) total += sums[w][lane];
+        put_few<EXACT>(p, total, (uint64_t)group * 16, lane);
+    };
+    uint32_t before = 0;
+    for (uint32_t group = blockIdx.x; group < groups; group += gridDim.x) {
+        v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int u = 0; u < RUNS; ++u) {
+            wait_reads();  // what was read of the run before, and the sums' place in LDS
+            wait_loads<0>();
+            meet_here();
+            float of[EACH];
+#pragma unroll
+            for (int t = 0; t < EACH; ++t) of[t] = of_next[t];
+            const uint8_t* from = lds[place] + r * kRun + wave * kWide;
+            place ^= 1;
+            const bool next_columns = u + 1 == RUNS;
+            if (!next_columns || group + gridDim.x < groups)
+                fetch(lds[place], next_columns ? group + gridDim.x : group, next_columns ? 0 : u + 1);
+            if (u == 0 && turn && wave == (int)(turn % kFewWaves)) put(before);
+#pragma unroll
+            for (int t = 0; t < EACH; ++t) {
+                const int i = u * EACH + t;
+                if ((uint32_t)(i * kFewWaves + wave) >= steps) continue;
+                const v8i bv = fragment(from + t * kFewWaves * (int)kWide, first, second);
+                const v4f now = product(Operand<EXACT>(bv), Operand<EXACT>(codes[i]));
+                const float by = scale[i] * of[t];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sum[c] = fmaf(now[c], by, sum[c]);
+            }
+        }
+        // The sums of two groups have places in turn: those of the one before the last have been written out before the last barrier.
+        meet[turn % 2][wave][lane] = sum;
+        before = group;
+        ++turn;
+    }
+    wait_reads();
+    meet_here();
+    if (wave == (int)(turn % kFewWaves)) put(before);
+}
+
+// Few columns, or long rows: eight waves share the blocks of k of 16 * GROUPS columns, whose weights and rows each asks for a block ahead,
+// into registers. The sums meet in LDS, in the order of the waves.
+template <class X, int GROUPS, bool PARTS, bool EXACT>
 __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(FewRows x, ProductParams p) {
-    __shared__ v4f meet[kFewWaves][GROUPS][64];
+    __shared__ v4f meet[GROUPS][kFewWaves][64];
     const int lane = threadIdx.x % 64, wave = wave_index(), r = lane % 16, part = lane / 16;
     const uint64_t n0 = (uint64_t)blockIdx.x * (16 * GROUPS);
     const uint8_t* b[GROUPS];
@@ -362,12 +523,19 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(FewRows x, ProductP
         b[i] = p.b + (row < p.n ? row : p.n - 1) * p.pitch + part * 16;
     }
     const auto* row = static_cast<const typename X::raw*>(x.x) + ((uint64_t)r < p.m ? r : p.m - 1) * x.stride + part * 16;
-    const uint64_t n_blocks = blocks_of(p.n), in = n0 / kWide;  // 128 is a multiple of a workgroup's columns
-    const float* b_scale = p.b_scale + in;
-    const uint32_t steps = (uint32_t)(p.pitch / kWide);
+    const uint64_t n_blocks = blocks_of(p.n);
+    uint32_t zero = 0;  // as above
+    asm volatile("" : "+v"(zero));
+    const float* b_scale = p.b_scale + n0 / kWide + zero;  // 128 is a multiple of a workgroup's columns
+    uint32_t begin = 0, steps = (uint32_t)(p.pitch / kWide);  // the blocks of this workgroup's part of the sum
+    if constexpr (PARTS) {
+        begin = blockIdx.y * p.part_steps;
+        steps = steps - begin < p.part_steps ? steps : begin + p.part_steps;
+        p.y = static_cast<float*>(p.y) + blockIdx.y * p.part_elements;
+    }
     v4i codes[GROUPS][2];
     Raw8<X> raw[4];
-    float scale = 0.0f;
+    float of_b = 0.0f;
     auto fetch = [&](uint32_t s) __attribute__((always_inline)) {
         if (s >= steps) return;
         const uint32_t k0 = s * kWide;
@@ -376,43 +544,22 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(FewRows x, ProductP
             codes[i][0] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(b[i] + k0));
             codes[i][1] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(b[i] + k0 + 64));
         }
-        const int left = (int)(p.k - k0) - part * 16;
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            const int at = h / 2 * 64 + h % 2 * 8;
-            if (left > at) raw[h].load(row + k0 + at, left - at);
-            else raw[h].none();
-        }
-        scale = b_scale[s * n_blocks];
+        load_pieces(raw, row, k0, (int)(p.k - k0) - part * 16);
+        of_b = b_scale[s * n_blocks];
     };
     v4f sum[GROUPS];
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) sum[i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    fetch(wave);
-    for (uint32_t s = wave; s < steps; s += kFewWaves) {
+    fetch(begin + wave);
+    for (uint32_t s = begin + wave; s < steps; s += kFewWaves) {
         v8i bv[GROUPS];
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i) bv[i] = __builtin_shufflevector(codes[i][0], codes[i][1], 0, 1, 2, 3, 4, 5, 6, 7);
-        float v[32], most = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = raw[e / 8].at(e % 8);
-        const float of_b = scale;
+        Raw8<X> here[4] = {raw[0], raw[1], raw[2], raw[3]};
+        float of = of_b, scale;
         fetch(s + kFewWaves);
-#pragma unroll
-        for (int e = 0; e < 32; ++e) most = fmaxf(most, fabsf(v[e]));
-        most = fmaxf(largest_of_rows(most), kLeastBlock);
-        const float up = kMostCode / most, of = most / kMostCode * of_b;
-        v8i av;
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            float w[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = v[h * 8 + e] * up;
-            const u32x2 two = codes8(w);
-            av[2 * h] = (int)two[0];
-            av[2 * h + 1] = (int)two[1];
-        }
-        const Operand<EXACT> rows(av);
+        const Operand<EXACT> rows(round_pieces(here, scale));
+        of *= scale;
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i) {
             const v4f now = product(Operand<EXACT>(bv[i]), rows);
@@ -421,29 +568,38 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_kernel(FewRows x, ProductP
         }
     }
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) meet[wave][i][lane] = sum[i];
+    for (int i = 0; i < GROUPS; ++i) meet[i][wave][lane] = sum[i];
     __syncthreads();
     if (wave >= GROUPS) return;
-    v4f total = meet[0][wave][lane];
+    v4f total = meet[wave][0][lane];
 #pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) total += meet[w][wave][lane];
-    // columns part * 4 ... of row r
-    const uint64_t n = n0 + wave * 16 + part * 4;
-    if (n >= p.n || (uint64_t)r >= p.m) return;
+    for (int w = 1; w < kFewWaves; ++w) total += meet[wave][w][lane];
+    put_few<EXACT || PARTS>(p, total, n0 + wave * 16, lane);
+}
+
+// The parts' sums, in their order, and what a product does with its result. Four columns to a lane.
+template <class O>
+__global__ __launch_bounds__(256) void join_kernel(ProductParams p, uint32_t parts) {
+    const uint64_t across = (p.n + 3) / 4, at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= across * p.m) return;
+    const uint64_t m = at / across, n = at % across * 4;
     const int left = p.n - n < 4 ? (int)(p.n - n) : 4;
-    float v[4];
+    const float* from = p.parts + m * p.n + n;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (uint32_t i = 0; i < parts; ++i)
 #pragma unroll
-    for (int c = 0; c < 4; ++c) v[c] = total[c] + (p.bias ? p.bias[n + (c < left ? c : 0)] : 0.0f);
-    const uint64_t at = r * p.y_stride + n;
-    if constexpr (EXACT) put_row<F32, 1>(static_cast<float*>(p.y) + at, v, left, false);
-    else if (p.out == QSDP_BF16) put_row<BF16, 1>(static_cast<uint16_t*>(p.y) + at, v, left, false);
-    else put_row<F16, 1>(static_cast<_Float16*>(p.y) + at, v, left, false);
+        for (int c = 0; c < 4; ++c) v[c] += from[i * p.part_elements + (c < left ? c : 0)];
+    if (p.bias)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) v[c] += p.bias[n + (c < left ? c : 0)];
+    put_row<O, 1>(static_cast<typename O::raw*>(p.y) + m * p.y_stride + n, v, left, p.accumulate);
 }
 
 }  // namespace
 
-template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT>
-static hipError_t launch_tiles(const ProductParams& p, hipStream_t s) {
+template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT, bool PARTS = false>
+static hipError_t launch_tiles(const ProductParams& p, hipStream_t s, unsigned parts = 1) {
     const uint32_t n_tiles = (uint32_t)((p.n + TN - 1) / TN);
     const uint64_t m_tiles = (p.m + TM - 1) / TM;
     // in several launches where the tiles are more than a grid holds
@@ -455,7 +611,7 @@ static hipError_t launch_tiles(const ProductParams& p, hipStream_t s) {
         q.a_scale += first;
         q.m = p.m - first < now * TM ? p.m - first : now * TM;
         q.y = static_cast<uint8_t*>(p.y) + first * p.y_stride * (p.out == QSDP_F32 ? 4 : 2);
-        hipLaunchKernelGGL((tiles_kernel<TN, TM, WN, WM, STAGES, SQUARE, EXACT>), dim3(n_tiles * (unsigned)now),
+        hipLaunchKernelGGL((tiles_kernel<TN, TM, WN, WM, STAGES, SQUARE, EXACT, PARTS>), dim3(n_tiles * (unsigned)now, parts),
                            dim3(Tile<TN, TM, WN, WM>::THREADS), 0, s, q, n_tiles, (uint32_t)now);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
@@ -463,8 +619,38 @@ static hipError_t launch_tiles(const ProductParams& p, hipStream_t s) {
     return hipSuccess;
 }
 
+// `launch` of the parts' sums into the workspace, and their join.
+template <class F>
+static hipError_t launch_parts(const ProductParams& p, uint64_t parts, hipStream_t s, F launch) {
+    ProductParams q = p;
+    q.part_steps = (uint32_t)((blocks_of(p.k) + parts - 1) / parts);
+    q.part_elements = p.m * p.n;
+    q.bias = nullptr;
+    q.accumulate = false;
+    q.out = QSDP_F32;
+    q.y = p.parts;
+    q.y_stride = p.n;
+    const hipError_t e = launch(q);
+    if (e != hipSuccess) return e;
+    q.bias = p.bias;
+    q.accumulate = p.accumulate;
+    q.y = p.y;
+    q.y_stride = p.y_stride;
+    const dim3 grid((unsigned)(((p.n + 3) / 4 * p.m + 255) / 256)), block(256);
+    if (p.out == QSDP_F32) hipLaunchKernelGGL((join_kernel<F32>), grid, block, 0, s, q, (uint32_t)parts);
+    else if (p.out == QSDP_BF16) hipLaunchKernelGGL((join_kernel<BF16>), grid, block, 0, s, q, (uint32_t)parts);
+    else hipLaunchKernelGGL((join_kernel<F16>), grid, block, 0, s, q, (uint32_t)parts);
+    return hipGetLastError();
+}
+
 template <bool SQUARE, bool EXACT>
 static hipError_t launch_product_of(const ProductParams& p, hipStream_t s) {
+    if (p.parts) {
+        const uint64_t parts = choose_parts(p.m, p.n, p.k);
+        return launch_parts(p, parts, s, [&](const ProductParams& q) {
+            return launch_tiles<64, 64, 32, 32, 3, SQUARE, EXACT, true>(q, s, (unsigned)parts);
+        });
+    }
     switch (choose_tile(p.m, p.n, p.k, EXACT)) {
         case ProductTile::T64: return launch_tiles<64, 64, 32, 32, 3, SQUARE, EXACT>(p, s);
         case ProductTile::T128: return launch_tiles<128, 128, 64, 64, 2, SQUARE, EXACT>(p, s);
@@ -479,23 +665,43 @@ hipError_t launch_product(bool b_square, const ProductParams& p, hipStream_t s) 
     return b_square ? launch_product_of<true, false>(p, s) : launch_product_of<false, false>(p, s);
 }
 
-template <class X, int GROUPS>
-static hipError_t launch_few(const FewRows& x, const ProductParams& p, hipStream_t s) {
-    const dim3 grid((unsigned)((p.n + 16 * GROUPS - 1) / (16 * GROUPS))), block(kFewWaves * 64);
-    if (p.out == QSDP_F32) hipLaunchKernelGGL((few_kernel<X, GROUPS, true>), grid, block, 0, s, x, p);
-    else hipLaunchKernelGGL((few_kernel<X, GROUPS, false>), grid, block, 0, s, x, p);
+template <class X, bool EXACT>
+static hipError_t launch_few_of(const FewRows& x, const ProductParams& p, hipStream_t s) {
+    const uint32_t groups = (uint32_t)((p.n + 15) / 16);
+    const dim3 block(kFewWaves * 64);
+    switch (choose_few(p.n, p.k)) {
+        case FewKernel::WIDE: {
+            // To a compute unit two workgroups; one where two runs' codes take more than half of the registers (spilled: 67 us for 57 at
+            // 16 x 50257 x 4096).
+            const uint32_t most = p.k <= kRun ? 512 : 256;
+            const dim3 grid(groups < most ? groups : most);
+            if (p.k <= kRun) hipLaunchKernelGGL((few_wide_kernel<X, 1, EXACT>), grid, block, 0, s, x, p, groups);
+            else hipLaunchKernelGGL((few_wide_kernel<X, 2, EXACT>), grid, block, 0, s, x, p, groups);
+            break;
+        }
+        case FewKernel::TWO: hipLaunchKernelGGL((few_kernel<X, 2, false, EXACT>), dim3((groups + 1) / 2), block, 0, s, x, p); break;
+        case FewKernel::ONE: {
+            const uint64_t parts = choose_few_parts(p.n, p.k);
+            if (parts > 1)
+                return launch_parts(p, parts, s, [&](const ProductParams& q) {
+                    hipLaunchKernelGGL((few_kernel<X, 1, true, EXACT>), dim3(groups, (unsigned)parts), block, 0, s, x, q);
+                    return hipGetLastError();
+                });
+            hipLaunchKernelGGL((few_kernel<X, 1, false, EXACT>), dim3(groups), block, 0, s, x, p);
+            break;
+        }
+    }
     return hipGetLastError();
 }
 
 template <class X>
-static hipError_t launch_few_of(const FewRows& x, const ProductParams& p, hipStream_t s) {
-    const int groups = few_groups(p.n);
-    return groups == 4 ? launch_few<X, 4>(x, p, s) : groups == 2 ? launch_few<X, 2>(x, p, s) : launch_few<X, 1>(x, p, s);
+static hipError_t launch_few_to(const FewRows& x, const ProductParams& p, hipStream_t s) {
+    return p.out == QSDP_F32 ? launch_few_of<X, true>(x, p, s) : launch_few_of<X, false>(x, p, s);
 }
 
 hipError_t launch_linear_few(const FewRows& x, const ProductParams& p, hipStream_t s) {
-    if (x.dtype == QSDP_F32) return launch_few_of<F32>(x, p, s);
-    return x.dtype == QSDP_BF16 ? launch_few_of<BF16>(x, p, s) : launch_few_of<F16>(x, p, s);
+    if (x.dtype == QSDP_F32) return launch_few_to<F32>(x, p, s);
+    return x.dtype == QSDP_BF16 ? launch_few_to<BF16>(x, p, s) : launch_few_to<F16>(x, p, s);
 }
 
 }  // namespace qsdp_train

@@ -21,7 +21,9 @@ int main(int argc, char** argv) {
         std::sscanf(argv[i], "%lu,%lu,%lu,%lu", a, a + 1, a + 2, a + 3);
         switch (argv[1][0]) {
             case 'p': std::printf("%d\n", (int)choose_tile(a[0], a[1], a[2], a[3] != 0)); break;
-            case 'f': std::printf("%d\n", few_groups(a[0])); break;
+            case 'f': std::printf("%d\n", (int)choose_few(a[0], a[1])); break;
+            case 'P': std::printf("%lu\n", (unsigned long)choose_parts(a[0], a[1], a[2])); break;
+            case 'F': std::printf("%lu\n", (unsigned long)choose_few_parts(a[0], a[1])); break;
             case 'n': std::printf("%d\n", (int)choose_norm(a[0], a[1])); break;
             case 'b': std::printf("%d\n", (int)choose_norm_backward(a[0])); break;
             case 'w': std::printf("%lu\n", (unsigned long)norm_workgroups(a[0], a[1])); break;
@@ -48,8 +50,22 @@ def test_products_of_the_gpu_tests_reach_every_kernel(ask):
     import test_gpu_blocks as gpu
     for exact, expected in ((0, set(TILES)), (1, {"T64", "T128"})):
         assert {TILES[v] for v in ask("p", [(*p, exact) for p in gpu.PRODUCTS])} == expected
-    assert set(ask("f", [(n,) for m, n, _ in gpu.PRODUCTS if m <= 16])) == {1, 2, 4}
-    assert all(TILES[v] != "T256" for v in ask("p", [(1 << 20, 1 << 20, 1 << 20, 1)]))
+    few = [(n, k) for m, n, k in gpu.PRODUCTS if m <= 16]
+    kernels = ask("f", few)
+    assert set(kernels) == {0, 1, 2}
+    wide = [(n, k) for (n, k), v in zip(few, kernels) if v == 2]
+    assert any(k <= 2048 for _, k in wide) and any(k > 2048 for _, k in wide) and any(n > 512 * 16 for n, _ in wide)
+    assert {1, 2, 4} <= set(ask("P", gpu.PRODUCTS)) and {1, 2, 5} <= set(ask("F", few))
+
+
+def test_parts_of_a_sum_are_none_empty(ask):
+    cases = [(1, n, k) for n in (1, 100, 2048, 4096, 20000) for k in list(range(1, 6000, 127)) + [8192, 12345, 1 << 20]]
+    for what, args in (("P", cases), ("F", [c[1:] for c in cases])):
+        for (_, n, k), parts in zip(cases, ask(what, args)):
+            steps = -(-k // 128)
+            each = -(-steps // parts)
+            assert 1 <= parts <= steps and (parts - 1) * each < steps and -(-n // 64) * parts <= max(448, -(-n // 64))
+    assert ask("P", [(0, 100, 10000)]) == [1]
 
 
 def test_rows_of_the_gpu_tests_reach_every_kernel(ask):
