@@ -173,10 +173,10 @@ __global__ __launch_bounds__(1024) void norm_stream_kernel(NormParams p) {
 // Workgroup g takes the rows g, g + G, ... of its teams; a team holds its row of x and dy, and the sums over its rows of dy h
 // and dy for its columns, in registers. The teams' sums meet in LDS in their order, the workgroups' in a kernel after this one:
 // no atomics, so equal calls give equal bits.
-template <class X, class Y, int TEAM, int NV>
-__global__ __launch_bounds__(kNormThreads, 4) void norm_backward_kernel(NormBackwardParams p) {
-    constexpr int TEAMS = kNormThreads / TEAM;
-    __shared__ float scratch[2 * kNormThreads / 64];
+template <class X, class Y, int THREADS, int TEAM, int NV>
+__global__ __launch_bounds__(THREADS, THREADS / 256) void norm_backward_kernel(NormBackwardParams p) {
+    constexpr int TEAMS = THREADS / TEAM;
+    __shared__ float scratch[2 * THREADS / 64];
     __shared__ __attribute__((aligned(16))) float meet[TEAMS > 1 ? 2 * 8 * NV * TEAM : 1];
     const int n = (int)p.n, t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
     const auto* x = static_cast<const typename X::raw*>(p.x);
@@ -443,9 +443,9 @@ hipError_t launch_norm(qsdp_dtype x, qsdp_dtype y, NormParams p, hipStream_t s) 
     });
 }
 
-template <class X, class Y, int TEAM, int NV>
+template <class X, class Y, int THREADS, int TEAM, int NV>
 static hipError_t launch_backward_team(const NormBackwardParams& p, hipStream_t s) {
-    hipLaunchKernelGGL((norm_backward_kernel<X, Y, TEAM, NV>), dim3((unsigned)norm_workgroups(p.rows, p.n)), dim3(kNormThreads), 0,
+    hipLaunchKernelGGL((norm_backward_kernel<X, Y, THREADS, TEAM, NV>), dim3((unsigned)norm_workgroups(p.rows, p.n)), dim3(THREADS), 0,
                        s, p);
     return hipGetLastError();
 }
@@ -453,12 +453,12 @@ static hipError_t launch_backward_team(const NormBackwardParams& p, hipStream_t 
 template <class X, class Y>
 static hipError_t launch_norm_backward_of(const NormBackwardParams& p, hipStream_t s) {
     switch (choose_norm_backward(p.n)) {
-        case NormBackwardTeam::T64: return launch_backward_team<X, Y, 64, 1>(p, s);
-        case NormBackwardTeam::T128: return launch_backward_team<X, Y, 128, 1>(p, s);
-        case NormBackwardTeam::T256: return launch_backward_team<X, Y, 256, 1>(p, s);
-        case NormBackwardTeam::T512: return launch_backward_team<X, Y, 512, 1>(p, s);
-        case NormBackwardTeam::T1024: return launch_backward_team<X, Y, 1024, 1>(p, s);
-        case NormBackwardTeam::T1024_2: return launch_backward_team<X, Y, 1024, 2>(p, s);
+        case NormBackwardTeam::T64: return launch_backward_team<X, Y, kNormThreads, 64, 1>(p, s);
+        case NormBackwardTeam::T128: return launch_backward_team<X, Y, kNormThreads, 128, 1>(p, s);
+        case NormBackwardTeam::T256: return launch_backward_team<X, Y, kNormThreads, 256, 1>(p, s);
+        case NormBackwardTeam::T512: return launch_backward_team<X, Y, kNormThreads, 512, 1>(p, s);
+        case NormBackwardTeam::T1024: return launch_backward_team<X, Y, kNormThreads, 1024, 1>(p, s);
+        case NormBackwardTeam::T512_4: return launch_backward_team<X, Y, 512, 512, 4>(p, s);
         case NormBackwardTeam::STREAM: break;
     }
     // the sums first: dx may overwrite what they read

@@ -22,7 +22,9 @@ constexpr NormTeam choose_norm(uint64_t rows, uint64_t n) {
     return NormTeam::STREAM;
 }
 
-enum class NormBackwardTeam { T64, T128, T256, T512, T1024, T1024_2, STREAM };
+// T512_4: 32 elements to a thread of workgroups half as large, which have twice the registers each (4096 x 16384 in bf16 113 us; 152
+// with 1024 threads of 16 elements, which spilled; 233 read again from memory).
+enum class NormBackwardTeam { T64, T128, T256, T512, T1024, T512_4, STREAM };
 
 constexpr NormBackwardTeam choose_norm_backward(uint64_t n) {
     if (n <= 512) return NormBackwardTeam::T64;
@@ -30,7 +32,7 @@ constexpr NormBackwardTeam choose_norm_backward(uint64_t n) {
     if (n <= 2048) return NormBackwardTeam::T256;
     if (n <= 4096) return NormBackwardTeam::T512;
     if (n <= 8192) return NormBackwardTeam::T1024;
-    if (n <= 16384) return NormBackwardTeam::T1024_2;
+    if (n <= 16384) return NormBackwardTeam::T512_4;
     return NormBackwardTeam::STREAM;
 }
 

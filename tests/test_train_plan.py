@@ -8,9 +8,9 @@ from paper_2302_02390_amd import build as lib_build
 
 TILES = ["T64", "T128", "T256"]
 NORMS = ["T64", "T64_2", "T128_2", "T256_2", "T512_2", "T1024_2", "T1024_4", "SHORT", "STREAM"]
-BACKWARD = ["T64", "T128", "T256", "T512", "T1024", "T1024_2", "STREAM"]
+BACKWARD = ["T64", "T128", "T256", "T512", "T1024", "T512_4", "STREAM"]
 ROOM = {"T64": 512, "T64_2": 1024, "T128": 1024, "T128_2": 2048, "T256": 2048, "SHORT": 2048, "T256_2": 4096, "T512": 4096,
-        "T512_2": 8192, "T1024": 8192, "T1024_2": 16384, "T1024_4": 32768}
+        "T512_2": 8192, "T1024": 8192, "T512_4": 16384, "T1024_2": 16384, "T1024_4": 32768}
 SOURCE = r"""
 #include "train/train_plan.hpp"
 #include <cstdio>
