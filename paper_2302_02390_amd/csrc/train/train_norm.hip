@@ -177,7 +177,7 @@ template <class X, class Y, int THREADS, int TEAM, int NV>
 __global__ __launch_bounds__(THREADS, THREADS / 256) void norm_backward_kernel(NormBackwardParams p) {
     constexpr int TEAMS = THREADS / TEAM;
     __shared__ float scratch[2 * THREADS / 64];
-    __shared__ __attribute__((aligned(16))) float meet[TEAMS > 1 ? 2 * 8 * NV * TEAM : 1];
+    __shared__ __attribute__((aligned(16))) f32x4 meet[TEAMS > 1 ? TEAMS : 1][2][TEAMS > 1 ? TEAM : 1][2];  // the teams' sums for dw and db
     const int n = (int)p.n, t = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
     const auto* x = static_cast<const typename X::raw*>(p.x);
     const auto* dy = static_cast<const typename Y::raw*>(p.dy);
@@ -263,36 +263,32 @@ __global__ __launch_bounds__(THREADS, THREADS / 256) void norm_backward_kernel(N
         }
     }
     if (!p.partial) return;
-    if constexpr (TEAMS > 1) {
-        for (int other = 1; other < TEAMS; ++other) {
-            __syncthreads();
-            if (team == other)
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        meet[(i * 16 + e) * TEAM + t] = dw[i][e];
-                        meet[(i * 16 + 8 + e) * TEAM + t] = db[i][e];
-                    }
-            __syncthreads();
-            if (team == 0)
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        dw[i][e] += meet[(i * 16 + e) * TEAM + t];
-                        db[i][e] += meet[(i * 16 + 8 + e) * TEAM + t];
-                    }
-        }
-        if (team) return;
-    }
     float* to = p.partial + (uint64_t)blockIdx.x * 2 * p.n;
+    if constexpr (TEAMS > 1) {
+        static_assert(NV == 1, "a piece of a row to a thread");
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int k = (i * TEAM + t) * 8;
-        if (k >= n) continue;
-        store8<F32>(to + k, n - k, dw[i]);
-        store8<F32>(to + p.n + k, n - k, db[i]);
+        for (int h = 0; h < 2; ++h) {
+            meet[team][0][t][h] = f32x4{dw[0][4 * h], dw[0][4 * h + 1], dw[0][4 * h + 2], dw[0][4 * h + 3]};
+            meet[team][1][t][h] = f32x4{db[0][4 * h], db[0][4 * h + 1], db[0][4 * h + 2], db[0][4 * h + 3]};
+        }
+        __syncthreads();
+#pragma unroll
+        for (int c = threadIdx.x; c < 16 * TEAM; c += THREADS) {
+            const float* from = reinterpret_cast<const float*>(meet) + c;
+            float sum = from[0];
+#pragma unroll
+            for (int other = 1; other < TEAMS; ++other) sum += from[other * 16 * TEAM];
+            const int of = c / (8 * TEAM), k = c % (8 * TEAM);
+            if (k < n) to[of * p.n + k] = sum;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int k = (i * TEAM + t) * 8;
+            if (k >= n) continue;
+            store8<F32>(to + k, n - k, dw[i]);
+            store8<F32>(to + p.n + k, n - k, db[i]);
+        }
     }
 }
 
@@ -377,12 +373,12 @@ __global__ __launch_bounds__(256) void norm_total_kernel(const float* partial, u
     const int part = threadIdx.x / 16;
     float sum = 0.0f;
     if (at < 2 * n) {
-        for (uint64_t g = part; g < workgroups; g += 16 * 8) {
-            float v[8];
+        for (uint64_t g = part; g < workgroups; g += 16 * 16) {
+            float v[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = g + i * 16 < workgroups ? partial[(g + i * 16) * 2 * n + at] : 0.0f;
+            for (int i = 0; i < 16; ++i) v[i] = g + i * 16 < workgroups ? partial[(g + i * 16) * 2 * n + at] : 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += v[i];
+            for (int i = 0; i < 16; ++i) sum += v[i];
         }
     }
     sums[part][threadIdx.x % 16] = sum;
