@@ -301,7 +301,7 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
                     const int at = q - A;
                     if (FETCH && at >= 0 && at < SLOTS) fetch(here, s + 2, at * OF_B / SLOTS, (at + 1) * OF_B / SLOTS);
                     if (FETCH && last) fetch(here, s + 2, OF_B + i * (MIDDLE - OF_B) / A, OF_B + (i + 1) * (MIDDLE - OF_B) / A);
-                    if (NEXT && j == 0) fetch(there, s + 1, MIDDLE + i * (S::LOADS - MIDDLE) / A, MIDDLE + (i + 1) * (S::LOADS - MIDDLE) / A);
+                    if (NEXT && j == 0) fetch(there, FETCH || s + 1 < steps ? s + 1 : s, MIDDLE + i * (S::LOADS - MIDDLE) / A, MIDDLE + (i + 1) * (S::LOADS - MIDDLE) / A);
                     __builtin_amdgcn_sched_barrier(0);
                 } else if (FETCH && last && i == 0) {
                     fetch(here, s + STAGES, 0, S::LOADS);
@@ -319,17 +319,21 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
     const std::false_type no;
     uint32_t s = 0;
     for (; s + (EARLY ? 2 : STAGES) < steps; ++s) step(s, yes, yes);
-    for (; s + 1 < steps; ++s) step(s, no, yes);
-    step(s, no, no);
+    for (; s < steps; ++s) step(s, no, yes);
     add(A - 2, B - 1, A * B - 2, factor);
     add(A - 1, B - 1, A * B - 1, factor);
     // sum[i][j][c]: column wn + part * WIDTH + i * 4 + c of row wm + j * 16 + r
     const uint64_t n = n0 + wn + part * WIDTH;
     if (n >= p.n) return;
     const int left = p.n - n < WIDTH ? (int)(p.n - n) : WIDTH;
-    float bias[WIDTH];
+    if (p.bias) {
 #pragma unroll
-    for (int e = 0; e < WIDTH; ++e) bias[e] = p.bias ? p.bias[n + (e < left ? e : 0)] : 0.0f;
+        for (int e = 0; e < WIDTH; ++e) {
+            const float bias = p.bias[n + (e < left ? e : 0)];
+#pragma unroll
+            for (int j = 0; j < B; ++j) sum[e / 4][j][e % 4] += bias;
+        }
+    }
     auto put = [&](auto* format) __attribute__((always_inline)) {
         typedef std::remove_pointer_t<decltype(format)> O;
         auto* y = static_cast<typename O::raw*>(p.y) + n + (PARTS ? blockIdx.y * p.part_elements : 0);
@@ -339,7 +343,7 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
             if (m >= p.m) continue;
             float v[WIDTH];
 #pragma unroll
-            for (int e = 0; e < WIDTH; ++e) v[e] = sum[e / 4][j][e % 4] + bias[e];
+            for (int e = 0; e < WIDTH; ++e) v[e] = sum[e / 4][j][e % 4];
             put_row<O, A>(y + m * p.y_stride, v, left, p.accumulate);
         }
     };

@@ -47,14 +47,14 @@ def test_every_product_is_one_that_calls_reach(kernels):
 
 
 def test_registers_and_lds(kernels):
-    """Tiles of 256 spill behind their loop, where the results are written; rows of 32 elements to a thread spill what a step of the
-    loop keeps beside both tensors. Nothing else does, but few registers of the longest rows forward."""
+    """Tiles of 256 by blocks of a row spill four addresses; rows of 32 elements to a thread spill what a step of the loop keeps beside
+    both tensors. Nothing else does, but few registers of the longest rows forward."""
     for group, found in kernels.items():
         for (name, args), (registers, spilled, lds) in found.items():
             numbers = _numbers(args)
             allowed = 0
             if name == "tiles_kernel" and numbers[0] == 256:
-                allowed = 96
+                allowed = 0 if numbers[5] else 4
             elif name == "norm_backward_kernel" and numbers[-1] == 4:
                 allowed = 96 if "3F32" in args else 16
             elif name == "norm_kernel" and numbers[-1] == 4:
