@@ -767,12 +767,17 @@ int qsdp_layer_norm_backward(const void* x, qsdp_dtype dtype, uint64_t rows, uin
  * B [n, k] in square blocks (b_square != 0) or blocks of a row, codes and scales as above, the codes
  * past k zero in both. Forward: A = x, B = W. Gradient of x: A = dy, B = W transposed. Gradient of W:
  * A = dy transposed, B = x transposed. bias float[n], nullable. m < 2^31, n <= 2^26, k <= 2^20.
+ * y must not overlap an operand. In binary32 the products of codes are exact and sums are binary32; in
+ * 16 bits the matrix units add eight neighbours' products at a time, cut off 2^-14 of the largest and
+ * lower, which the rounding of y covers.
  *   workspace  qsdp_matmul_blocks_bytes(m, n, k) bytes, 16-byte aligned, let a call of few tiles and a
  *              long sum share the sum among workgroups (0 bytes: no use for one). Less or none is
- *              allowed and slower; the order of additions goes by whether it is given.
+ *              allowed and slower; the order of additions goes by whether it is given. Calls that can
+ *              run at once need one each, also those in captured graphs.
  *
- * qsdp_linear_blocks: y = x W^T + bias with W in square blocks, x [m, k] rounded on the way.
- *   workspace  qsdp_linear_blocks_bytes(m, n, k) bytes, 16-byte aligned
+ * qsdp_linear_blocks: y = x W^T + bias with W in square blocks, x [m, k] rounded on the way: up to 16
+ * rows by the product's workgroups themselves, more by a launch before it. m <= 2^26.
+ *   workspace  qsdp_linear_blocks_bytes(m, n, k) bytes, 16-byte aligned, needed (no preparation, not kept)
  */
 int qsdp_quantize_blocks(const void* x, qsdp_dtype dtype, uint64_t rows, uint64_t cols,
                          uint64_t row_stride, int square, uint8_t* codes, float* scales,
@@ -806,6 +811,8 @@ int qsdp_linear_blocks(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k, 
  * word 0 (for m) or 1 (for v) of the Philox block with counter (block, stream 3); block = 8 * first + the
  * block's number in its tensor. So each rounding is right in the mean over seeds; give every step
  * another one. A non-finite gradient makes its x non-finite and its block's moments unspecified.
+ * beta1, beta2 in [0, 1), eps a normal number (at least 2^-126), bias1, bias2 > 0, all finite. The quotient
+ * in u is within two units in its last place.
  *   table       DEVICE copy of a table that qsdp_adamw_build has completed, 8-byte aligned
  *   pieces      what that returned
  *   seed_dev    nullable device uint64, added to seed when the kernel starts

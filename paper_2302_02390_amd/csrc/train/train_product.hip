@@ -5,7 +5,7 @@
 // result: four multiplications and additions of a wave for each instruction, which run beside the next one.
 // That instruction aligns the products of eight neighbours of k to the largest of them and cuts off what lies some 15 bits below:
 // random operands' sums come out 1.3e-5 of their norm off (16 x 16 x 128 and 32 x 32 x 64 alike; codes within a factor of 2^9 are
-// exact). That is lost in 16-bit results, whose rounding is 2^-9 or 2^-12. Results in binary32 go by bf16 instructions
+// exact). That is lost in 16-bit results, whose rounding is off by up to 2^-8 or 2^-11. Results in binary32 go by bf16 instructions
 // (EXACT): every code is a bf16 number, the products are exact, and the matrix units take twice the time.
 #include <type_traits>
 
@@ -132,11 +132,15 @@ __device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_
 }
 
 // A workgroup computes TN columns x TM rows of y in steps of a block of 128. Both operands' codes go straight from memory into
-// LDS, two steps deep, and one barrier a step separates them. LDS holds rows of 128 bytes whose eight pieces of 16 are permuted by the
+// LDS, two or three steps deep, between one barrier a step (two where a step's columns make room early). LDS holds rows of 128 bytes whose eight pieces of 16 are permuted by the
 // row (piece c in place c ^ key), so that the rows of a fragment read the same piece from all banks; the permutation is in the
 // addresses that the lanes read from memory. A wave multiplies WN columns (first operand, four rows of whose result are in a lane) by
 // WM rows. Which columns a fragment has is free: every fourth four, so that a lane ends with WN / 4 neighbours of a row. It keeps a step's columns in registers and walks over the rows, sixteen at a time. While these are
-// multiplied the next sixteen come out of LDS and the sums before go into the result; with the last ones the next step begins.
+// multiplied the next sixteen come out of LDS and the sums before go into the result; with the last ones the next step begins. (The
+// last step begins a next one too, on what LDS and the last block hold: a copy of the step without it spilled 57-80 registers.)
+// Results in 16 bits are bound by the matrix units and the clock under their load: 8192 x 8192 x 8192 435-445 us, 2.5 PFLOP/s. Exact
+// ones by vector instructions, 5.6 for each of the matrix units', of which two convert codes and two scale and add: 8192 x 2048 x 8192
+// 250-270 us, 1.0-1.1 PFLOP/s, vector units busy in 78 % of the cycles, matrix units in 55 %.
 template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT, bool PARTS = false>
 __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(ProductParams p, uint32_t n_tiles, uint32_t m_tiles) {
     typedef Tile<TN, TM, WN, WM> S;
