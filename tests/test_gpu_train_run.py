@@ -210,6 +210,36 @@ def test_results_past_32_bits():
     assert near(y[-200:], *product(ha, hb, False))
 
 
+def test_more_workgroups_than_a_grid_has():
+    """Products of more than 2^20 tiles, and 2^20 rows that no team holds, go in several launches."""
+    m, n, k = (1 << 26) + 300, 130, 100
+    codes = torch.zeros((m, 128), dtype=torch.uint8, device=DEV)
+    codes[:, :k] = torch.randint(0, 0x70, (1, k), dtype=torch.uint8, device=DEV)
+    scales = torch.linspace(0.5, 1.0, m, device=DEV).view(1, m)
+    b = matrix(n, k, torch.bfloat16, seed=2, std=0.05)
+    bc = qb.alloc_blocks(n, k, True, DEV)
+    qb.qsdp_quantize_blocks(b.to(DEV), True, *bc)
+    y = torch.empty((m, n), dtype=torch.bfloat16, device=DEV)
+    qb.qsdp_matmul_blocks(codes, scales, *bc[:2], k, None, y)
+    hb = held(*blocks(b, 128, 128), 128, 128)
+    for rows in (slice(0, 200), slice((1 << 26) - 100, (1 << 26) + 300)):
+        ha = held(codes[rows, :k].view(torch.float8_e4m3fn).float().cpu(), scales[:, rows].t().cpu(), 1, 128)
+        assert near(y[rows], *product(ha, hb, False))
+    del codes, scales, y
+    rows, n = (1 << 20) + 3, 32769
+    x = torch.empty((rows, n), dtype=torch.bfloat16, device=DEV).normal_(generator=torch.Generator(DEV).manual_seed(1))
+    stats = torch.empty((rows, 2), device=DEV)
+    at = slice(rows - 5, rows)
+    before = x[at].cpu()
+    want, s, _, off, s_off, _ = norm(before, None, None, EPS)
+    dy = torch.empty_like(x)
+    qb.qsdp_layer_norm(x, None, None, EPS, dy, stats)
+    assert near(dy[at], want, off) and near(stats[at], s, s_off)
+    grads, offs = norm_grad(before, None, dy[at].cpu(), EPS)
+    qb.qsdp_layer_norm_backward(x, None, stats, dy, dy)
+    assert near(dy[at], grads["dx"], offs["dx"])
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_a_tensor_past_32_bits(bits):
     n = (1 << 32) + 5000
