@@ -131,16 +131,17 @@ __device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_
     m = band * kBand + in % high;
 }
 
-// A workgroup computes TN columns x TM rows of y in steps of a block of 128. Both operands' codes go straight from memory into
-// LDS, two or three steps deep, between one barrier a step (two where a step's columns make room early). LDS holds rows of 128 bytes whose eight pieces of 16 are permuted by the
-// row (piece c in place c ^ key), so that the rows of a fragment read the same piece from all banks; the permutation is in the
-// addresses that the lanes read from memory. A wave multiplies WN columns (first operand, four rows of whose result are in a lane) by
-// WM rows. Which columns a fragment has is free: every fourth four, so that a lane ends with WN / 4 neighbours of a row. It keeps a step's columns in registers and walks over the rows, sixteen at a time. While these are
-// multiplied the next sixteen come out of LDS and the sums before go into the result; with the last ones the next step begins. (The
-// last step begins a next one too, on what LDS and the last block hold: a copy of the step without it spilled 57-80 registers.)
-// Results in 16 bits are bound by the matrix units and the clock under their load: 8192 x 8192 x 8192 435-445 us, 2.5 PFLOP/s. Exact
-// ones by vector instructions, 5.6 for each of the matrix units', of which two convert codes and two scale and add: 8192 x 2048 x 8192
-// 250-270 us, 1.0-1.1 PFLOP/s, vector units busy in 78 % of the cycles, matrix units in 55 %.
+// A workgroup computes TN columns x TM rows of y in steps of a block of 128. Both operands' codes go straight from memory into LDS, two
+// or three steps deep, between one barrier a step (two where a step's columns make room early). LDS holds rows of 128 bytes whose eight
+// pieces of 16 are permuted by the row (piece c in place c ^ key), so that the rows of a fragment read the same piece from all banks; the
+// permutation is in the addresses that the lanes read from memory. A wave multiplies WN columns (first operand, four rows of whose result
+// are in a lane) by WM rows. Which columns a fragment has is free: every fourth four, so that a lane ends with WN / 4 neighbours of a
+// row. It keeps a step's columns in registers and walks over the rows, sixteen at a time. While these are multiplied the next sixteen
+// come out of LDS and the sums before go into the result; with the last ones the next step begins. (The last step begins a next one too,
+// on what LDS and the last block hold: a copy of the step without it spilled 57-80 registers.) Results in 16 bits are bound by the matrix
+// units and the clock under their load: 8192 x 8192 x 8192 435-445 us, 2.5 PFLOP/s. Exact ones by vector instructions, 4.6 for each of
+// the matrix units', of which two convert codes and two scale and add: 8192 x 2048 x 8192 250-270 us, 1.0-1.1 PFLOP/s, vector units busy
+// in 78 % of the cycles, matrix units in 55 %.
 template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT, bool PARTS = false>
 __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(ProductParams p, uint32_t n_tiles, uint32_t m_tiles) {
     typedef Tile<TN, TM, WN, WM> S;
@@ -263,9 +264,8 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
         for (int c = 0; c < 4; ++c)
             sum[i][j][c] = fmaf(now[at % 4][c], SQUARE ? of_a : of_a * of_b[SQUARE ? 0 : i][c], sum[i][j][c]);
     };
-    // One step; FETCH: a further one is asked for, NEXT: there is a next one. Without a branch, behind which the compiler would move the
-    // sums.
-    auto step = [&](uint32_t s, auto FETCH, auto NEXT) __attribute__((always_inline)) {
+    // One step; FETCH: a further one is asked for. Without a branch, behind which the compiler would move the sums.
+    auto step = [&](uint32_t s, auto FETCH) __attribute__((always_inline)) {
         uint8_t* here = lds[s % STAGES];
         uint8_t* there = lds[(s + 1) % STAGES];
 #pragma unroll
@@ -273,7 +273,7 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
             const int set = j % 2;
             const bool last = j + 1 == B;
             if (EARLY && j == 1 && FETCH) meet_here();  // all have this step's columns in registers
-            if (last && NEXT) {
+            if (last) {
                 // The next step is there for all waves, and all have read this one.
                 wait_reads();
                 if (FETCH) wait_loads<EARLY ? OF_B : (STAGES - 2) * S::LOADS>();
@@ -281,7 +281,7 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
                 meet_here();
             }
             const Operand<EXACT> rows(av[set]);
-            if (last && NEXT) {
+            if (last) {
                 read_a(there, 0, 0);
                 read_scales(there);
                 __builtin_amdgcn_sched_barrier(0);
@@ -294,7 +294,7 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
                 now[q % 4] = product(Operand<EXACT>(bv[i]), rows);
                 __builtin_amdgcn_sched_barrier(0);
                 if (last) {
-                    if (NEXT) read_b(there, i);
+                    read_b(there, i);
                 } else if (i == 0) {
                     read_a(here, j + 1, 1 - set);
                 }
@@ -305,7 +305,9 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
                     const int at = q - A;
                     if (FETCH && at >= 0 && at < SLOTS) fetch(here, s + 2, at * OF_B / SLOTS, (at + 1) * OF_B / SLOTS);
                     if (FETCH && last) fetch(here, s + 2, OF_B + i * (MIDDLE - OF_B) / A, OF_B + (i + 1) * (MIDDLE - OF_B) / A);
-                    if (NEXT && j == 0) fetch(there, FETCH || s + 1 < steps ? s + 1 : s, MIDDLE + i * (S::LOADS - MIDDLE) / A, MIDDLE + (i + 1) * (S::LOADS - MIDDLE) / A);
+                    if (j == 0)  // (the last step's own rows again, where there is no next one)
+                        fetch(there, FETCH || s + 1 < steps ? s + 1 : s, MIDDLE + i * (S::LOADS - MIDDLE) / A,
+                              MIDDLE + (i + 1) * (S::LOADS - MIDDLE) / A);
                     __builtin_amdgcn_sched_barrier(0);
                 } else if (FETCH && last && i == 0) {
                     fetch(here, s + STAGES, 0, S::LOADS);
@@ -319,11 +321,9 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
             }
         }
     };
-    const std::true_type yes;
-    const std::false_type no;
     uint32_t s = 0;
-    for (; s + (EARLY ? 2 : STAGES) < steps; ++s) step(s, yes, yes);
-    for (; s < steps; ++s) step(s, no, yes);
+    for (; s + (EARLY ? 2 : STAGES) < steps; ++s) step(s, std::true_type());
+    for (; s < steps; ++s) step(s, std::false_type());
     add(A - 2, B - 1, A * B - 2, factor);
     add(A - 1, B - 1, A * B - 1, factor);
     // sum[i][j][c]: column wn + part * WIDTH + i * 4 + c of row wm + j * 16 + r
