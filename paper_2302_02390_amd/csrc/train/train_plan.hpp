@@ -86,17 +86,20 @@ constexpr uint64_t choose_few_parts(uint64_t n, uint64_t k) {
     return choose_few(n, k) == FewKernel::ONE ? parts_of((n + 15) / 16, (k + 127) / 128, 24) : 1;
 }
 
-enum class ProductTile { T64, T128, T256 };
+enum class ProductTile { T64, T128, T256, T64_4 };
 
 // exact: results in binary32, whose operands take twice the registers in the 256-wide tile. T256 against T128, results in 16 bits:
 // 134 us for 150 at 8192 x 8192 x 2048, 84 for 90 with k = 1024, 60 for 60 with 512; 61 for 57 at 6144 x 4096 x 2048, one pass and a half.
 // T64 against T128: 13.8 us for 23 at 1000 x 1024 x 4096, 21.5 for 17.9 at 2048 x 2048 x 2048.
+// T64_4: four steps in LDS, of which a compute unit has room for two tiles, instead of three: 7.5 us for 8.3 at 333 x 4093 x 1000, 12.0 for
+// 13.1 at 1000 x 1024 x 4096, 12.1 for 10.5 at 1500 x 1500 x 1500 (576 tiles); exact ones of blocks of a row 23.2 for 20.8.
 constexpr ProductTile choose_tile(uint64_t m, uint64_t n, uint64_t k, bool exact) {
     const uint64_t of_128 = (m + 127) / 128 * ((n + 127) / 128), of_256 = (m + 255) / 256 * ((n + 255) / 256);
     // passes over the chip, whose compute units hold two of 128 or one of 256
     const uint64_t passes_128 = (of_128 + 511) / 512, passes_256 = (of_256 + 255) / 256;
     if (!exact && of_256 >= 224 && k >= 1024 && 9 * passes_256 <= 5 * passes_128) return ProductTile::T256;
-    return of_128 >= 224 ? ProductTile::T128 : ProductTile::T64;
+    if (of_128 >= 224) return ProductTile::T128;
+    return !exact && (m + 63) / 64 * ((n + 63) / 64) <= 512 ? ProductTile::T64_4 : ProductTile::T64;
 }
 
 // Parts against none, results in 16 bits: 13.4 us for 21.8 at 125 x 2048 x 8192, 26 for 40 at 768 x 768 x 16384, 11.3 for 12.5 at

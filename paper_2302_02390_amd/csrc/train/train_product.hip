@@ -656,7 +656,7 @@ static hipError_t launch_product_of(const ProductParams& p, hipStream_t s) {
     if (p.parts) {
         const uint64_t parts = choose_parts(p.m, p.n, p.k);
         return launch_parts(p, parts, s, [&](const ProductParams& q) {
-            return launch_tiles<64, 64, 32, 32, 3, SQUARE, EXACT, true>(q, s, (unsigned)parts);
+            return launch_tiles<64, 64, 32, 32, EXACT ? 3 : 4, SQUARE, EXACT, true>(q, s, (unsigned)parts);
         });
     }
     switch (choose_tile(p.m, p.n, p.k, EXACT)) {
@@ -664,6 +664,10 @@ static hipError_t launch_product_of(const ProductParams& p, hipStream_t s) {
         case ProductTile::T128: return launch_tiles<128, 128, 64, 64, 2, SQUARE, EXACT>(p, s);
         case ProductTile::T256:
             if constexpr (!EXACT) return launch_tiles<256, 256, 64, 128, 2, SQUARE, EXACT>(p, s);
+            break;
+        case ProductTile::T64_4:
+            if constexpr (!EXACT) return launch_tiles<64, 64, 32, 32, 4, SQUARE, EXACT>(p, s);
+            break;
     }
     return hipErrorInvalidValue;
 }

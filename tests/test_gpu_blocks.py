@@ -101,7 +101,7 @@ def _operands(m, n, k, square, seed=0):
 SMALL = [(1, 1, 1), (1, 64, 128), (3, 65, 129), (16, 100, 300), (17, 63, 127), (1, 2048, 2048), (16, 8200, 260), (5, 32805, 130),
          (2, 40, 5000), (3, 8195, 4200), (4, 700, 3000), (16, 32769, 4096), (7, 33000, 2200), (3, 1001, 6300), (16, 300, 16390),
          (33, 4097, 640), (64, 64, 1024), (65, 127, 513), (130, 129, 256), (200, 1000, 2048), (513, 300, 4096), (200, 130, 8200),
-         (1000, 1024, 384)]
+         (1000, 1024, 384), (1540, 1490, 650)]
 LARGE = [(1930, 1950, 100), (1921, 1921, 200), (1920, 2000, 300), (1930, 1950, 1030), (3850, 3830, 1030), (3850, 3830, 4100), (3841, 3841, 4353)]
 PRODUCTS = SMALL + LARGE
 

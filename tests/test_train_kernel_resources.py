@@ -33,10 +33,11 @@ def _numbers(args):
 
 def test_every_product_is_one_that_calls_reach(kernels):
     """Tiles by whether the weight's blocks are square, the result exact and the sum in parts: those of 256 in 16 bits alone, parts in
-    tiles of 64 alone."""
+    tiles of 64 alone, which hold four steps where the result is not exact (or three, if they are many)."""
     found = kernels["product"]
     tiles = {_numbers(args) for name, args in found if name == "tiles_kernel"}
-    expected = {(64, 64, 32, 32, 3, square, exact, parts) for square in (0, 1) for exact in (0, 1) for parts in (0, 1)}
+    expected = {(64, 64, 32, 32, 3, square, exact, parts) for square in (0, 1) for exact, parts in ((0, 0), (1, 0), (1, 1))}
+    expected |= {(64, 64, 32, 32, 4, square, 0, parts) for square in (0, 1) for parts in (0, 1)}
     expected |= {(128, 128, 64, 64, 2, square, exact, 0) for square in (0, 1) for exact in (0, 1)}
     expected |= {(256, 256, 64, 128, 2, square, 0, 0) for square in (0, 1)}
     assert tiles == expected

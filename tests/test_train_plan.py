@@ -6,7 +6,7 @@ import pytest
 
 from paper_2302_02390_amd import build as lib_build
 
-TILES = ["T64", "T128", "T256"]
+TILES = ["T64", "T128", "T256", "T64_4"]
 NORMS = ["T64", "T64_2", "T128_2", "T256_2", "T512_2", "T1024_2", "T1024_4", "SHORT", "STREAM"]
 BACKWARD = ["T64", "T128", "T256", "T512", "T1024", "T512_4", "STREAM"]
 ROOM = {"T64": 512, "T64_2": 1024, "T128": 1024, "T128_2": 2048, "T256": 2048, "SHORT": 2048, "T256_2": 4096, "T512": 4096,
