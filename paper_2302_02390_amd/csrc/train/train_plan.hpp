@@ -92,7 +92,7 @@ enum class ProductTile { T64, T128, T256, T64_4 };
 // 134 us for 150 at 8192 x 8192 x 2048, 84 for 90 with k = 1024, 60 for 60 with 512; 61 for 57 at 6144 x 4096 x 2048, one pass and a half.
 // T64 against T128: 13.8 us for 23 at 1000 x 1024 x 4096, 21.5 for 17.9 at 2048 x 2048 x 2048.
 // T64_4: four steps in LDS, of which a compute unit has room for two tiles, instead of three: 7.5 us for 8.3 at 333 x 4093 x 1000, 12.0 for
-// 13.1 at 1000 x 1024 x 4096, 12.1 for 10.5 at 1500 x 1500 x 1500 (576 tiles); exact ones of blocks of a row 23.2 for 20.8.
+// 13.1 at 1000 x 1024 x 4096, 12.1 for 10.5 at 1500 x 1500 x 1500 (576 tiles). Exact ones have two teams of waves instead.
 constexpr ProductTile choose_tile(uint64_t m, uint64_t n, uint64_t k, bool exact) {
     const uint64_t of_128 = (m + 127) / 128 * ((n + 127) / 128), of_256 = (m + 255) / 256 * ((n + 255) / 256);
     // passes over the chip, whose compute units hold two of 128 or one of 256

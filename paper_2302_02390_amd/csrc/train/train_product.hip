@@ -141,16 +141,18 @@ __device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_
 // on what LDS and the last block hold: a copy of the step without it spilled 57-80 registers.) Results in 16 bits are bound by the matrix
 // units and the clock under their load: 8192 x 8192 x 8192 435-445 us, 2.5 PFLOP/s. Exact ones by vector instructions, 4.6 for each of
 // the matrix units', of which two convert codes and two scale and add: 8192 x 2048 x 8192 250-270 us, 1.0-1.1 PFLOP/s, vector units busy
-// in 78 % of the cycles, matrix units in 55 %.
-template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT, bool PARTS = false>
-__global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(ProductParams p, uint32_t n_tiles, uint32_t m_tiles) {
+// in 78 % of the cycles, matrix units in 55 %. Two teams of waves share the steps of an exact tile of 64 and join their sums in LDS: 16.1 us
+// for 20.5 at 1000 x 1024 x 4096, 9.0 for 10.8 at 125 x 2048 x 2048 (in 16 bits 11.4 for 12.0 and 8.5 for 7.4 at 333 x 4093 x 1000).
+template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT, bool PARTS = false, int TEAMS = 1>
+__global__ __launch_bounds__((TN / WN) * (TM / WM) * TEAMS * 64, 2) void tiles_kernel(ProductParams p, uint32_t n_tiles, uint32_t m_tiles) {
     typedef Tile<TN, TM, WN, WM> S;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES][S::BYTES];
+    __shared__ __attribute__((aligned(1024))) uint8_t rings[TEAMS * STAGES][S::BYTES];
     constexpr int A = WN / 16, B = WM / 16, WIDTH = 4 * A;  // fragments; consecutive columns of a lane
     static_assert(B % 2 == 0 && A % 2 == 0, "fragments and products in turn");
     uint32_t n_tile, m_tile;
     place(blockIdx.x, n_tiles, m_tiles, n_tile, m_tile);
-    const int lane = threadIdx.x % 64, wave = wave_index();
+    const int lane = threadIdx.x % 64, wave = wave_index() % S::WAVES, team = wave_index() / S::WAVES;
+    uint8_t (*const lds)[S::BYTES] = rings + team * STAGES;
     const uint64_t n0 = (uint64_t)n_tile * TN, m0 = (uint64_t)m_tile * TM;
     // what the lane loads: a piece of 16 bytes of a row of eight; rows past the matrix are its last one
     uint32_t b_at[S::B_LOADS], a_at[S::A_LOADS];
@@ -172,6 +174,8 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
         begin = blockIdx.y * p.part_steps;
         steps = steps - begin < p.part_steps ? steps - begin : p.part_steps;
     }
+    const uint32_t all = steps;  // of all teams, which take them in turn
+    steps = (all + TEAMS - 1) / TEAMS;
     const uint8_t* b = p.b + n0 * p.pitch + begin * kWide;
     const uint8_t* a = p.a + m0 * p.pitch + begin * kWide;
     // Scales: 64 to a load; waves that have none of their own load another's again. A column has a scale of its own, or that of its
@@ -184,6 +188,7 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
     const float* b_scale = p.b_scale + (SQUARE ? of_column / kWide : of_column) + begin * b_scales;
     // loads [from, to) of the wave's of a step
     auto fetch = [&](uint8_t* at, uint32_t s, int from, int to) __attribute__((always_inline)) {
+        if constexpr (TEAMS > 1) s = s * TEAMS + team < all ? s * TEAMS + team : all - 1;
         const uint32_t k0 = s * kWide;
 #pragma unroll
         for (int l = from; l < to; ++l) {
@@ -288,6 +293,7 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
             }
             factor_before = factor;
             factor = SQUARE ? of[set] * (j ? of_b[0][0] : of_b_next[0][0]) : of[set];
+            if (TEAMS > 1 && s * TEAMS + team >= all) factor = 0.0f;  // another team's step again
 #pragma unroll
             for (int i = 0; i < A; ++i) {
                 const int q = j * A + i;
@@ -326,6 +332,25 @@ __global__ __launch_bounds__((TN / WN) * (TM / WM) * 64, 2) void tiles_kernel(Pr
     for (; s < steps; ++s) step(s, std::false_type());
     add(A - 2, B - 1, A * B - 2, factor);
     add(A - 1, B - 1, A * B - 1, factor);
+    if constexpr (TEAMS > 1) {
+        static_assert(TEAMS == 2, "one team's sums meet the other's");
+        v4f* meet = reinterpret_cast<v4f*>(rings) + threadIdx.x % (S::WAVES * 64);
+        static_assert(sizeof(rings) >= TN * TM * 4, "their room");
+        wait_reads();
+        meet_here();
+        if (team)
+#pragma unroll
+            for (int i = 0; i < A; ++i)
+#pragma unroll
+                for (int j = 0; j < B; ++j) meet[(i * B + j) * S::WAVES * 64] = sum[i][j];
+        wait_reads();
+        meet_here();
+        if (team) return;
+#pragma unroll
+        for (int i = 0; i < A; ++i)
+#pragma unroll
+            for (int j = 0; j < B; ++j) sum[i][j] += meet[(i * B + j) * S::WAVES * 64];
+    }
     // sum[i][j][c]: column wn + part * WIDTH + i * 4 + c of row wm + j * 16 + r
     const uint64_t n = n0 + wn + part * WIDTH;
     if (n >= p.n) return;
@@ -606,7 +631,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductParams p, uint32_t par
 
 }  // namespace
 
-template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT, bool PARTS = false>
+template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT, bool PARTS = false, int TEAMS = 1>
 static hipError_t launch_tiles(const ProductParams& p, hipStream_t s, unsigned parts = 1) {
     const uint32_t n_tiles = (uint32_t)((p.n + TN - 1) / TN);
     const uint64_t m_tiles = (p.m + TM - 1) / TM;
@@ -619,8 +644,8 @@ static hipError_t launch_tiles(const ProductParams& p, hipStream_t s, unsigned p
         q.a_scale += first;
         q.m = p.m - first < now * TM ? p.m - first : now * TM;
         q.y = static_cast<uint8_t*>(p.y) + first * p.y_stride * (p.out == QSDP_F32 ? 4 : 2);
-        hipLaunchKernelGGL((tiles_kernel<TN, TM, WN, WM, STAGES, SQUARE, EXACT, PARTS>), dim3(n_tiles * (unsigned)now, parts),
-                           dim3(Tile<TN, TM, WN, WM>::THREADS), 0, s, q, n_tiles, (uint32_t)now);
+        hipLaunchKernelGGL((tiles_kernel<TN, TM, WN, WM, STAGES, SQUARE, EXACT, PARTS, TEAMS>), dim3(n_tiles * (unsigned)now, parts),
+                           dim3(Tile<TN, TM, WN, WM>::THREADS * TEAMS), 0, s, q, n_tiles, (uint32_t)now);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -656,11 +681,11 @@ static hipError_t launch_product_of(const ProductParams& p, hipStream_t s) {
     if (p.parts) {
         const uint64_t parts = choose_parts(p.m, p.n, p.k);
         return launch_parts(p, parts, s, [&](const ProductParams& q) {
-            return launch_tiles<64, 64, 32, 32, EXACT ? 3 : 4, SQUARE, EXACT, true>(q, s, (unsigned)parts);
+            return launch_tiles<64, 64, 32, 32, EXACT ? 2 : 4, SQUARE, EXACT, true, EXACT ? 2 : 1>(q, s, (unsigned)parts);
         });
     }
     switch (choose_tile(p.m, p.n, p.k, EXACT)) {
-        case ProductTile::T64: return launch_tiles<64, 64, 32, 32, 3, SQUARE, EXACT>(p, s);
+        case ProductTile::T64: return launch_tiles<64, 64, 32, 32, EXACT ? 2 : 3, SQUARE, EXACT, false, EXACT ? 2 : 1>(p, s);
         case ProductTile::T128: return launch_tiles<128, 128, 64, 64, 2, SQUARE, EXACT>(p, s);
         case ProductTile::T256:
             if constexpr (!EXACT) return launch_tiles<256, 256, 64, 128, 2, SQUARE, EXACT>(p, s);

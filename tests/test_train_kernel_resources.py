@@ -32,14 +32,16 @@ def _numbers(args):
 
 
 def test_every_product_is_one_that_calls_reach(kernels):
-    """Tiles by whether the weight's blocks are square, the result exact and the sum in parts: those of 256 in 16 bits alone, parts in
-    tiles of 64 alone, which hold four steps where the result is not exact (or three, if they are many)."""
+    """Tiles by whether the weight's blocks are square, the result exact, the sum in parts, and teams: those of 256 in 16 bits alone,
+    parts in tiles of 64 alone, which hold four steps (or three, if they are many), or two teams' two where the result is exact."""
     found = kernels["product"]
     tiles = {_numbers(args) for name, args in found if name == "tiles_kernel"}
-    expected = {(64, 64, 32, 32, 3, square, exact, parts) for square in (0, 1) for exact, parts in ((0, 0), (1, 0), (1, 1))}
-    expected |= {(64, 64, 32, 32, 4, square, 0, parts) for square in (0, 1) for parts in (0, 1)}
-    expected |= {(128, 128, 64, 64, 2, square, exact, 0) for square in (0, 1) for exact in (0, 1)}
-    expected |= {(256, 256, 64, 128, 2, square, 0, 0) for square in (0, 1)}
+    both = (0, 1)
+    expected = {(64, 64, 32, 32, 2, square, 1, parts, 2) for square in both for parts in both}
+    expected |= {(64, 64, 32, 32, 4, square, 0, parts, 1) for square in both for parts in both}
+    expected |= {(64, 64, 32, 32, 3, square, 0, 0, 1) for square in both}
+    expected |= {(128, 128, 64, 64, 2, square, exact, 0, 1) for square in both for exact in both}
+    expected |= {(256, 256, 64, 128, 2, square, 0, 0, 1) for square in both}
     assert tiles == expected
     few = [(_numbers(args)) for name, args in found if name == "few_kernel"]
     assert sorted(few) == sorted([(groups, parts, exact) for groups, parts in ((1, 0), (1, 1), (2, 0)) for exact in (0, 1)] * 3)
