@@ -777,7 +777,8 @@ int qsdp_layer_norm_backward(const void* x, qsdp_dtype dtype, uint64_t rows, uin
  *              run at once need one each, also those in captured graphs.
  *
  * qsdp_linear_blocks: y = x W^T + bias with W in square blocks, x [m, k] rounded on the way: up to 16
- * rows by the product's workgroups themselves, more by a launch before it. m <= 2^26.
+ * rows by the product's workgroups themselves, more by a launch before it. m <= 2^26. Up to 16 rows have
+ * exact products and binary32 sums whatever the format of y.
  *   workspace  qsdp_linear_blocks_bytes(m, n, k) bytes, 16-byte aligned, needed (no preparation, not kept)
  */
 int qsdp_quantize_blocks(const void* x, qsdp_dtype dtype, uint64_t rows, uint64_t cols,
