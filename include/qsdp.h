@@ -812,7 +812,10 @@ int qsdp_linear_blocks(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k, 
  * element i of a block is (h + 1/2) / 2^12, h the upper 12 bits of (word + i * 0x9E3779B9) mod 2^32,
  * word 0 (for m) or 1 (for v) of the Philox block with counter (block, stream 3); block = 8 * first + the
  * block's number in its tensor. So each rounding is right in the mean over seeds; give every step
- * another one. A non-finite gradient makes its x non-finite and its block's moments unspecified.
+ * another one. A non-finite gradient makes its x non-finite and its block's moments unspecified. A finite
+ * one whose v overflows (|g| from about 2^64 / sqrt(1-beta2) on) gives u = 0 and an infinite v, which stays
+ * so and keeps u at 0; with 8 bits it is held as R = 2^64 and code 255, and where it shares a block any other
+ * v > 0 is held as (2^64 / 255^2)^2 at least. |m| / bias1 must not overflow.
  * beta1, beta2 in [0, 1), eps a normal number (at least 2^-126), bias1, bias2 > 0, all finite. The quotient
  * in u is within two units in its last place.
  *   table       DEVICE copy of a table that qsdp_adamw_build has completed, 8-byte aligned

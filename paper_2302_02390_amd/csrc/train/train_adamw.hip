@@ -19,6 +19,9 @@ namespace {
 
 constexpr float kMostM = 127.0f * 127.0f, kMostV = 255.0f * 255.0f;
 constexpr float kLeast = 0x1p-96f;  // a block whose largest value is below is kept as zeros
+// An infinite second moment, of a finite gradient whose square overflows, is held with this R: its code 255 stands for 2^64, whose square is
+// infinite again, codes up to 254 for finite squares. (With R = inf all other elements of the block would be infinite or NaN in the next step.)
+constexpr float kMostRoot = 0x1p64f;
 
 struct Step {
     float lr, beta1, beta2, rest1, rest2, eps, inverse1, inverse2, decay;
@@ -69,7 +72,7 @@ __device__ __forceinline__ void store4(void* p, uint64_t at, uint64_t n, const f
     }
 }
 
-// The root to nearest of numbers from 2^-96 on, in a third of the instructions that all numbers take: Newton's step for both the
+// The root to nearest of finite numbers from 2^-96 on, in a third of the instructions that all numbers take: Newton's step for both the
 // root and half its reciprocal, and the rest of the square (Markstein).
 __device__ __forceinline__ float root_of(float v) {
     const float y = __builtin_amdgcn_rsqf(v), s = v * y, h = 0.5f * y, e = fmaf(-h, s, 0.5f);
@@ -213,7 +216,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamWParams p) {
     for (int j = 0; j < 2; ++j) {
         const float m_unit = top[j].x * (1.0f / kMostM), v_unit = top[j].y * (1.0f / kMostV);
         const uint32_t biased = mc[j] ^ 0x80808080u;  // as unsigned bytes about 128
-        bool tiny = false;
+        bool special = false;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float c = (float)(uint8_t)(biased >> (e * 8)) - 128.0f, d = (float)(uint8_t)(vc[j] >> (e * 8));
@@ -221,17 +224,22 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamWParams p) {
             root[j][e] = r * r;
             m[j][e] = m_unit * (c * fabsf(c));
             s.moments(g[j][e], m[j][e], root[j][e]);
-            tiny |= root[j][e] < 0x1p-96f;
+            special |= !(root[j][e] >= kLeast && root[j][e] < __builtin_inff());
         }
-        if (__any(tiny)) {
+        if (__any(special)) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) root[j][e] = sqrtf(root[j][e]);
+            for (int e = 0; e < 4; ++e) {
+                const float exact = sqrtf(root[j][e]);
+                x[j][e] = s.weight(x[j][e], m[j][e], exact);
+                root[j][e] = fminf(exact, kMostRoot);
+            }
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) root[j][e] = root_of(root[j][e]);
+            for (int e = 0; e < 4; ++e) {
+                root[j][e] = root_of(root[j][e]);
+                x[j][e] = s.weight(x[j][e], m[j][e], root[j][e]);
+            }
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[j][e] = s.weight(x[j][e], m[j][e], root[j][e]);
         m_top[j] = fmaxf(fmaxf(fabsf(m[j][0]), fabsf(m[j][1])), fmaxf(fabsf(m[j][2]), fabsf(m[j][3])));
         v_top[j] = fmaxf(fmaxf(root[j][0], root[j][1]), fmaxf(root[j][2], root[j][3]));
         put_weights(t, at[j], x[j]);
