@@ -1,10 +1,10 @@
-"""Gradients of layer norm against differences along the gradients themselves, where a slope is a norm and
+"""Gradients of layer norm and of products in blocks against differences along the gradients themselves, where a slope is a norm and
 its bound a small part of it: a gradient that is missing, halved, of the wrong sign or wrong in one part fails."""
 import pytest
 import torch
 
 from paper_2302_02390_amd import binding as qb
-from train_util import DEV, DTYPES, matrix, norm, norm_grad
+from train_util import DEV, DTYPES, blocks, held, matrix, norm, norm_grad, product
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +50,24 @@ def test_layer_norm(rows, n, x, y, w):
     check(lambda v: f(xs, v, bias), weight.double(), dw, grads["dw"], offs["dw"], 1e-2, size, 0.0)
     check(lambda v: f(xs, weight, v), bias.double(), db, grads["db"], offs["db"], 1e-2, size, 0.0)
 
+
+@pytest.mark.parametrize("m,n,k,dtype", [(200, 260, 300, "bf16"), (333, 1000, 520, "f16"), (130, 500, 1100, "bf16")])
+def test_product(m, n, k, dtype):
+    """The product of what the codes stand for is linear in either side."""
+    x, w, dy = (matrix(r, c, DTYPES[dtype], seed=i, std=s) for i, (r, c, s) in enumerate(((m, k, 1.0), (n, k, 0.05), (m, n, 0.01))))
+    xq, dq, wq = qb.alloc_blocks(m, k, False, DEV), qb.alloc_blocks(m, n, False, DEV), qb.alloc_blocks(n, k, True, DEV)
+    for t, square, to in ((x, False, xq), (dy, False, dq), (w, True, wq)):
+        qb.qsdp_quantize_blocks(t.to(DEV), square, *to)
+    dx, dw = torch.empty((m, k), dtype=DTYPES[dtype], device=DEV), torch.empty((n, k), device=DEV)
+    qb.qsdp_matmul_blocks(*dq[:2], *wq[2:], n, None, dx)
+    qb.qsdp_matmul_blocks(*dq[2:], *xq[2:], m, None, dw)
+    hx, hw, hd = held(*blocks(x, 1, 128), 1, 128), held(*blocks(w, 128, 128), 128, 128), held(*blocks(dy, 1, 128), 1, 128)
+    want, off = product(hd, hw.t().contiguous(), False)
+    off = off + want.abs() * torch.finfo(dx.dtype).eps / 2 + torch.finfo(dx.dtype).smallest_normal * torch.finfo(dx.dtype).eps
+    size = float((hx.abs() @ hw.abs().t() * hd.abs()).sum())
+    check(lambda v: float((v @ hw.t() * hd).sum()), hx, dx, want, off, 1.0, size, 0.0)
+    # the weight's gradient rounds dy and x along their columns: its own held values
+    ht, hdt = held(*blocks(x.t(), 1, 128), 1, 128), held(*blocks(dy.t(), 1, 128), 1, 128)
+    want, off = product(hdt, ht, True)
+    size = float((ht.t().abs() @ hw.abs().t() * hdt.t().abs()).sum())
+    check(lambda v: float((ht.t() @ v.t() * hdt.t()).sum()), hw, dw, want, off, 1.0, size, 0.0)
