@@ -30,3 +30,54 @@ def test_few_rows_keep_what_large_terms_leave(m, n, k, dtype):
     qb.qsdp_linear_blocks(x.to(DTYPES[dtype]).to(DEV), *codes, None, y)
     want = torch.tensor(13.0 * -(-k // 128)).to(y.dtype).float()
     assert bool((y.float().cpu() == want).all()), (y.float().unique().tolist()[:8], float(want))
+
+
+def _rounded(x, square=False):
+    codes = qb.alloc_blocks(*x.shape, square, DEV)[:2]
+    qb.qsdp_quantize_blocks(x.to(DEV), square, *codes)
+    return codes
+
+
+# m, n, k of many rows, one of each kind of tile and a sum in parts
+MANY = [(200, 300, 520), (1930, 1950, 260), (3850, 3830, 1030), (700, 3000, 128), (64, 70, 8200)]
+
+
+@pytest.mark.parametrize("m,n,k", MANY)
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_what_is_cut_off_is_cut_towards_zero(m, n, k, dtype):
+    """448 * 448 has its first bit at 2^17, so 13 beside it and its negative may lose what lies below 2^3: every block keeps 5 to 13
+    of it, and -13 keeps the same, negative. Binary32 results keep all."""
+    room = torch.empty(max(16, qb.matmul_blocks_bytes(m, n, k)), dtype=torch.uint8, device=DEV)
+    x = torch.zeros((m, -(-k // 128), 128))
+    x[:, :, :3] = torch.tensor([448.0, -448.0, 1.0])
+    a, blocks = _rounded(x.view(m, -1)[:, :k].contiguous()), -(-k // 128)
+    got = {}
+    for sign in (1.0, -1.0):
+        w = torch.zeros((n, blocks, 128))
+        w[:, :, :3] = torch.tensor([448.0, 448.0, 13.0 * sign])
+        b = _rounded(w.view(n, -1)[:, :k].contiguous())
+        for to in (dtype, "f32"):
+            y = torch.empty((m, n), dtype=DTYPES[to], device=DEV)
+            qb.qsdp_matmul_blocks(*a, *b, k, None, y, False, room)
+            got[to, sign] = y.float()
+        assert bool((got["f32", sign] == 13.0 * sign * blocks).all())
+        size, half = got[dtype, sign] * sign, 13.0 * blocks * torch.finfo(DTYPES[dtype]).eps / 2
+        assert bool((size >= 5.0 * blocks - half).all()) and bool((size <= 13.0 * blocks + half).all())
+    assert torch.equal(got[dtype, 1.0], -got[dtype, -1.0])
+
+
+@pytest.mark.parametrize("k", [1024, 65536])
+def test_signed_terms_take_the_cuts_out(k):
+    """Each product of normal operands is cut by less than 2^-14 of the largest of eight, whose square is (2.6)^2 times a product's in the
+    mean, towards zero, so with either sign alike: 2^-14 * 2.6 / sqrt 3 = 9.2e-5 of the norm at most, for any k, beside the rounding's
+    2.07e-4: together less than 1.1 times the rounding alone. Cuts to one side would add up, to 3e-4 at 65536."""
+    m = n = 512
+    gen = torch.Generator(DEV).manual_seed(k)
+    a, b = (torch.randn((r, k), device=DEV, generator=gen) for r in (m, n))
+    a, b = _rounded(a), _rounded(b)
+    held = lambda t: (t[0].double().view(m, -1, 128) * t[1].t().double()[:, :, None]).view(m, k)
+    want = held(a) @ held(b).t().contiguous()
+    y = torch.empty((m, n), dtype=torch.float16, device=DEV)
+    qb.qsdp_matmul_blocks(*a, *b, k, None, y)
+    assert float((y.double() - want).norm()) <= 1.1 * float((want.half().double() - want).norm())
+
