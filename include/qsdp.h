@@ -773,7 +773,7 @@ int qsdp_layer_norm_backward(const void* x, qsdp_dtype dtype, uint64_t rows, uin
  * 1.3e-5 of their norm for any k, which adds less than 1 % to what the rounding of y is off, but where
  * large products of eight cancel, what they leave can lose digits that y has room for. The largest values
  * of two blocks that meet must have a product below 2^145, or what is summed over them may be an infinity
- * or a NaN.
+ * or a NaN, and from 2^-108 on, or the product of the scales is subnormal and loses digits.
  *   workspace  qsdp_matmul_blocks_bytes(m, n, k) bytes, 16-byte aligned, let a call of few tiles and a
  *              long sum share the sum among workgroups (0 bytes: no use for one). Less or none is
  *              allowed and slower; the order of additions goes by whether it is given. Calls that can

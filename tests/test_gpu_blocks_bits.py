@@ -81,3 +81,27 @@ def test_signed_terms_take_the_cuts_out(k):
     qb.qsdp_matmul_blocks(*a, *b, k, None, y)
     assert float((y.double() - want).norm()) <= 1.1 * float((want.half().double() - want).norm())
 
+
+@pytest.mark.parametrize("m", [1, 200])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("square", [False, True])
+def test_blocks_of_the_least_and_the_largest_scales(m, dtype, square):
+    """Largest values whose products are 2^-108 and 2^144, the limits that are stated. A scale is 2^e / 448 rounded, two of them and
+    their product: three roundings of 2^-24; codes 448 (first case) or 0.875 (second) are exact."""
+    n, k = 130, 256
+    for x, w, each in ((torch.full((m, k), 2.0 ** -54), torch.full((n, k), 2.0 ** -54), 128 * 2.0 ** -108),
+                       (torch.tensor([2.0 ** 72, 2.0 ** 63, 0.0]), torch.tensor([0.0, 2.0 ** 62, 2.0 ** 72]), 2.0 ** 125)):
+        if x.dim() == 1:
+            few, (x, w) = (x, w), (torch.zeros((r, 2, 128)) for r in (m, n))
+            x[:, :, :3], w[:, :, :3] = few
+            x, w = x.view(m, k), w.view(n, k)
+        a, b = _rounded(x), _rounded(w, square)
+        y = torch.empty((m, n), dtype=DTYPES[dtype], device=DEV)
+        qb.qsdp_matmul_blocks(*a, *b, k, None, y)
+        ys = [y]
+        if square:
+            ys.append(torch.empty_like(y))
+            qb.qsdp_linear_blocks(x.to(DEV), *b, None, ys[1])
+        for y in ys:  # two blocks: their sum and its rounding to the format
+            off = (3 + 1) * 2.0 ** -24 + torch.finfo(y.dtype).eps / 2
+            assert bool(((y.double() / (2 * each) - 1).abs() <= off).all()), (float(y[0, 0]), 2 * each)
