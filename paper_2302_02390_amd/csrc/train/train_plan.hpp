@@ -36,7 +36,7 @@ constexpr NormBackwardTeam choose_norm_backward(uint64_t n) {
     return NormBackwardTeam::STREAM;
 }
 
-// Threads of a backward workgroup, and the rows that it has at once.
+// Threads of a backward workgroup, and the rows that it has at once. (T512_4 has 512, for one row at a time.)
 constexpr int kNormThreads = 1024;
 constexpr uint64_t norm_rows_at_once(uint64_t n) {
     switch (choose_norm_backward(n)) {
@@ -93,6 +93,8 @@ enum class ProductTile { T64, T128, T256, T64_4 };
 // T64 against T128: 13.8 us for 23 at 1000 x 1024 x 4096, 21.5 for 17.9 at 2048 x 2048 x 2048.
 // T64_4: four steps in LDS, of which a compute unit has room for two tiles, instead of three: 7.5 us for 8.3 at 333 x 4093 x 1000, 12.0 for
 // 13.1 at 1000 x 1024 x 4096, 12.1 for 10.5 at 1500 x 1500 x 1500 (576 tiles). Exact ones have two teams of waves instead.
+// A tile counts whatever part of it the matrix fills: 17, 32 and 64 rows of 50257 x 2048 take tiles of 128, in 27.7, 28.0 and 30.1 us with
+// their rounding (binary32: 37.8, 38.5, 40.4), for 24 us of 16 rows by the kernels of few rows.
 constexpr ProductTile choose_tile(uint64_t m, uint64_t n, uint64_t k, bool exact) {
     const uint64_t of_128 = (m + 127) / 128 * ((n + 127) / 128), of_256 = (m + 255) / 256 * ((n + 255) / 256);
     // passes over the chip, whose compute units hold two of 128 or one of 256
