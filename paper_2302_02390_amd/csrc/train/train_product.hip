@@ -133,7 +133,7 @@ __device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_
 }
 
 // A workgroup computes TN columns x TM rows of y in steps of a block of 128. Both operands' codes go straight from memory into LDS, two
-// or three steps deep, between one barrier a step (two where a step's columns make room early). LDS holds rows of 128 bytes whose eight
+// to four steps deep, between one barrier a step (two where a step's columns make room early). LDS holds rows of 128 bytes whose eight
 // pieces of 16 are permuted by the row (piece c in place c ^ key), so that the rows of a fragment read the same piece from all banks; the
 // permutation is in the addresses that the lanes read from memory. A wave multiplies WN columns (first operand, four rows of whose result
 // are in a lane) by WM rows. Which columns a fragment has is free: every fourth four, so that a lane ends with WN / 4 neighbours of a
