@@ -727,7 +727,9 @@ int qsdp_linear_codes(const void* x, qsdp_dtype dtype, uint64_t m, uint64_t k,
  * weight, bias: [n] in w_dtype, which is QSDP_F32 or the format of y; a NULL one is 1 (0). y has
  * the format of x, or any where x is QSDP_F32; it may overwrite x where the formats and strides are
  * the same. stats, nullable: {mean, rstd} of each row, what the gradient needs. eps >= 0 (0 and a
- * constant row: NaN). A row with a NaN or an infinity: NaN. n <= 2^24.
+ * constant row: NaN). A row with a NaN or an infinity: NaN. n <= 2^24. Sums are binary32: that of a row and of
+ * its centred squares must stay below 2^128 and, for the gradient, |mean| rstd too; with eps = 0 the mean
+ * square must be 2^-126 at least. Rows beyond give finite or non-finite numbers that are not the formula's.
  */
 int qsdp_layer_norm(const void* x, qsdp_dtype dtype, uint64_t rows, uint64_t n, uint64_t row_stride,
                     const void* weight, const void* bias, qsdp_dtype w_dtype, float eps, void* y,
