@@ -141,8 +141,8 @@ __device__ __forceinline__ void place(uint32_t id, uint32_t n_tiles, uint32_t m_
 // come out of LDS and the sums before go into the result; with the last ones the next step begins. (The last step begins a next one too,
 // on what LDS and the last block hold: a copy of the step without it spilled 57-80 registers.) Results in 16 bits are bound by the matrix
 // units and the clock under their load: 8192 x 8192 x 8192 435-445 us, 2.5 PFLOP/s. Exact ones by vector instructions, 4.6 for each of
-// the matrix units', of which two convert codes and two scale and add: 8192 x 2048 x 8192 250-270 us, 1.0-1.1 PFLOP/s, vector units busy
-// in 78 % of the cycles, matrix units in 55 %. Two teams of waves share the steps of an exact tile of 64 and join their sums in LDS: 16.1 us
+// the matrix units', of which two convert codes and two scale and add: 8192 x 2048 x 8192 250-320 us, 0.9-1.1 PFLOP/s, vector units busy
+// in 75 % of the waves' time, matrix units in 53 %. Two teams of waves share the steps of an exact tile of 64 and join their sums in LDS: 16.1 us
 // for 20.5 at 1000 x 1024 x 4096, 9.0 for 10.8 at 125 x 2048 x 2048 (in 16 bits 11.4 for 12.0 and 8.5 for 7.4 at 333 x 4093 x 1000).
 template <int TN, int TM, int WN, int WM, int STAGES, bool SQUARE, bool EXACT, bool PARTS = false, int TEAMS = 1>
 __global__ __launch_bounds__((TN / WN) * (TM / WM) * TEAMS * 64, 2) void tiles_kernel(ProductParams p, uint32_t n_tiles, uint32_t m_tiles) {
